@@ -352,6 +352,124 @@ q4_status q4_dequantize(const int32_t* C, int64_t ldc, int32_t rows, int32_t col
                         float* R, int64_t ldr, void* stream);
 
 /*
+ * 8-bit floating point with a scale per 128 values, and the expert layer of a language model
+ * around its product.  Extension of the paper's scheme (Section II-A: one scale per matrix;
+ * Section II-B: integer values) to the operands such models are served and trained with.
+ *
+ * Codes are e4m3 (sign, 4 exponent bits with bias 7, 3 mantissa bits; largest value 448, no
+ * infinity, 0x7F / 0xFF = NaN), one per byte.  x ~= scale * code.  Scales are float32:
+ *   groups   one scale per 128 consecutive columns of a row (the last group may be shorter),
+ *            stored S[block of columns][row], pitch in elements >= rows;
+ *   blocks   one scale per 128 x 128 values, S[block of rows][block of columns], pitch in
+ *            elements >= ceil(cols / 128).
+ * Sums and scales' products are float32.  Everything below is asynchronous on `stream`,
+ * allocates nothing and checks its host-side arguments before anything is launched.  Numbers
+ * that live on the device (starts, slot, source, expert numbers) are bounds-checked by the
+ * kernels: what lies outside its range is treated as absent, nothing outside a buffer is touched.
+ */
+typedef enum { Q4_F32 = 0, Q4_BF16 = 1, Q4_F16 = 2 } q4_type;
+
+#define Q4_F8_BLOCKS 1   /* q4_f8_quantize: a scale per 128 x 128 block instead of per group       */
+#define Q4_F8_POW2   2   /* q4_f8_quantize: scales rounded up to powers of two                     */
+#define Q4_F8_B_ROWS 4   /* q4_gemm_f8: SB holds Bt's rows by group, [ceil(K/128)][N], not by block */
+
+/*
+ * Codes and scales of a matrix X [rows x cols] (x_type a q4_type, pitch ldx elements):
+ *   a = max(max |x| over the group or block, 2^-60),  s = a / 448 (float32 division),
+ *   code = e4m3(x * (448 / a)), both roundings to nearest even;
+ * with Q4_F8_POW2: s rounded up to a power of two and code = e4m3(x / s).
+ * Q [rows][ldq bytes], S: the codes and their scales.  Qt [cols][ldqt bytes], St: the same of X
+ * transposed (its groups run along 128 rows of X), taken from the same read; for a weight matrix
+ * quantized by blocks both share the scales.  Either pair may be NULL, not both.
+ * source (device, [rows], or NULL): row r is made from row source[r] / topk of X, which has
+ * x_rows rows; a negative or too large entry gives a row of zeros.  With q4_expert_sort's
+ * `source` this is the gather of tokens in expert order.  Without source, topk and x_rows are
+ * ignored.  A group that holds a NaN or an infinity gets a scale that is not finite.
+ */
+q4_status q4_f8_quantize(const void* X, int32_t x_type, int64_t ldx, int32_t rows, int32_t cols,
+                         const int32_t* source, int32_t topk, int32_t x_rows, int32_t flags,
+                         uint8_t* Q, int64_t ldq, float* S, int64_t lds,
+                         uint8_t* Qt, int64_t ldqt, float* St, int64_t ldst, void* stream);
+
+/*
+ * Product of such operands:
+ *   C[m][n] = sum_b SA[b][m] * SB(n, b) * sum_{k in block b} A[m][k] * Bt[n][k]
+ * A [M][lda], Bt [N][ldb] (bytes, depth-contiguous), SA by group; SB by 128 x 128 block of Bt
+ * (weights), or by group with Q4_F8_B_ROWS (both operands activations, as in the gradient of a
+ * weight matrix).  C [M x N], c_type a q4_type, pitch ldc elements, rounded once.
+ * Forward: A = input, Bt = weights [out][in].  Gradient of the input: A = the output's gradient,
+ * Bt = the transposed weights (Qt of q4_f8_quantize).  Gradient of the weights: both operands the
+ * transposed codes (Qt, St), depth = tokens, Q4_F8_B_ROWS.
+ * Fast path: A, Bt 16-byte aligned and lda, ldb multiples of 16; anything else runs a slower
+ * general kernel.
+ */
+q4_status q4_gemm_f8(const uint8_t* A, int64_t lda, const float* SA, int64_t ldsa,
+                     const uint8_t* Bt, int64_t ldb, const float* SB, int64_t ldsb, int32_t flags,
+                     void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K,
+                     void* stream);
+
+/*
+ * The product by experts: rows starts[e] .. starts[e + 1] of A and C (starts: device, E + 1
+ * non-decreasing values of 0 .. M) are multiplied with expert e's weights, rows e * N .. of Bt
+ * [E * N][ldb], whose scales are rows e * ceil(N / 128) .. of SB.  Rows of C outside every segment
+ * are left untouched; experts without rows cost nothing.  E <= Q4_MAX_EXPERTS.
+ */
+q4_status q4_gemm_f8_experts(const uint8_t* A, int64_t lda, const float* SA, int64_t ldsa,
+                             const uint8_t* Bt, int64_t ldb, const float* SB, int64_t ldsb,
+                             const int32_t* starts, int32_t E,
+                             void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K,
+                             void* stream);
+
+/*
+ * The gradient of the experts' weights: C_e [M x N] = A[:, seg e] * Bt[:, seg e]^T over the depth
+ * segment starts[e] .. starts[e + 1] of A [M][lda] and Bt [N][ldb], both scaled by group along the
+ * depth K (Qt, St of q4_f8_quantize over rows in expert order).  Segments begin on multiples of 128
+ * (q4_expert_sort with align = 128), so that no group spans two experts; a start that does not is
+ * rounded down.  C is [E * M][ldc]; an expert without rows gets zeros.
+ */
+q4_status q4_gemm_f8_experts_wgrad(const uint8_t* A, int64_t lda, const float* SA, int64_t ldsa,
+                                   const uint8_t* Bt, int64_t ldb, const float* SB, int64_t ldsb,
+                                   const int32_t* starts, int32_t E,
+                                   void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K,
+                                   void* stream);
+
+/*
+ * Tokens sorted by expert: ids [n] (n = tokens * topk pairs, pair i = token i / topk) holds expert
+ * numbers; values outside 0 .. E - 1 mean that the pair is dropped.  Pairs of one expert keep their
+ * order.  Expert e's segment starts at starts[e] (starts [E + 1], multiples of align) and holds its
+ * pairs first, then, up to starts[e + 1], rows of no pair.
+ *   source [rows]  pair of each row, -1 where there is none (also behind the last segment)
+ *   slot   [n]     row of each pair, -1 if dropped
+ * rows >= q4_expert_sort_rows(n, E, align).  ws: q4_expert_sort_workspace_bytes(n, E) bytes, 4-byte
+ * aligned (may be NULL when that is 0).  1 <= E <= Q4_MAX_EXPERTS, 1 <= align <= 65536.
+ */
+#define Q4_MAX_EXPERTS 1024
+q4_status q4_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t align, int32_t* starts,
+                         int32_t* source, int32_t rows, int32_t* slot,
+                         void* ws, size_t ws_bytes, void* stream);
+size_t    q4_expert_sort_workspace_bytes(int32_t n, int32_t E);
+int64_t   q4_expert_sort_rows(int32_t n, int32_t E, int32_t align);
+
+/*
+ * Rows between token order and expert order; type a q4_type, D values per row, pitches in elements,
+ * sums in float32 and in the order of j, one rounding.  w [tokens][topk] float32 or NULL (= 1).
+ *   q4_expert_gather        Xs[r] = w[source[r]] * X[source[r] / topk], zeros where source[r] < 0
+ *   q4_expert_combine       Out[t] = sum_j w[t][j] * Y[slot[t][j]], dropped pairs left out
+ *   q4_expert_combine_grad  dY[slot[t][j]] = w[t][j] * dOut[t], zeros in rows with source[r] < 0;
+ *                           dw[t][j] = sum_d dOut[t][d] * Y[slot[t][j]][d], 0 for dropped pairs
+ * `rows` is the number of rows on the experts' side (Xs, Y, dY, source).  The gradient of the
+ * unweighted gather is q4_expert_combine with w = NULL.
+ */
+q4_status q4_expert_gather(const void* X, int64_t ldx, int32_t type, int32_t D, int32_t tokens, int32_t topk,
+                           const int32_t* source, int32_t rows, const float* w, void* Xs, int64_t ldxs, void* stream);
+q4_status q4_expert_combine(const void* Y, int64_t ldy, int32_t type, int32_t D, int32_t rows,
+                            const int32_t* slot, const float* w, int32_t tokens, int32_t topk,
+                            void* Out, int64_t ldo, void* stream);
+q4_status q4_expert_combine_grad(const void* dOut, int64_t ldd, const void* Y, int64_t ldy, int32_t type, int32_t D,
+                                 int32_t rows, const int32_t* source, const int32_t* slot, const float* w,
+                                 int32_t tokens, int32_t topk, void* dY, int64_t lddy, float* dw, void* stream);
+
+/*
  * q4_gemm with HOST operands: copies A and Bt to the device, runs q4_gemm and
  * copies C back, then synchronizes `stream`.  The work is ordered behind `stream`
  * and goes in row slices over `stream` and one stream of the library's own (created

@@ -64,6 +64,7 @@ static unsigned* status_ptr()
 }
 
 unsigned* device_status_ptr() { return status_ptr(); }
+int kernel_variant() { return variant(); }
 
 static q4_status check_gemm(const uint8_t* A, int64_t lda, const uint8_t* Bt, int64_t ldb,
                             int32_t M, int32_t N, int32_t K, int32_t za, int32_t zb)

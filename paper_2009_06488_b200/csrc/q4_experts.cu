@@ -1,0 +1,335 @@
+// The expert layer around the experts' products: tokens sorted by expert, rows gathered in that
+// order, and the weighted sum back to token order with its gradient.
+//
+// Sort: a counting sort of n = tokens * topk expert numbers that keeps pairs of one expert in their
+// order.  Every warp owns a contiguous piece of the pairs; with base[warp][e] = the first row of expert
+// e that is the warp's, it walks its piece 32 pairs at a time, and a pair's row is base + the number of
+// lower lanes with the same expert (match).  The bases are a scan over experts (segments rounded up to
+// `align`), over the chunks of other thread blocks (counted by a first kernel) and over the warps.  All
+// counts are integers: the result does not depend on any order of execution.
+// Bound: latency (two short kernels; one for up to kOneBlock pairs).
+//
+// Rows: a row's D values are spread over up to 256 threads, 8 (16 bytes of a 16-bit type) each; a token's
+// topk rows are loaded before they are summed, in order and in binary32.  Bound: HBM.
+#include "q4_f8.cuh"
+
+namespace q4 {
+namespace experts {
+
+constexpr int NW = 16;                     // warps of a sort block
+constexpr int64_t kOneBlock = 4096;        // pairs per block; up to as many are sorted by one block
+constexpr int kMaxChunks = 128;
+
+static int chunks_of(int64_t n)
+{
+    const int64_t g = (n + kOneBlock - 1) / kOneBlock;
+    return (int)(g < 1 ? 1 : g > kMaxChunks ? kMaxChunks : g);
+}
+
+__global__ void __launch_bounds__(512)
+count_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int64_t chunk, int32_t* __restrict__ hist)
+{
+    extern __shared__ int32_t cnt[];       // [E]
+    for (int e = threadIdx.x; e < E; e += blockDim.x) cnt[e] = 0;
+    __syncthreads();
+    const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
+    for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
+        const int e = ids[i];
+        if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) hist[(int64_t)blockIdx.x * E + e] = cnt[e];
+}
+
+__global__ void __launch_bounds__(NW * 32)
+place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t align, int64_t chunk,
+             const int32_t* __restrict__ hist, int32_t* __restrict__ starts, int32_t* __restrict__ source,
+             int32_t rows, int32_t* __restrict__ slot)
+{
+    extern __shared__ int32_t sm[];
+    int32_t* base = sm;                    // [NW][E]: counts of a warp's piece, then its next row
+    int32_t* total = sm + NW * E;          // [E] pairs of an expert
+    int32_t* before = total + E;           // [E] of them in earlier chunks
+    int32_t* first = before + E;           // [E + 1] first row of an expert
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
+    const int64_t piece = ((chunk + NW - 1) / NW + 31) / 32 * 32;
+    const int64_t wlo = min(hi, lo + warp * piece), whi = min(hi, wlo + piece);
+
+    for (int i = threadIdx.x; i < NW * E; i += blockDim.x) base[i] = 0;
+    __syncthreads();
+    for (int64_t i = wlo + lane; i < whi; i += 32) {
+        const int e = ids[i];
+        if (e >= 0 && e < E) atomicAdd(&base[warp * E + e], 1);
+    }
+    for (int e = threadIdx.x; hist && e < E; e += blockDim.x) {
+        int b = 0, t = 0;
+        for (int c = 0; c < (int)gridDim.x; ++c) {
+            const int h = hist[(int64_t)c * E + e];
+            if (c < (int)blockIdx.x) b += h;
+            t += h;
+        }
+        total[e] = t;
+        before[e] = b;
+    }
+    __syncthreads();
+    if (!hist) {
+        for (int e = threadIdx.x; e < E; e += blockDim.x) {
+            int t = 0;
+            for (int w = 0; w < NW; ++w) t += base[w * E + e];
+            total[e] = t;
+            before[e] = 0;
+        }
+        __syncthreads();
+    }
+    if (warp == 0) {
+        int at = 0;
+        for (int e0 = 0; e0 < E; e0 += 32) {
+            const int e = e0 + lane;
+            const int t = e < E ? (total[e] + align - 1) / align * align : 0;
+            int s = t;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xFFFFFFFFu, s, o);
+                if (lane >= o) s += u;
+            }
+            if (e < E) first[e] = at + s - t;
+            at += __shfl_sync(0xFFFFFFFFu, s, 31);
+        }
+        if (lane == 0) first[E] = at;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        int at = first[e] + before[e];
+        for (int w = 0; w < NW; ++w) {
+            const int c = base[w * E + e];
+            base[w * E + e] = at;
+            at += c;
+        }
+    }
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= E; e += blockDim.x) starts[e] = first[e];
+    // rows that no pair takes: behind each expert's pairs, and behind the last segment
+    for (int e = (int)blockIdx.x + warp * (int)gridDim.x; e < E; e += NW * (int)gridDim.x)
+        for (int r = first[e] + total[e] + lane; r < first[e + 1]; r += 32) if (r < rows) source[r] = -1;
+    for (int64_t r = (int64_t)first[E] + blockIdx.x * blockDim.x + threadIdx.x; r < rows; r += (int64_t)gridDim.x * blockDim.x)
+        source[r] = -1;
+    __syncthreads();
+
+    for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
+        const int64_t i = i0 + lane;
+        int e = i < whi ? ids[i] : -1;
+        if (e >= E || e < 0) e = -1;
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
+        const int r = e >= 0 ? base[warp * E + e] + __popc(same & ((1u << lane) - 1u)) : -1;
+        if (i < whi) {
+            slot[i] = r;
+            if (e >= 0 && r < rows) source[r] = (int32_t)i;
+        }
+        __syncwarp();
+        if (e >= 0 && (int)(__ffs(same) - 1) == lane) base[warp * E + e] += __popc(same);
+        __syncwarp();
+    }
+}
+
+// ------------------------------------------------------------------------------------- rows
+// A block's 256 threads are TY rows (or tokens) of TX threads, TX a power of two of 8..256.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+gather_kernel(const ExpertRowsParams p, int tx_bits)
+{
+    using T = typename f8::Elem<TYPE>::T;
+    const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
+    const int64_t r = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
+    if (r >= p.rows) return;
+    const int pair = p.source[r], t = pair / p.topk;
+    const bool on = pair >= 0 && t < p.tokens;
+    const float w = on && p.w ? p.w[pair] : 1.0f;
+    const T* src = static_cast<const T*>(p.X) + (on ? t * p.ldx : 0);
+    T* dst = static_cast<T*>(p.out) + r * p.ldo;
+    for (int c = tx * 8; c < p.D; c += TX * 8) {
+        const int n = min(8, p.D - c);
+        float v[8];
+        f8::load8(src + c, on ? n : 0, p.vec, v);
+        if (p.w) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= w;
+        }
+        f8::store8(dst + c, n, p.vec, v);
+    }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+combine_kernel(const ExpertRowsParams p, int tx_bits)
+{
+    using T = typename f8::Elem<TYPE>::T;
+    const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
+    const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
+    if (t >= p.tokens) return;
+    const int c = (blockIdx.y * TX + tx) * 8;
+    if (c >= p.D) return;
+    const int n = min(8, p.D - c);
+    float acc[8] = {};
+    for (int j0 = 0; j0 < p.topk; j0 += 8) {
+        float v[8][8], w[8];
+        bool on[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = j0 + j < p.topk;
+            const int s = in ? p.slot[t * p.topk + j0 + j] : -1;
+            on[j] = s >= 0 && s < p.rows;
+            w[j] = on[j] && p.w ? p.w[t * p.topk + j0 + j] : 1.0f;
+            f8::load8(static_cast<const T*>(p.Y) + (on[j] ? s * p.ldy + c : 0), on[j] ? n : 0, p.vec, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (on[j])
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
+    }
+    f8::store8(static_cast<T*>(p.out) + t * p.ldo + c, n, p.vec, acc);
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
+{
+    using T = typename f8::Elem<TYPE>::T;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float zero[8] = {};
+    if ((int)blockIdx.x >= token_blocks) {
+        // rows that belong to no pair get zeros: 32 rows per warp
+        const int64_t r0 = ((int64_t)blockIdx.x - token_blocks) * 256 + warp * 32;
+        const int pair = r0 + lane < p.rows ? p.source[r0 + lane] : 0;
+        unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0);
+        for (; none; none &= none - 1) {
+            T* dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
+            for (int c = lane * 8; c < p.D; c += 256) f8::store8(dst + c, min(8, p.D - c), p.vec, zero);
+        }
+        return;
+    }
+    __shared__ float part[8][8];
+    const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
+    const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
+    const bool mine = t < p.tokens;
+    const T* g = static_cast<const T*>(p.X) + (mine ? t * p.ldx : 0);
+    for (int j0 = 0; j0 < p.topk; j0 += 8) {
+        int s[8];
+        float w[8], dot[8] = {};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = mine && j0 + j < p.topk;
+            s[j] = in ? p.slot[t * p.topk + j0 + j] : -1;
+            if (s[j] >= p.rows) s[j] = -1;
+            w[j] = s[j] >= 0 && p.w ? p.w[t * p.topk + j0 + j] : 1.0f;
+        }
+        for (int c = tx * 8; mine && c < p.D; c += TX * 8) {
+            const int n = min(8, p.D - c);
+            float d[8], y[8][8];
+            f8::load8(g + c, n, p.vec, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                f8::load8(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, p.vec, y[j]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (s[j] < 0) continue;
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dot[j] = fmaf(d[i], y[j][i], dot[j]);
+                    o[i] = w[j] * d[i];
+                }
+                f8::store8(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, p.vec, o);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            for (int o = min(TX, 32) >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
+            if (TX > 32 && lane == 0) part[warp][j] = dot[j];
+        }
+        if (TX > 32) {
+            __syncthreads();
+            if (tx < 8) {
+                float sum = 0.0f;
+                for (int k = 0; k < TX / 32; ++k) sum += part[warp + k][tx];
+                if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = sum;
+            }
+            __syncthreads();
+        } else if (tx == 0 && mine) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) if (j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
+        }
+    }
+}
+
+static int tx_bits_of(int D)
+{
+    int b = 3;
+    while (b < 8 && (8 << b) < D) ++b;
+    return b;
+}
+
+}  // namespace experts
+
+using namespace experts;
+
+size_t expert_sort_ws_bytes(int64_t n, int32_t E)
+{
+    const int g = chunks_of(n);
+    return g == 1 ? 0 : (size_t)g * (size_t)E * 4;
+}
+
+cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t align, int32_t* starts, int32_t* source,
+                               int32_t rows, int32_t* slot, void* ws, cudaStream_t st)
+{
+    const int g = chunks_of(n);
+    const int64_t chunk = ((int64_t)n + g - 1) / g;
+    const size_t smem = ((size_t)(NW + 3) * E + 1) * 4;
+    const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (NW + 3) * 1024 * 4 + 4);
+    if (e != cudaSuccess) return e;
+    int32_t* hist = static_cast<int32_t*>(ws);
+    if (g > 1) {
+        count_kernel<<<g, 512, (size_t)E * 4, st>>>(ids, n, E, chunk, hist);
+        count_launch();
+    }
+    place_kernel<<<g, NW * 32, smem, st>>>(ids, n, E, align, chunk, g > 1 ? hist : nullptr, starts, source, rows, slot);
+    count_launch();
+    return cudaGetLastError();
+}
+
+cudaError_t launch_expert_gather(const ExpertRowsParams& p, cudaStream_t st)
+{
+    const int b = tx_bits_of(p.D), ty = 256 >> b;
+    const unsigned grid = (unsigned)(((int64_t)p.rows + ty - 1) / ty);
+    if (p.type == Q4_F32) gather_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b);
+    else if (p.type == Q4_BF16) gather_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b);
+    else gather_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b);
+    count_launch();
+    return cudaGetLastError();
+}
+
+cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st)
+{
+    const int b = tx_bits_of(p.D), ty = 256 >> b;
+    const dim3 grid((unsigned)(((int64_t)p.tokens + ty - 1) / ty), (unsigned)((p.D + (8 << b) - 1) / (8 << b)));
+    if (p.type == Q4_F32) combine_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b);
+    else if (p.type == Q4_BF16) combine_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b);
+    else combine_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b);
+    count_launch();
+    return cudaGetLastError();
+}
+
+cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t st)
+{
+    const int b = tx_bits_of(p.D), ty = 256 >> b;
+    const int tb = (int)(((int64_t)p.tokens + ty - 1) / ty);
+    const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
+    if (p.type == Q4_F32) combine_grad_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b, tb);
+    else if (p.type == Q4_BF16) combine_grad_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b, tb);
+    else combine_grad_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b, tb);
+    count_launch();
+    return cudaGetLastError();
+}
+
+}  // namespace q4

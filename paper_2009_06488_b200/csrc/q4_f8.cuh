@@ -1,0 +1,148 @@
+// Shared pieces of the e4m3 (8-bit float) kernels with a scale per 128 values and of the
+// expert-layer kernels: element types, eight-at-a-time loads and stores, launch parameters.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "q4_common.cuh"
+
+namespace q4 {
+namespace f8 {
+
+constexpr int BLK = 128;                 // values under one scale
+
+__host__ __device__ inline int64_t blocks_of(int64_t n) { return (n + BLK - 1) / BLK; }
+
+template <int TYPE> struct Elem;
+template <> struct Elem<Q4_F32>  { using T = float; };
+template <> struct Elem<Q4_BF16> { using T = __nv_bfloat16; };
+template <> struct Elem<Q4_F16>  { using T = __half; };
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+// Eight consecutive values as floats; `n` of them exist (0..8, the others read 0).  `vec`: the
+// address is a multiple of 16 bytes.
+__device__ __forceinline__ void load8(const float* p, int n, bool vec, float (&v)[8])
+{
+    if (n == 8 && vec) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? __ldg(p + i) : 0.0f;
+}
+__device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi, const __nv_bfloat16*)
+{
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi, const __half*)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    lo = f.x; hi = f.y;
+}
+template <typename H>
+__device__ __forceinline__ void load8(const H* p, int n, bool vec, float (&v)[8])
+{
+    if (n == 8 && vec) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
+        unpack2(w.x, v[0], v[1], p); unpack2(w.y, v[2], v[3], p);
+        unpack2(w.z, v[4], v[5], p); unpack2(w.w, v[6], v[7], p);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
+}
+__device__ __forceinline__ void store8(float* p, int n, bool vec, const float (&v)[8])
+{
+    if (n == 8 && vec) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, const __nv_bfloat16*)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, const __half*)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename H>
+__device__ __forceinline__ void store8(H* p, int n, bool vec, const float (&v)[8])
+{
+    if (n == 8 && vec) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1], p), pack2(v[2], v[3], p),
+                                                  pack2(v[4], v[5], p), pack2(v[6], v[7], p));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < n) p[i] = from_f<H>(v[i]);
+}
+
+inline size_t type_size(int type) { return type == Q4_F32 ? 4 : 2; }
+
+struct QuantizeParams {
+    const void* X;
+    int64_t ldx;
+    int32_t rows, cols;            // of the output
+    const int32_t* source;         // NULL, or row r comes from X's row source[r] / topk (-1: zeros)
+    int32_t topk, x_rows;
+    uint8_t* Q;  int64_t ldq;  float* S;  int64_t lds;       // both or neither
+    uint8_t* Qt; int64_t ldqt; float* St; int64_t ldst;      // both or neither
+    int32_t pow2;
+    int32_t x_vec, q_vec, qt_vec;  // 16-byte loads / 8-byte stores / 16-byte stores are aligned
+};
+
+// One product, dense or grouped.
+enum GroupMode { kDense = 0, kExpertRows = 1, kExpertDepth = 2 };
+struct GemmF8Params {
+    const uint8_t* A;  int64_t lda;  const float* SA; int64_t ldsa;     // SA [block of K][row of A]
+    const uint8_t* Bt; int64_t ldb;  const float* SB; int64_t ldsb;     // see b_rows
+    int32_t b_rows;                // SB: 0 = [block of N][block of K], 1 = [block of K][row of Bt]
+    void* C; int64_t ldc; int32_t c_type;
+    int32_t M, N, K;
+    int32_t mode, E;
+    const int32_t* starts;         // E + 1 row (kExpertRows) or depth (kExpertDepth) positions
+    unsigned* status;
+};
+
+}  // namespace f8
+
+cudaError_t launch_f8_quantize(const f8::QuantizeParams& p, int x_type, bool blocks, cudaStream_t st);
+cudaError_t launch_gemm_f8_simt(const f8::GemmF8Params& p, cudaStream_t st);
+
+size_t      expert_sort_ws_bytes(int64_t n, int32_t E);
+cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t align, int32_t* starts, int32_t* source,
+                               int32_t rows, int32_t* slot, void* ws, cudaStream_t st);
+struct ExpertRowsParams {
+    int32_t type, topk, D;
+    int32_t tokens, rows;
+    const void* Y; int64_t ldy;        // rows of the experts' side
+    const void* X; int64_t ldx;        // rows of the tokens' side (the output's gradient, or the gather's input)
+    const int32_t* slot;               // [tokens][topk] row of each pair, negative = none
+    const int32_t* source;             // [rows] pair of each row, negative = none
+    const float* w;                    // [tokens][topk] or NULL (= 1)
+    void* out; int64_t ldo;
+    float* dw;                         // [tokens][topk] (gradient only)
+    int32_t vec;                       // every row begins on a multiple of 16 bytes
+};
+cudaError_t launch_expert_gather(const ExpertRowsParams& p, cudaStream_t st);
+cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st);
+cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t st);
+
+}  // namespace q4
