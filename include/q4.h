@@ -424,8 +424,8 @@ q4_status q4_gemm_f8_experts(const uint8_t* A, int64_t lda, const float* SA, int
  * The gradient of the experts' weights: C_e [M x N] = A[:, seg e] * Bt[:, seg e]^T over the depth
  * segment starts[e] .. starts[e + 1] of A [M][lda] and Bt [N][ldb], both scaled by group along the
  * depth K (Qt, St of q4_f8_quantize over rows in expert order).  Segments begin on multiples of 128
- * (q4_expert_sort with align = 128), so that no group spans two experts; a start that does not is
- * rounded down.  C is [E * M][ldc]; an expert without rows gets zeros.
+ * (q4_expert_sort with align = 128), so that no group spans two experts; a value that is no multiple
+ * (and not K itself) is rounded down.  C is [E * M][ldc]; an expert without rows gets zeros.
  */
 q4_status q4_gemm_f8_experts_wgrad(const uint8_t* A, int64_t lda, const float* SA, int64_t ldsa,
                                    const uint8_t* Bt, int64_t ldb, const float* SB, int64_t ldsb,

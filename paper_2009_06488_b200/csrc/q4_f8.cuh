@@ -125,6 +125,8 @@ struct GemmF8Params {
 
 cudaError_t launch_f8_quantize(const f8::QuantizeParams& p, int x_type, bool blocks, cudaStream_t st);
 cudaError_t launch_gemm_f8_simt(const f8::GemmF8Params& p, cudaStream_t st);
+bool        gemm_f8_pair_supported(const f8::GemmF8Params& p);
+q4_status   launch_gemm_f8_pair(const f8::GemmF8Params& p, cudaStream_t st);
 
 size_t      expert_sort_ws_bytes(int64_t n, int32_t E);
 cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t align, int32_t* starts, int32_t* source,

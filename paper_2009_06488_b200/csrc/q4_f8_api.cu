@@ -31,6 +31,10 @@ q4_status run_product(f8::GemmF8Params& p, const char* call, void* stream)
 {
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
+    if (kernel_variant() != 1 && gemm_f8_pair_supported(p)) {
+        log_choice(call, "CTA-pair tcgen05 kernel");
+        return launch_gemm_f8_pair(p, stream_of(stream));
+    }
     log_choice(call, "general kernel");
     return done(launch_gemm_f8_simt(p, stream_of(stream)));
 }
