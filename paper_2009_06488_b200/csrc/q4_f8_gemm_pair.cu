@@ -102,6 +102,16 @@ __device__ __forceinline__ uint4 lds128_cluster(uint32_t a)
     return v;
 }
 
+// A load that stays where it is written (the compiler would move a plain one down to its use, a round of four
+// blocks later, and expose its latency); 0 where `in` is false.
+__device__ __forceinline__ float load_ahead(const float* at, bool in)
+{
+    float v;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t"
+                 "@p ld.global.nc.f32 %0, [%1];\n\t}" : "=f"(v) : "l"(at), "r"((int)in) : "memory");
+    return v;
+}
+
 struct PairParams {
     GemmF8Params g;
     int32_t tiles_m, tiles_n;        // kDense, kExpertDepth: of one product
@@ -264,7 +274,6 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         Walk<BN> walk(p, lane);
         // ------------------------------------------------------------ TMA producer
-        const bool one = elect_one();
         const uint32_t full_leader = map_to_cta(bar_full(0), leader);
         uint32_t st = 0, ph = 0;
         for (int tile = cluster_id; walk.get(tile, t); tile += nclusters) {
@@ -276,7 +285,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             const uint32_t bytes = (uint32_t)((rows > TMC - FEW ? TMC : few * FEW) + halves * 64) * ROWB;
             for (int b = 0; b < t.nkb; ++b) {
                 mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
-                if (one) {
+                if (elect_one()) {
                     const uint32_t full = full_leader + 8u * st;
                     mbar_expect_tx_cluster(full, bytes);
                     const uint32_t dst = sbase + st * C::STAGE;
@@ -301,8 +310,8 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         if (rank == 0) {
             Walk<BN> walk(p, lane);
-            const bool one = elect_one();
             const uint16_t both = (uint16_t)(3u << leader);
+            const uint64_t desc0 = make_kmajor_sw128_desc(sbase);
             uint32_t st = 0, ph = 0, used[HALVES] = {};
             for (int tile = cluster_id; walk.get(tile, t); tile += nclusters) {
                 share(t);
@@ -310,8 +319,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 for (int b = 0; b < t.nkb; ++b) {
                     mbar_wait(bar_full(st), ph, abort_flag, g.status);
                     tc_fence_after();
-                    const uint32_t ua = sbase + st * C::STAGE;
-                    const uint64_t adesc = make_kmajor_sw128_desc(ua);
+                    const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4));
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h) {
                         if (h >= halves) break;
@@ -320,8 +328,8 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                         const uint32_t sph = (HALVES == 2 ? u >> 1 : u >> 2) & 1u;
                         mbar_wait(bar_tempty(slot), sph ^ 1u, abort_flag, g.status);
                         tc_fence_after();
-                        if (one) {
-                            const uint64_t bdesc = make_kmajor_sw128_desc(ua + (TMC + 64 * h) * ROWB);
+                        if (elect_one()) {
+                            const uint64_t bdesc = adesc + (uint64_t)((TMC + 64 * h) * ROWB >> 4);
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 tc_mma_f8_pair(tmem_base + (uint32_t)(slot * 128), adesc + (uint64_t)(2 * i),
@@ -372,12 +380,12 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool in = b0 + i < t.nkb;
-                    sa[i] = in && row < t.m_end ? __ldg(sa_at + (b0 + i) * g.ldsa) : 0.0f;
+                    sa[i] = load_ahead(sa_at + (b0 + i) * g.ldsa, in && row < t.m_end);
                     if (!BROWS) {
-                        sb[i] = in && c0 < g.N ? __ldg(sb_at + b0 + i) : 0.0f;
+                        sb[i] = load_ahead(sb_at + b0 + i, in && c0 < g.N);
                     } else if (i < 4 * CW / 128) {
                         const int el = i * 128 + st_id, kb = el / CW, n = c0 + el % CW;
-                        sb[i] = b0 + kb < t.nkb && n < g.N ? __ldg(sb_at + (b0 + kb) * g.ldsb + n) : 0.0f;
+                        sb[i] = load_ahead(sb_at + (b0 + kb) * g.ldsb + n, b0 + kb < t.nkb && n < g.N);
                     }
                 }
             };
