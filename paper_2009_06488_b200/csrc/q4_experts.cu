@@ -32,18 +32,22 @@ count_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int64_t chun
     extern __shared__ int32_t cnt[];       // [E]
     for (int e = threadIdx.x; e < E; e += blockDim.x) cnt[e] = 0;
     __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
+#pragma unroll 8
     for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
-        const int e = ids[i];
+        const int e = __ldg(ids + i);
         if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) hist[(int64_t)blockIdx.x * E + e] = cnt[e];
 }
 
+// Launched while count_kernel runs (programmatic serialization): what needs only the ids comes first.
 __global__ void __launch_bounds__(NW * 32)
 place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t align, int64_t chunk,
-             const int32_t* __restrict__ hist, int32_t* __restrict__ starts, int32_t* __restrict__ source,
+             const int32_t* hist, int32_t* __restrict__ starts, int32_t* __restrict__ source,
              int32_t rows, int32_t* __restrict__ slot)
 {
     extern __shared__ int32_t sm[];
@@ -55,33 +59,55 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
     const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
     const int64_t piece = ((chunk + NW - 1) / NW + 31) / 32 * 32;
     const int64_t wlo = min(hi, lo + warp * piece), whi = min(hi, wlo + piece);
+    const bool kept = piece <= 8 * 32;     // a lane's ids stay in registers
 
-    for (int i = threadIdx.x; i < NW * E; i += blockDim.x) base[i] = 0;
+    if (!hist) asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int i = threadIdx.x; i < (NW + 2) * E; i += blockDim.x) sm[i] = 0;
     __syncthreads();
-    for (int64_t i = wlo + lane; i < whi; i += 32) {
-        const int e = ids[i];
-        if (e >= 0 && e < E) atomicAdd(&base[warp * E + e], 1);
-    }
-    for (int e = threadIdx.x; hist && e < E; e += blockDim.x) {
-        int b = 0, t = 0;
-        for (int c = 0; c < (int)gridDim.x; ++c) {
-            const int h = hist[(int64_t)c * E + e];
-            if (c < (int)blockIdx.x) b += h;
-            t += h;
+    int32_t mine[8];
+    if (kept) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t i = wlo + k * 32 + lane;
+            mine[k] = i < whi ? __ldg(ids + i) : -1;
         }
-        total[e] = t;
-        before[e] = b;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (mine[k] >= 0 && mine[k] < E) atomicAdd(&base[warp * E + mine[k]], 1);
+    } else {
+#pragma unroll 8
+        for (int64_t i = wlo + lane; i < whi; i += 32) {
+            const int e = __ldg(ids + i);
+            if (e >= 0 && e < E) atomicAdd(&base[warp * E + e], 1);
+        }
     }
-    __syncthreads();
-    if (!hist) {
+    if (hist) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        // thread (e, part) sums a part of the chunks: as many parts as the block has threads for
+        const int parts = max(1, (int)blockDim.x / E), G = (int)gridDim.x;
+        for (int u = threadIdx.x; u < parts * E; u += blockDim.x) {
+            const int e = u % E, part = u / E;
+            int b = 0, t = 0;
+#pragma unroll 8
+            for (int c = part; c < G; c += parts) {
+                const int h = hist[(int64_t)c * E + e];
+                t += h;
+                b += c < (int)blockIdx.x ? h : 0;
+            }
+            atomicAdd(&total[e], t);
+            atomicAdd(&before[e], b);
+        }
+    } else {
+        __syncthreads();
         for (int e = threadIdx.x; e < E; e += blockDim.x) {
             int t = 0;
+#pragma unroll
             for (int w = 0; w < NW; ++w) t += base[w * E + e];
             total[e] = t;
-            before[e] = 0;
         }
-        __syncthreads();
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __syncthreads();
     if (warp == 0) {
         int at = 0;
         for (int e0 = 0; e0 < E; e0 += 32) {
@@ -101,6 +127,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) {
         int at = first[e] + before[e];
+#pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int c = base[w * E + e];
             base[w * E + e] = at;
@@ -116,9 +143,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
         source[r] = -1;
     __syncthreads();
 
-    for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
-        const int64_t i = i0 + lane;
-        int e = i < whi ? ids[i] : -1;
+    auto place = [&](int64_t i, int e) {
         if (e >= E || e < 0) e = -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
         const int r = e >= 0 ? base[warp * E + e] + __popc(same & ((1u << lane) - 1u)) : -1;
@@ -129,12 +154,21 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
         __syncwarp();
         if (e >= 0 && (int)(__ffs(same) - 1) == lane) base[warp * E + e] += __popc(same);
         __syncwarp();
+    };
+    if (kept) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (wlo + k * 32 < whi) place(wlo + k * 32 + lane, mine[k]);
+    } else {
+        for (int64_t i0 = wlo; i0 < whi; i0 += 32) place(i0 + lane, i0 + lane < whi ? __ldg(ids + i0 + lane) : -1);
     }
 }
 
 // ------------------------------------------------------------------------------------- rows
 // A block's 256 threads are TY rows (or tokens) of TX threads, TX a power of two of 8..256.
-template <int TYPE>
+using f8::Eight;
+
+template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256)
 gather_kernel(const ExpertRowsParams p, int tx_bits)
 {
@@ -149,17 +183,32 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     T* dst = static_cast<T*>(p.out) + r * p.ldo;
     for (int c = tx * 8; c < p.D; c += TX * 8) {
         const int n = min(8, p.D - c);
-        float v[8];
-        f8::load8(src + c, on ? n : 0, p.vec, v);
+        Eight<T> v;
+        f8::load8<VEC>(v, src + c, on ? n : 0);
         if (p.w) {
+            float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= w;
+            for (int i = 0; i < 8; ++i) f[i] = v.get(i) * w;
+            f8::pack8(v, f);
         }
-        f8::store8(dst + c, n, p.vec, v);
+        f8::store8<VEC>(dst + c, n, v);
     }
 }
 
-template <int TYPE>
+// Rows and weights of pairs j0 .. j0 + 7 of a token; -1 where there is none.
+__device__ __forceinline__ void pairs_of(const ExpertRowsParams& p, int64_t t, bool mine, int j0, int (&s)[8], float (&w)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const bool in = mine && j0 + j < p.topk;
+        s[j] = in ? __ldg(p.slot + t * p.topk + j0 + j) : -1;
+        w[j] = in && p.w ? __ldg(p.w + t * p.topk + j0 + j) : 1.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) if (s[j] >= p.rows) s[j] = -1;
+}
+
+template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256)
 combine_kernel(const ExpertRowsParams p, int tx_bits)
 {
@@ -172,40 +221,57 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const int n = min(8, p.D - c);
     float acc[8] = {};
     for (int j0 = 0; j0 < p.topk; j0 += 8) {
-        float v[8][8], w[8];
-        bool on[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool in = j0 + j < p.topk;
-            const int s = in ? p.slot[t * p.topk + j0 + j] : -1;
-            on[j] = s >= 0 && s < p.rows;
-            w[j] = on[j] && p.w ? p.w[t * p.topk + j0 + j] : 1.0f;
-            f8::load8(static_cast<const T*>(p.Y) + (on[j] ? s * p.ldy + c : 0), on[j] ? n : 0, p.vec, v[j]);
-        }
+        int s[8];
+        float w[8];
+        Eight<T> v[8];
+        pairs_of(p, t, true, j0, s, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (on[j])
+            f8::load8<VEC>(v[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j][i], acc[i]);
+        for (int j = 0; j < 8; ++j)
+            if (s[j] >= 0)                          // a dropped pair's weight may be anything
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j].get(i), acc[i]);
     }
-    f8::store8(static_cast<T*>(p.out) + t * p.ldo + c, n, p.vec, acc);
+    Eight<T> o;
+    f8::pack8(o, acc);
+    f8::store8<VEC>(static_cast<T*>(p.out) + t * p.ldo + c, n, o);
 }
 
-template <int TYPE>
+// Sums of eight values over the 32 lanes of a warp; lane l < 8 returns the sum of value l.  Each step
+// halves the values and doubles the lanes that were summed: 9 shuffles instead of 40.
+__device__ __forceinline__ float reduce8(float (&d)[8], int lane)
+{
+#pragma unroll
+    for (int b = 4; b; b >>= 1) {
+        const bool up = lane & b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j >= b) break;
+            const float give = up ? d[j] : d[j + b];
+            d[j] = (up ? d[j + b] : d[j]) + __shfl_xor_sync(0xFFFFFFFFu, give, b);
+        }
+    }
+    d[0] += __shfl_xor_sync(0xFFFFFFFFu, d[0], 8);
+    return d[0] + __shfl_xor_sync(0xFFFFFFFFu, d[0], 16);
+}
+
+template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
     using T = typename f8::Elem<TYPE>::T;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float zero[8] = {};
     if ((int)blockIdx.x >= token_blocks) {
         // rows that belong to no pair get zeros: 32 rows per warp
         const int64_t r0 = ((int64_t)blockIdx.x - token_blocks) * 256 + warp * 32;
         const int pair = r0 + lane < p.rows ? p.source[r0 + lane] : 0;
-        unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0);
-        for (; none; none &= none - 1) {
+        Eight<T> zero;
+        zero.zero();
+        for (unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0); none; none &= none - 1) {
             T* dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
-            for (int c = lane * 8; c < p.D; c += 256) f8::store8(dst + c, min(8, p.D - c), p.vec, zero);
+            for (int c = lane * 8; c < p.D; c += 256) f8::store8<VEC>(dst + c, min(8, p.D - c), zero);
         }
         return;
     }
@@ -217,48 +283,44 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
     for (int j0 = 0; j0 < p.topk; j0 += 8) {
         int s[8];
         float w[8], dot[8] = {};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool in = mine && j0 + j < p.topk;
-            s[j] = in ? p.slot[t * p.topk + j0 + j] : -1;
-            if (s[j] >= p.rows) s[j] = -1;
-            w[j] = s[j] >= 0 && p.w ? p.w[t * p.topk + j0 + j] : 1.0f;
-        }
+        pairs_of(p, t, mine, j0, s, w);
         for (int c = tx * 8; mine && c < p.D; c += TX * 8) {
             const int n = min(8, p.D - c);
-            float d[8], y[8][8];
-            f8::load8(g + c, n, p.vec, d);
+            Eight<T> d, y[8];
+            f8::load8<VEC>(d, g + c, n);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                f8::load8(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, p.vec, y[j]);
+                f8::load8<VEC>(y[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (s[j] < 0) continue;
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    dot[j] = fmaf(d[i], y[j][i], dot[j]);
-                    o[i] = w[j] * d[i];
+                    dot[j] = fmaf(d.get(i), y[j].get(i), dot[j]);
+                    o[i] = w[j] * d.get(i);
                 }
-                f8::store8(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, p.vec, o);
+                Eight<T> e;
+                f8::pack8(e, o);
+                f8::store8<VEC>(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, e);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            for (int o = min(TX, 32) >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
-            if (TX > 32 && lane == 0) part[warp][j] = dot[j];
-        }
-        if (TX > 32) {
+        if (TX >= 32) {
+            const float sum = reduce8(dot, lane);
+            if (lane < 8) part[warp][lane] = sum;
             __syncthreads();
             if (tx < 8) {
-                float sum = 0.0f;
-                for (int k = 0; k < TX / 32; ++k) sum += part[warp + k][tx];
-                if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = sum;
+                float all = 0.0f;
+                for (int k = 0; k < TX / 32; ++k) all += part[warp + k][tx];
+                if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = all;
             }
             __syncthreads();
-        } else if (tx == 0 && mine) {
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) if (j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
+            for (int j = 0; j < 8; ++j) {
+                for (int o = TX >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
+                if (tx == 0 && mine && j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
+            }
         }
     }
 }
@@ -274,6 +336,16 @@ static int tx_bits_of(int D)
 
 using namespace experts;
 
+#define Q4_ROWS_LAUNCH(kernel, grid, args)                                                          \
+    do {                                                                                            \
+        if (p.type == Q4_F32) p.vec ? kernel<Q4_F32, true><<<grid, 256, 0, st>>> args               \
+                                    : kernel<Q4_F32, false><<<grid, 256, 0, st>>> args;             \
+        else if (p.type == Q4_BF16) p.vec ? kernel<Q4_BF16, true><<<grid, 256, 0, st>>> args        \
+                                          : kernel<Q4_BF16, false><<<grid, 256, 0, st>>> args;      \
+        else p.vec ? kernel<Q4_F16, true><<<grid, 256, 0, st>>> args                                \
+                   : kernel<Q4_F16, false><<<grid, 256, 0, st>>> args;                              \
+    } while (0)
+
 size_t expert_sort_ws_bytes(int64_t n, int32_t E)
 {
     const int g = chunks_of(n);
@@ -286,25 +358,38 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
     const int g = chunks_of(n);
     const int64_t chunk = ((int64_t)n + g - 1) / g;
     const size_t smem = ((size_t)(NW + 3) * E + 1) * 4;
-    const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (NW + 3) * 1024 * 4 + 4);
-    if (e != cudaSuccess) return e;
-    int32_t* hist = static_cast<int32_t*>(ws);
-    if (g > 1) {
-        count_kernel<<<g, 512, (size_t)E * 4, st>>>(ids, n, E, chunk, hist);
-        count_launch();
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
     }
-    place_kernel<<<g, NW * 32, smem, st>>>(ids, n, E, align, chunk, g > 1 ? hist : nullptr, starts, source, rows, slot);
+    int32_t* hist = static_cast<int32_t*>(ws);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)g);
+    cfg.blockDim = dim3(512);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (g > 1) {
+        cfg.dynamicSmemBytes = (size_t)E * 4;
+        const cudaError_t err = cudaLaunchKernelEx(&cfg, count_kernel, ids, n, E, chunk, hist);
+        count_launch();
+        if (err != cudaSuccess) return err;
+    }
+    cfg.dynamicSmemBytes = smem;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, place_kernel, ids, n, E, align, chunk,
+                                               (const int32_t*)(g > 1 ? hist : nullptr), starts, source, rows, slot);
     count_launch();
-    return cudaGetLastError();
+    return err;
 }
 
 cudaError_t launch_expert_gather(const ExpertRowsParams& p, cudaStream_t st)
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const unsigned grid = (unsigned)(((int64_t)p.rows + ty - 1) / ty);
-    if (p.type == Q4_F32) gather_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b);
-    else if (p.type == Q4_BF16) gather_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b);
-    else gather_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b);
+    Q4_ROWS_LAUNCH(gather_kernel, grid, (p, b));
     count_launch();
     return cudaGetLastError();
 }
@@ -313,9 +398,7 @@ cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st)
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const dim3 grid((unsigned)(((int64_t)p.tokens + ty - 1) / ty), (unsigned)((p.D + (8 << b) - 1) / (8 << b)));
-    if (p.type == Q4_F32) combine_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b);
-    else if (p.type == Q4_BF16) combine_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b);
-    else combine_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b);
+    Q4_ROWS_LAUNCH(combine_kernel, grid, (p, b));
     count_launch();
     return cudaGetLastError();
 }
@@ -325,9 +408,7 @@ cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t s
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const int tb = (int)(((int64_t)p.tokens + ty - 1) / ty);
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
-    if (p.type == Q4_F32) combine_grad_kernel<Q4_F32><<<grid, 256, 0, st>>>(p, b, tb);
-    else if (p.type == Q4_BF16) combine_grad_kernel<Q4_BF16><<<grid, 256, 0, st>>>(p, b, tb);
-    else combine_grad_kernel<Q4_F16><<<grid, 256, 0, st>>>(p, b, tb);
+    Q4_ROWS_LAUNCH(combine_grad_kernel, grid, (p, b, tb));
     count_launch();
     return cudaGetLastError();
 }

@@ -27,51 +27,29 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
-// Eight consecutive values as floats; `n` of them exist (0..8, the others read 0).  `vec`: the
-// address is a multiple of 16 bytes.
-__device__ __forceinline__ void load8(const float* p, int n, bool vec, float (&v)[8])
-{
-    if (n == 8 && vec) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        return;
-    }
+// Eight consecutive values as they lie in memory (NW 32-bit words), so that many of them can be in flight
+// or held at a register cost of the type's own size.
+template <typename T> struct Eight {
+    static constexpr int NW = 2 * (int)sizeof(T);
+    uint32_t w[NW];
+    __device__ __forceinline__ float get(int i) const;          // i is a constant after unrolling
+    __device__ __forceinline__ void zero()
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? __ldg(p + i) : 0.0f;
-}
-__device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi, const __nv_bfloat16*)
-{
-    lo = __uint_as_float(w << 16);
-    hi = __uint_as_float(w & 0xFFFF0000u);
-}
-__device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi, const __half*)
-{
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    lo = f.x; hi = f.y;
-}
-template <typename H>
-__device__ __forceinline__ void load8(const H* p, int n, bool vec, float (&v)[8])
-{
-    if (n == 8 && vec) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-        unpack2(w.x, v[0], v[1], p); unpack2(w.y, v[2], v[3], p);
-        unpack2(w.z, v[4], v[5], p); unpack2(w.w, v[6], v[7], p);
-        return;
+        for (int k = 0; k < NW; ++k) w[k] = 0;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
-}
-__device__ __forceinline__ void store8(float* p, int n, bool vec, const float (&v)[8])
+};
+template <> __device__ __forceinline__ float Eight<float>::get(int i) const { return __uint_as_float(w[i]); }
+template <> __device__ __forceinline__ float Eight<__nv_bfloat16>::get(int i) const
 {
-    if (n == 8 && vec) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
 }
+template <> __device__ __forceinline__ float Eight<__half>::get(int i) const
+{
+    const __half2 h = *reinterpret_cast<const __half2*>(&w[i >> 1]);
+    return i & 1 ? __high2float(h) : __low2float(h);
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi, const __nv_bfloat16*)
 {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -82,16 +60,51 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, const __half*)
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <typename H>
-__device__ __forceinline__ void store8(H* p, int n, bool vec, const float (&v)[8])
+__device__ __forceinline__ void pack8(Eight<float>& e, const float (&v)[8])
 {
-    if (n == 8 && vec) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1], p), pack2(v[2], v[3], p),
-                                                  pack2(v[4], v[5], p), pack2(v[6], v[7], p));
-        return;
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < n) p[i] = from_f<H>(v[i]);
+    for (int i = 0; i < 8; ++i) e.w[i] = __float_as_uint(v[i]);
+}
+template <typename H> __device__ __forceinline__ void pack8(Eight<H>& e, const float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.w[i] = pack2(v[2 * i], v[2 * i + 1], (const H*)nullptr);
+}
+
+// VEC: all eight exist (n = 8, or 0 for none) at an address that is a multiple of 16 bytes; else `n` of
+// them (0..8) are read one by one.  What does not exist reads 0.  The data is streamed: read once.
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(Eight<T>& e, const T* p, int n)
+{
+    if constexpr (VEC) {
+        e.zero();
+        if (n > 0) {
+#pragma unroll
+            for (int k = 0; k < Eight<T>::NW / 4; ++k)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(e.w[4 * k]), "=r"(e.w[4 * k + 1]), "=r"(e.w[4 * k + 2]), "=r"(e.w[4 * k + 3])
+                             : "l"(reinterpret_cast<const uint4*>(p) + k));
+        }
+    } else {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
+        pack8(e, v);                               // exact: the values are of the type
+    }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, int n, const Eight<T>& e)
+{
+    if constexpr (VEC) {
+        if (n > 0) {
+#pragma unroll
+            for (int k = 0; k < Eight<T>::NW / 4; ++k)
+                reinterpret_cast<uint4*>(p)[k] = make_uint4(e.w[4 * k], e.w[4 * k + 1], e.w[4 * k + 2], e.w[4 * k + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = from_f<T>(e.get(i));
+    }
 }
 
 inline size_t type_size(int type) { return type == Q4_F32 ? 4 : 2; }
@@ -105,7 +118,8 @@ struct QuantizeParams {
     uint8_t* Q;  int64_t ldq;  float* S;  int64_t lds;       // both or neither
     uint8_t* Qt; int64_t ldqt; float* St; int64_t ldst;      // both or neither
     int32_t pow2;
-    int32_t x_vec, q_vec, qt_vec;  // 16-byte loads / 8-byte stores / 16-byte stores are aligned
+    int32_t x_vec;                 // rows of X begin on multiples of 16 bytes and cols is a multiple of 8
+    int32_t q_vec, qt_vec;         // 8-byte stores to Q / 16-byte stores to Qt are aligned
 };
 
 // One product, dense or grouped.
@@ -141,7 +155,7 @@ struct ExpertRowsParams {
     const float* w;                    // [tokens][topk] or NULL (= 1)
     void* out; int64_t ldo;
     float* dw;                         // [tokens][topk] (gradient only)
-    int32_t vec;                       // every row begins on a multiple of 16 bytes
+    int32_t vec;                       // rows begin on multiples of 16 bytes and D is a multiple of 8
 };
 cudaError_t launch_expert_gather(const ExpertRowsParams& p, cudaStream_t st);
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st);

@@ -73,7 +73,7 @@ q4_status q4_f8_quantize(const void* X, int32_t x_type, int64_t ldx, int32_t row
     p.Q = Q; p.ldq = ldq; p.S = S; p.lds = lds;
     p.Qt = Qt; p.ldqt = ldqt; p.St = St; p.ldst = ldst;
     p.pow2 = (flags & Q4_F8_POW2) ? 1 : 0;
-    p.x_vec = aligned(X, 16) && ldx * (int64_t)f8::type_size(x_type) % 16 == 0;
+    p.x_vec = cols % 8 == 0 && aligned(X, 16) && ldx * (int64_t)f8::type_size(x_type) % 16 == 0;
     p.q_vec = aligned(Q, 8) && ldq % 8 == 0;
     p.qt_vec = aligned(Qt, 16) && ldqt % 16 == 0;
     return done(launch_f8_quantize(p, x_type, blocks, stream_of(stream)));
@@ -158,7 +158,7 @@ q4_status q4_expert_gather(const void* X, int64_t ldx, int32_t type, int32_t D, 
     if ((tokens > 0 && !X) || !source || !Xs) return Q4_ERR_INVALID_ARG;
     const size_t z = f8::type_size(type);
     if (!aligned(X, z) || !aligned(Xs, z) || !aligned(source, 4) || !aligned(w, 4)) return Q4_ERR_ALIGNMENT;
-    p.vec = aligned(X, 16) && aligned(Xs, 16) && ldx * z % 16 == 0 && ldxs * z % 16 == 0;
+    p.vec = D % 8 == 0 && aligned(X, 16) && aligned(Xs, 16) && ldx * z % 16 == 0 && ldxs * z % 16 == 0;
     return done(launch_expert_gather(p, stream_of(stream)));
 }
 
@@ -174,7 +174,7 @@ q4_status q4_expert_combine(const void* Y, int64_t ldy, int32_t type, int32_t D,
     if ((rows > 0 && !Y) || !slot || !Out) return Q4_ERR_INVALID_ARG;
     const size_t z = f8::type_size(type);
     if (!aligned(Y, z) || !aligned(Out, z) || !aligned(slot, 4) || !aligned(w, 4)) return Q4_ERR_ALIGNMENT;
-    p.vec = aligned(Y, 16) && aligned(Out, 16) && ldy * z % 16 == 0 && ldo * z % 16 == 0;
+    p.vec = D % 8 == 0 && aligned(Y, 16) && aligned(Out, 16) && ldy * z % 16 == 0 && ldo * z % 16 == 0;
     return done(launch_expert_combine(p, stream_of(stream)));
 }
 
@@ -191,7 +191,7 @@ q4_status q4_expert_combine_grad(const void* dOut, int64_t ldd, const void* Y, i
     const size_t z = f8::type_size(type);
     if (!aligned(dOut, z) || !aligned(Y, z) || !aligned(dY, z) || !aligned(slot, 4) || !aligned(source, 4) ||
         !aligned(w, 4) || !aligned(dw, 4)) return Q4_ERR_ALIGNMENT;
-    p.vec = aligned(dOut, 16) && aligned(Y, 16) && aligned(dY, 16) && ldd * z % 16 == 0 && ldy * z % 16 == 0 &&
+    p.vec = D % 8 == 0 && aligned(dOut, 16) && aligned(Y, 16) && aligned(dY, 16) && ldd * z % 16 == 0 && ldy * z % 16 == 0 &&
             lddy * z % 16 == 0;
     return done(launch_expert_combine_grad(p, stream_of(stream)));
 }

@@ -23,7 +23,21 @@
 namespace q4 {
 namespace f8 {
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// Maxima of |x| on the values' own bit patterns: element-wise over the words of eight values, then of
+// all eight as the pattern of a binary32 number.
+template <typename T> __device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max_words<float>(uint32_t a, uint32_t b) { return max(a, b & 0x7FFFFFFFu); }
+template <> __device__ __forceinline__ uint32_t max_words<__nv_bfloat16>(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
+template <> __device__ __forceinline__ uint32_t max_words<__half>(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
+template <typename T> __device__ __forceinline__ uint32_t pattern(const Eight<T>& e, int i) { return __float_as_uint(e.get(i)); }
+template <typename T> __device__ __forceinline__ uint32_t max_of(const Eight<T>& e)
+{
+    Eight<T> m;
+    m.w[0] = max_words<T>(0, e.w[0]);
+#pragma unroll
+    for (int k = 1; k < Eight<T>::NW; ++k) m.w[0] = max_words<T>(m.w[0], e.w[k]);
+    return sizeof(T) == 4 ? m.w[0] : max(pattern(m, 0), pattern(m, 1));
+}
 
 // Scale of a block whose largest |x| has the bit pattern `a`, and its inverse.
 __device__ __forceinline__ void scale_of(uint32_t a, int pow2, float& s, float& inv)
@@ -44,18 +58,16 @@ __device__ __forceinline__ uint32_t cvt2(float lo, float hi)
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint2 cvt8(const float (&v)[8], float inv)
-{
-    return make_uint2(cvt2(v[0] * inv, v[1] * inv) | (cvt2(v[2] * inv, v[3] * inv) << 16),
-                      cvt2(v[4] * inv, v[5] * inv) | (cvt2(v[6] * inv, v[7] * inv) << 16));
-}
+__device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d) { return cvt2(a, b) | (cvt2(c, d) << 16); }
 
-template <int TYPE, int RT, bool BLOCKS>
+// VEC: every row of X begins on a multiple of 16 bytes and cols is a multiple of 8.
+template <int TYPE, int RT, bool BLOCKS, bool VEC>
 __global__ void __launch_bounds__(256)
 quantize_kernel(const QuantizeParams p)
 {
     using T = typename Elem<TYPE>::T;
     constexpr int TR = 16 * RT;                            // rows of the tile
+    constexpr int NW = Eight<T>::NW;
     __shared__ uint32_t col_max[RT == 8 ? 8 : 1][BLK];     // per warp; blocks: [0][warp]
     __shared__ float row_scale[TR];
     __shared__ __align__(16) uint8_t tile[RT == 8 ? BLK * BLK : 16];
@@ -68,37 +80,38 @@ quantize_kernel(const QuantizeParams p)
     const int c0 = cb * BLK + cx * 8;
     const int nc = min(8, max(0, p.cols - c0));
 
-    float v[RT][8];
+    Eight<T> v[RT];
+    int64_t from[RT];
+    if (p.source) {
+        // a thread of each row fetches its number
+        int s = -1;
+        if (cx < RT && r0 + cx < p.rows) s = __ldg(p.source + r0 + cx);
+        const int64_t r = s >= 0 && s / p.topk < p.x_rows ? s / p.topk : -1;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        int64_t r = r0 + i;
-        bool on = r < p.rows;
-        if (on && p.source) {
-            const int s = p.source[r];
-            r = s / p.topk;
-            on = s >= 0 && r < p.x_rows;
-        }
-        load8(static_cast<const T*>(p.X) + (on ? r * p.ldx + c0 : 0), on ? nc : 0, p.x_vec, v[i]);
+        for (int i = 0; i < RT; ++i) from[i] = __shfl_sync(0xFFFFFFFFu, r, (lane & 16) + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) from[i] = r0 + i < p.rows ? r0 + i : -1;
     }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+        load8<VEC>(v[i], static_cast<const T*>(p.X) + (from[i] >= 0 ? from[i] * p.ldx + c0 : 0), from[i] >= 0 ? nc : 0);
 
-    uint32_t block_max = 0;
+    float binv = 0.0f;
     if (BLOCKS) {
+        uint32_t a = 0;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) block_max = max(block_max, abs_bits(v[i][j]));
-        block_max = __reduce_max_sync(0xFFFFFFFFu, block_max);
-        if (lane == 0) col_max[0][warp] = block_max;
+        for (int i = 0; i < RT; ++i) a = max(a, max_of(v[i]));
+        a = __reduce_max_sync(0xFFFFFFFFu, a);
+        if (lane == 0) col_max[0][warp] = a;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 8; ++w) block_max = max(block_max, col_max[0][w]);
-    }
-    float bs = 0.0f, binv = 0.0f;
-    if (BLOCKS) {
-        scale_of(block_max, p.pow2, bs, binv);
+        for (int w = 0; w < 8; ++w) a = max(a, col_max[0][w]);
+        float s;
+        scale_of(a, p.pow2, s, binv);
         if (threadIdx.x == 0) {
-            if (p.S) p.S[(int64_t)rb * p.lds + cb] = bs;
-            if (p.St) p.St[(int64_t)cb * p.ldst + rb] = bs;
+            if (p.S) p.S[(int64_t)rb * p.lds + cb] = s;
+            if (p.St) p.St[(int64_t)cb * p.ldst + rb] = s;
         }
     }
 
@@ -107,9 +120,7 @@ quantize_kernel(const QuantizeParams p)
         for (int i = 0; i < RT; ++i) {
             float inv = binv;
             if (!BLOCKS) {
-                uint32_t a = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) a = max(a, abs_bits(v[i][j]));
+                uint32_t a = max_of(v[i]);
 #pragma unroll
                 for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
                 float s;
@@ -117,14 +128,16 @@ quantize_kernel(const QuantizeParams p)
                 if (cx == 0) row_scale[ry * RT + i] = s;
             }
             if (r0 + i < p.rows && nc > 0) {
-                const uint2 q = cvt8(v[i], inv);
+                uint32_t q[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    q[k] = cvt4(v[i].get(4 * k) * inv, v[i].get(4 * k + 1) * inv, v[i].get(4 * k + 2) * inv, v[i].get(4 * k + 3) * inv);
                 uint8_t* dst = p.Q + (r0 + i) * p.ldq + c0;
                 if (nc == 8 && p.q_vec) {
-                    *reinterpret_cast<uint2*>(dst) = q;
+                    *reinterpret_cast<uint2*>(dst) = make_uint2(q[0], q[1]);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < nc) dst[j] = (uint8_t)((j < 4 ? q.x >> (8 * j) : q.y >> (8 * (j - 4))) & 0xFFu);
+                    for (int j = 0; j < 8; ++j) if (j < nc) dst[j] = (uint8_t)((q[j >> 2] >> (8 * (j & 3))) & 0xFFu);
                 }
             }
         }
@@ -139,13 +152,18 @@ quantize_kernel(const QuantizeParams p)
         float inv[8];
         if (!BLOCKS) {
             // maxima of my 8 columns: over my rows, the warp's other row of threads, the other warps
+            Eight<T> m;
+            m.zero();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint32_t a = 0;
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int i = 0; i < RT; ++i) a = max(a, abs_bits(v[i][j]));
-                a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 16));
-                if (lane < 16) col_max[RT == 8 ? warp : 0][cx * 8 + j] = a;
+                for (int k = 0; k < NW; ++k) m.w[k] = max_words<T>(m.w[k], v[i].w[k]);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) m.w[k] = max_words<T>(m.w[k], __shfl_xor_sync(0xFFFFFFFFu, m.w[k], 16));
+            if (lane < 16) {
+                uint4* at = reinterpret_cast<uint4*>(&col_max[RT == 8 ? warp : 0][cx * 8]);
+                at[0] = make_uint4(pattern(m, 0), pattern(m, 1), pattern(m, 2), pattern(m, 3));
+                at[1] = make_uint4(pattern(m, 4), pattern(m, 5), pattern(m, 6), pattern(m, 7));
             }
             __syncthreads();
             if (threadIdx.x < BLK) {
@@ -168,10 +186,14 @@ quantize_kernel(const QuantizeParams p)
         // column c's 128 codes: 16 pieces of 8 bytes, piece q at q ^ (c / 8)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float t[8];
+            uint32_t q[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = v[i < RT ? i : 0][j];
-            *reinterpret_cast<uint2*>(&tile[(cx * 8 + j) * BLK + ((ry ^ cx) << 3)]) = cvt8(t, inv[j]);
+            for (int k = 0; k < 2; ++k) {
+                const int i = RT == 8 ? 4 * k : 0;
+                q[k] = cvt4(v[i].get(j) * inv[j], v[RT == 8 ? i + 1 : 0].get(j) * inv[j], v[RT == 8 ? i + 2 : 0].get(j) * inv[j],
+                            v[RT == 8 ? i + 3 : 0].get(j) * inv[j]);
+            }
+            *reinterpret_cast<uint2*>(&tile[(cx * 8 + j) * BLK + ((ry ^ cx) << 3)]) = make_uint2(q[0], q[1]);
         }
         __syncthreads();
         const int64_t rt0 = (int64_t)rb * BLK;
@@ -195,23 +217,23 @@ quantize_kernel(const QuantizeParams p)
     }
 }
 
-template <int TYPE>
+template <int TYPE, bool VEC>
 static void launch_typed(const QuantizeParams& p, bool blocks, cudaStream_t st)
 {
     // column blocks vary fastest: neighbouring tiles read neighbouring pieces of the same rows
     const unsigned tiles = (unsigned)(blocks_of(p.cols) * (blocks || p.Qt ? blocks_of(p.rows) : (p.rows + 31) / 32));
-    if (blocks) quantize_kernel<TYPE, 8, true><<<tiles, 256, 0, st>>>(p);
-    else if (p.Qt) quantize_kernel<TYPE, 8, false><<<tiles, 256, 0, st>>>(p);
-    else quantize_kernel<TYPE, 2, false><<<tiles, 256, 0, st>>>(p);
+    if (blocks) quantize_kernel<TYPE, 8, true, VEC><<<tiles, 256, 0, st>>>(p);
+    else if (p.Qt) quantize_kernel<TYPE, 8, false, VEC><<<tiles, 256, 0, st>>>(p);
+    else quantize_kernel<TYPE, 2, false, VEC><<<tiles, 256, 0, st>>>(p);
 }
 
 }  // namespace f8
 
 cudaError_t launch_f8_quantize(const f8::QuantizeParams& p, int x_type, bool blocks, cudaStream_t st)
 {
-    if (x_type == Q4_F32) f8::launch_typed<Q4_F32>(p, blocks, st);
-    else if (x_type == Q4_BF16) f8::launch_typed<Q4_BF16>(p, blocks, st);
-    else f8::launch_typed<Q4_F16>(p, blocks, st);
+    if (x_type == Q4_F32) p.x_vec ? f8::launch_typed<Q4_F32, true>(p, blocks, st) : f8::launch_typed<Q4_F32, false>(p, blocks, st);
+    else if (x_type == Q4_BF16) p.x_vec ? f8::launch_typed<Q4_BF16, true>(p, blocks, st) : f8::launch_typed<Q4_BF16, false>(p, blocks, st);
+    else p.x_vec ? f8::launch_typed<Q4_F16, true>(p, blocks, st) : f8::launch_typed<Q4_F16, false>(p, blocks, st);
     count_launch();
     return cudaGetLastError();
 }
