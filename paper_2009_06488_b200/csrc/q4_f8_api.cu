@@ -31,7 +31,12 @@ q4_status run_product(f8::GemmF8Params& p, const char* call, void* stream)
 {
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
-    if (kernel_variant() != 1 && gemm_f8_pair_supported(p)) {
+    const int variant = kernel_variant();
+    if ((variant == 0 || variant == 3) && gemm_f8_few_supported(p)) {
+        log_choice(call, "few-rows kernel");
+        return launch_gemm_f8_few(p, stream_of(stream));
+    }
+    if (variant != 1 && gemm_f8_pair_supported(p)) {
         log_choice(call, "CTA-pair tcgen05 kernel");
         return launch_gemm_f8_pair(p, stream_of(stream));
     }

@@ -9,7 +9,7 @@
 //
 //   warp 0       TMA producer    per block: the CTA's 128 rows of A and its half of the tile's rows of Bt, 128 bytes
 //                                each, 128-byte swizzle; rows past the end of the segment are not loaded
-//   warp 1       MMA issuer      (leader CTA) four 32-deep steps per block and 128 columns
+//   warps 1, 2   MMA issuers     (leader CTA) four 32-deep steps per block and 128 columns
 //   warps 4..11  accumulators    each thread one row and BN / 2 columns; then scaled sums out through swizzled
 //                                staging slices and TMA stores (whole 32-row groups) or 16-byte stores (ragged ones)
 //
@@ -238,7 +238,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(bar_full(s), 2);       // one announcement per CTA's producer
-            mbar_init(bar_empty(s), 1);      // the leader's commit
+            mbar_init(bar_empty(s), HALVES);  // the leader's commits, one per issuer that reads the stage
         }
         for (int a = 0; a < 4; ++a) {
             mbar_init(bar_tfull(a), 1);
@@ -276,7 +276,10 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         // ------------------------------------------------------------ TMA producer
         const uint32_t full_leader = map_to_cta(bar_full(0), leader);
         uint32_t st = 0, ph = 0;
-        for (int tile = cluster_id; walk.get(tile, t); tile += nclusters) {
+        Tile next;
+        bool more = walk.get(cluster_id, next);
+        for (int tile = cluster_id; more;) {
+            t = next;
             share(t);
             const int rows = clamp_to(t.m_end - t.m0 - (int)rank * TMC, 0, TMC);
             const int arow = (int)t.arow + (int)rank * TMC;
@@ -300,45 +303,55 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 __syncwarp();
                 if (++st == C::STAGES) { st = 0; ph ^= 1u; }
             }
-            if (lds32(abort_flag)) break;
+            more = walk.get(tile += nclusters, next) && !lds32(abort_flag);
         }
         __syncwarp();
         cluster_sync_all();
         if (SPLIT) cluster_sync_all();
-    } else if (warp == 1) {
-        // ------------------------------------------------------------ pair MMA issuer (leader)
+    } else if (warp < 3) {
+        // ------------------------------------------------------------ pair MMA issuers (leader)
+        // Each block's product has a slot of its own, so its order does not matter.  One warp's waits and commits
+        // for a block take longer than its multiplication: two warps share them, by column half, or by blocks
+        // in turn where there is one half.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         if (rank == 0) {
+            const int who = warp - 1;
             Walk<BN> walk(p, lane);
             const uint16_t both = (uint16_t)(3u << leader);
             const uint64_t desc0 = make_kmajor_sw128_desc(sbase);
-            uint32_t st = 0, ph = 0, used[HALVES] = {};
-            for (int tile = cluster_id; walk.get(tile, t); tile += nclusters) {
+            const uint64_t bstep = (uint64_t)((TMC + (HALVES == 2 ? 64 * who : 0)) * ROWB >> 4);
+            uint32_t st = 0, ph = 0, u = 0;
+            Tile next;
+            bool more = walk.get(cluster_id, next);
+            for (int tile = cluster_id; more;) {
+                t = next;
                 share(t);
-                const int halves = HALVES == 2 && g.N - t.n0 > 128 ? 2 : 1;
+                tile += nclusters;
+                if (t.nkb == 0) more = walk.get(tile, next);
+                const bool empty = HALVES == 2 && who == 1 && g.N - t.n0 <= 128;     // no such half
                 for (int b = 0; b < t.nkb; ++b) {
-                    mbar_wait(bar_full(st), ph, abort_flag, g.status);
-                    tc_fence_after();
-                    const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4));
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h) {
-                        if (h >= halves) break;
-                        const uint32_t u = used[h]++;
-                        const int slot = HALVES == 2 ? h * 2 + (int)(u & 1u) : (int)(u & 3u);
-                        const uint32_t sph = (HALVES == 2 ? u >> 1 : u >> 2) & 1u;
-                        mbar_wait(bar_tempty(slot), sph ^ 1u, abort_flag, g.status);
+                    if (b == 1 || t.nkb == 1) more = walk.get(tile, next);     // while the first block is multiplied
+                    if (HALVES == 2 || (int)(u & 1u) == who) {
+                        mbar_wait(bar_full(st), ph, abort_flag, g.status);
                         tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t bdesc = adesc + (uint64_t)((TMC + 64 * h) * ROWB >> 4);
+                        if (!empty) {
+                            const int slot = HALVES == 2 ? who * 2 + (int)(u & 1u) : (int)(u & 3u);
+                            const uint32_t sph = (HALVES == 2 ? u >> 1 : u >> 2) & 1u;
+                            mbar_wait(bar_tempty(slot), sph ^ 1u, abort_flag, g.status);
+                            tc_fence_after();
+                            const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4));
+                            if (elect_one()) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                tc_mma_f8_pair(tmem_base + (uint32_t)(slot * 128), adesc + (uint64_t)(2 * i),
-                                               bdesc + (uint64_t)(2 * i), i ? 1u : 0u);
-                            tc_commit_pair(bar_tfull(slot), both);
-                            if (h == halves - 1) tc_commit_pair(bar_empty(st), both);
+                                for (int i = 0; i < 4; ++i)
+                                    tc_mma_f8_pair(tmem_base + (uint32_t)(slot * 128), adesc + (uint64_t)(2 * i),
+                                                   adesc + bstep + (uint64_t)(2 * i), i ? 1u : 0u);
+                                tc_commit_pair(bar_tfull(slot), both);
+                            }
                         }
+                        if (elect_one()) tc_commit_pair(bar_empty(st), both);
                         __syncwarp();
                     }
+                    if (HALVES == 1 || !empty) ++u;
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
                 if (lds32(abort_flag)) break;
@@ -349,7 +362,8 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         cluster_sync_all();      // no CTA leaves or frees tensor memory while another may still use it
         if (SPLIT) cluster_sync_all();
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+        if (warp == 1)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         cluster_sync_all();
@@ -364,37 +378,51 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         const uint32_t sb_s = sbase + C::OFF_SB + (uint32_t)(set * 2 * 4 * CW * 4);
         const int st_id = lg * 32 + lane;                 // thread of the set
         uint32_t used = 0;
-        for (int tile = cluster_id; walk.get(tile, t); tile += nclusters) {
+        // what I need of a tile
+        int c0, rows, nkb, row;                           // first column, valid rows from my warp's first, blocks, my row of A
+        bool live;
+        int64_t crow;                                     // C row of my warp's first
+        const float *sa_at, *sb_at;
+        float sa[4], sb[4];
+        auto enter = [&]() {
             share(t);
-            const int c0 = t.n0 + set * CW;               // my first column
-            if (HALVES == 2 && set == 1 && g.N - t.n0 <= 128) continue;     // nothing is multiplied there
-            const int row = t.m0 + (int)rank * TMC + lg * 32 + lane;
-            const int rows = t.m_end - (t.m0 + (int)rank * TMC + lg * 32);  // valid rows from my warp's first
-            const bool live = rows > 0 && c0 < g.N;
+            const int m0 = t.m0 + (int)rank * TMC + lg * 32;
+            c0 = t.n0 + set * CW;
+            rows = t.m_end - m0;
+            row = m0 + lane;
+            live = rows > 0 && c0 < g.N;
+            nkb = HALVES == 2 && set == 1 && g.N - t.n0 <= 128 ? 0 : t.nkb;     // nothing is multiplied in my half
+            crow = t.crow + (int)rank * TMC + lg * 32;
             const int64_t kb0 = t.k0 / ROWB;
-            const float* sa_at = g.SA + kb0 * g.ldsa + row;
-            const float* sb_at = g.SB + (BROWS ? kb0 * g.ldsb : (t.sbrow + (HALVES == 2 ? set : 0)) * g.ldsb + kb0);
-            float sa[4] = {}, sb[4] = {};
-            // the next four blocks' scales, loaded a round of four blocks ahead
-            auto fetch = [&](int b0) {
+            sa_at = g.SA + kb0 * g.ldsa + row;
+            sb_at = g.SB + (BROWS ? kb0 * g.ldsb : (t.sbrow + (HALVES == 2 ? set : 0)) * g.ldsb + kb0);
+        };
+        // scales of blocks b0 .. b0 + 3, loaded a round of four blocks ahead
+        auto fetch = [&](int b0) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool in = b0 + i < t.nkb;
-                    sa[i] = load_ahead(sa_at + (b0 + i) * g.ldsa, in && row < t.m_end);
-                    if (!BROWS) {
-                        sb[i] = load_ahead(sb_at + b0 + i, in && c0 < g.N);
-                    } else if (i < 4 * CW / 128) {
-                        const int el = i * 128 + st_id, kb = el / CW, n = c0 + el % CW;
-                        sb[i] = load_ahead(sb_at + (b0 + kb) * g.ldsb + n, b0 + kb < t.nkb && n < g.N);
-                    }
+            for (int i = 0; i < 4; ++i) {
+                const bool in = b0 + i < nkb;
+                sa[i] = load_ahead(sa_at + (b0 + i) * g.ldsa, in && rows > lane);
+                if (!BROWS) {
+                    sb[i] = load_ahead(sb_at + b0 + i, in && c0 < g.N);
+                } else if (i < 4 * CW / 128) {
+                    const int el = i * 128 + st_id, kb = el / CW, n = c0 + el % CW;
+                    sb[i] = load_ahead(sb_at + (b0 + kb) * g.ldsb + n, b0 + kb < nkb && n < g.N);
                 }
-            };
+            }
+        };
+        int tile = cluster_id;
+        bool more = walk.get(tile, t);
+        if (more) {
+            enter();
             fetch(0);
+        }
+        while (more) {
             unsigned long long acc[CW / 2];
 #pragma unroll
             for (int i = 0; i < CW / 2; ++i) acc[i] = 0;
 #pragma unroll 1
-            for (int b0 = 0; b0 < t.nkb; b0 += 4) {
+            for (int b0 = 0; b0 < nkb; b0 += 4) {
                 float s[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] = BROWS ? sa[i] : sa[i] * sb[i];
@@ -406,7 +434,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory");
                 }
                 fetch(b0 + 4);
-                const int n = min(4, t.nkb - b0);
+                const int n = min(4, nkb - b0);
 #pragma unroll 1
                 for (int i = 0; i < n; ++i) {
                     const uint32_t u = used++;
@@ -453,7 +481,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     s[0] = s[1]; s[1] = s[2]; s[2] = s[3];
                 }
             }
-            if (BROWS && t.nkb > 0) asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory");  // buffers free for the next tile
+            if (BROWS && nkb > 0) asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory");  // buffers free for the next tile
 
             if (SPLIT) {
                 // partial tile [128 rows][BN + 4] over the ring, which nothing reads or fills any more: this pair's
@@ -466,86 +494,93 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     unpack_f2(acc[2 * i + 1], v.z, v.w);
                     sts128(part + 16u * (uint32_t)i, v);
                 }
-            } else if (live) {
-                if (lane == 0) bulk_wait_read();           // the previous tile's stores have read my slices
-                __syncwarp();
+            }
+            // the next tile and its first scales, which arrive while this one is stored
+            const int c0_now = c0, rows_now = rows;
+            const int64_t crow_now = crow;
+            const bool store = !SPLIT && live;
+            more = walk.get(tile += nclusters, t);
+            if (more) {
+                enter();
+                fetch(0);
+            }
+            if (store) {
                 const int es = g.c_type == Q4_F32 ? 4 : 2, per = 128 / es;      // columns per slice
-                const int64_t crow = t.crow + (int)rank * TMC + lg * 32;
-                auto flush = [&](int q, uint32_t slice) {
-                    const int nc = c0 + q * per;
-                    __syncwarp();
+                // slices q0, q0 + 1 to memory
+                auto flush = [&](int q0) {
                     // a store clips rows and columns at the matrix's end, columns in pieces of 16 bytes only
-                    if (p.c_vec && rows >= 32 && (nc + per <= g.N || g.N * es % 16 == 0)) {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(&tmC, slice, nc, (int)crow);
-                            bulk_commit();
-                        }
-                        return;
-                    }
+                    const bool whole = p.c_vec && rows_now >= 32;
+                    fence_async_smem();
+                    __syncwarp();
 #pragma unroll 1
-                    for (int it = 0; it < 8; ++it) {
-                        const int rr = it * 4 + (lane >> 3), ch = lane & 7, col = nc + ch * (16 / es);
-                        const uint4 v = lds128(slice + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)));
-                        if (rr >= rows || col >= g.N) continue;
-                        uint8_t* dst = static_cast<uint8_t*>(g.C) + ((crow + rr) * g.ldc + col) * es;
-                        const int have = min(16 / es, g.N - col);
-                        if (p.c_vec && have == 16 / es) {
-                            *reinterpret_cast<uint4*>(dst) = v;
-                        } else {
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    for (int q = q0; q < q0 + 2; ++q) {
+                        const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
+                        const int nc = c0_now + q * per;
+                        if (q >= CW / per || nc >= g.N) break;
+                        if (whole && (nc + per <= g.N || g.N * es % 16 == 0)) {
+                            if (lane == 0) {
+                                tma_store_2d(&tmC, slice, nc, (int)crow_now);
+                                bulk_commit();
+                            }
+                            continue;
+                        }
+#pragma unroll 1
+                        for (int it = 0; it < 8 && it * 4 < rows_now; ++it) {
+                            const int rr = it * 4 + (lane >> 3), ch = lane & 7, col = nc + ch * (16 / es);
+                            const uint4 v = lds128(slice + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)));
+                            if (rr >= rows_now || col >= g.N) continue;
+                            uint8_t* dst = static_cast<uint8_t*>(g.C) + ((crow_now + rr) * g.ldc + col) * es;
+                            const int have = min(16 / es, g.N - col);
+                            if (p.c_vec && have == 16 / es) {
+                                *reinterpret_cast<uint4*>(dst) = v;
+                            } else {
+                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                if (j >= have) break;
-                                if (es == 4) { if (j < 4) reinterpret_cast<uint32_t*>(dst)[j] = w[j & 3]; }
-                                else reinterpret_cast<uint16_t*>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                                for (int j = 0; j < 8; ++j) {
+                                    if (j >= have) break;
+                                    if (es == 4) { if (j < 4) reinterpret_cast<uint32_t*>(dst)[j] = w[j & 3]; }
+                                    else reinterpret_cast<uint16_t*>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                                }
                             }
                         }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 };
+                const uint32_t mine = slices + (uint32_t)(lane * 128), sw = (uint32_t)(lane & 7);
                 if (g.c_type == Q4_F32) {
 #pragma unroll
-                    for (int q = 0; q < CW / 32; ++q) {
-                        if (c0 + q * 32 < g.N) {
-                            const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
-                            if (q >= 2) {
-                                if (lane == 0) bulk_wait_read_but_one();
-                                __syncwarp();
-                            }
+                    for (int q0 = 0; q0 < CW / 32; q0 += 2) {
+                        if (c0_now + q0 * 32 < g.N) {
+                            if (lane == 0) bulk_wait_read();           // earlier stores have read my slices
+                            __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
+                            for (int j = 0; j < 16; ++j) {
                                 uint4 v;
-                                unpack_f2(acc[16 * q + 2 * j], v.x, v.y);
-                                unpack_f2(acc[16 * q + 2 * j + 1], v.z, v.w);
-                                sts128(slice + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4)), v);
+                                unpack_f2(acc[16 * q0 + 2 * j], v.x, v.y);
+                                unpack_f2(acc[16 * q0 + 2 * j + 1], v.z, v.w);
+                                sts128(mine + (uint32_t)((j >> 3) * SLICE) + ((((uint32_t)j & 7u) ^ sw) << 4), v);
                             }
-                            flush(q, slice);
+                            flush(q0);
                         }
                     }
                 } else {
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
 #pragma unroll
-                    for (int q = 0; q < CW / 64; ++q) {
-                        if (c0 + q * 64 < g.N) {
-                            const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
+                    for (int j = 0; j < CW / 8; ++j) {
+                        uint32_t w[4];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                uint32_t w[4];
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    uint32_t lo, hi;
-                                    unpack_f2(acc[32 * q + 4 * j + k], lo, hi);
-                                    const float a = __uint_as_float(lo), b = __uint_as_float(hi);
-                                    w[k] = g.c_type == Q4_BF16 ? pack2(a, b, (const __nv_bfloat16*)nullptr)
-                                                               : pack2(a, b, (const __half*)nullptr);
-                                }
-                                sts128(slice + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4)),
-                                       make_uint4(w[0], w[1], w[2], w[3]));
-                            }
-                            flush(q, slice);
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t lo, hi;
+                            unpack_f2(acc[4 * j + k], lo, hi);
+                            const float x = __uint_as_float(lo), y = __uint_as_float(hi);
+                            w[k] = g.c_type == Q4_BF16 ? pack2(x, y, (const __nv_bfloat16*)nullptr)
+                                                       : pack2(x, y, (const __half*)nullptr);
                         }
+                        sts128(mine + (uint32_t)((j >> 3) * SLICE) + ((((uint32_t)j & 7u) ^ sw) << 4),
+                               make_uint4(w[0], w[1], w[2], w[3]));
                     }
+                    flush(0);
                 }
             }
             if (!BROWS && lds32(abort_flag)) break;      // with BROWS the set's warps stay together (named barrier)
