@@ -139,6 +139,7 @@ struct GemmF8Params {
 
 cudaError_t launch_f8_quantize(const f8::QuantizeParams& p, int x_type, bool blocks, cudaStream_t st);
 cudaError_t launch_gemm_f8_simt(const f8::GemmF8Params& p, cudaStream_t st);
+int         f8_pairs_of_device();              // SMs / 2 of the current device
 bool        gemm_f8_few_supported(const f8::GemmF8Params& p);
 q4_status   launch_gemm_f8_few(const f8::GemmF8Params& p, cudaStream_t st);
 bool        gemm_f8_pair_supported(const f8::GemmF8Params& p);

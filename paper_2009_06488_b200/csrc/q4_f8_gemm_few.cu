@@ -1,44 +1,47 @@
-// e4m3 product with block scales for few rows of A (tokens being decoded): every weight is read once,
-// straight from memory into the registers of warp-level matrix instructions.
+// e4m3 product with block scales for few rows of A (tokens being decoded): every weight is read once and
+// the weights' stream never pauses.
 //
 //   C[m][n] = sum over blocks b of 128 depth values of  SA[b][m] * SB(n, b) * sum_k a(m, k) b(n, k)
 //
-// The matrix instruction (16 x 8 x 32) has Bt's rows as its 16 and the rows of A as its 8.  A block of 8 warps
-// owns 16 * R rows of Bt; each warp takes every eighth depth block and keeps scaled binary32 sums, which are
-// added over the warps, in order, through shared memory.  The order of depth values inside a block is
-// free as long as both operands share it: lane (g, t) takes the 32 bytes t * 32 .. of the rows it
-// needs, so a quad of lanes reads a row's 128 bytes, and no operand passes through shared memory.
-// Bound: HBM.  The tensor memory path would first stage the same bytes in shared memory and drain a 128-row
-// accumulator per block for a handful of rows.
+// One persistent CTA per SM walks tiles of 16 * R rows of Bt (output columns) by up to 16 rows of A of one
+// expert.  Four producer warps keep a ring of stages filled by TMA, a block of depth per stage: the tile's rows of Bt,
+// 16 rows of A (128-byte swizzle) and their scales (4-byte asynchronous copies), tile after tile without a
+// break.  Eight consumer warps take the stages in turn: warp-level matrix instructions (16 x 8 x 32) with
+// Bt's rows as their 16 and the rows of A as their 8, scaled binary32 sums in registers, which are added over the
+// warps, in order, at the tile's end while the next tiles' stages arrive.
+// The order of depth values inside a block is free as long as both operands share it: lane (g, t) takes
+// 16-byte pieces 2 t and 2 t + 1 of its rows, which the swizzle spreads over all banks.
+// Bound: HBM.  The tensor memory kernel would drain a 128-row accumulator per block for a handful of rows.
+#include <cuda.h>
+
 #include "q4_f8.cuh"
+#include "q4_tc_ptx.cuh"
 
 namespace q4 {
+
+bool make_byte_map(CUtensorMap* tm, const uint8_t* base, int64_t ld, int rows, int kbytes, int box_rows);
+
 namespace f8 {
 
-constexpr int NWARP = 8;
+constexpr int CONSUMERS = 8, PRODUCERS = 4;
+constexpr int MB = 16;                    // rows of A per tile
 
-struct Chunk { uint4 lo, hi; };           // 32 consecutive depth values
+template <int R> struct FewCfg {
+    static constexpr int NB = 16 * R;                          // rows of Bt per tile
+    static constexpr int STAGE = (NB + MB) * BLK;
+    static constexpr int STAGES = R == 4 ? 14 : 24;
+    static constexpr int OFF_SCALE = STAGES * STAGE;           // per stage: 16 SA, 64 SB
+    static constexpr int SCALE = (MB + 64) * 4;
+    static constexpr int OFF_PART = OFF_SCALE + STAGES * SCALE;
+    static constexpr int PITCH = NB + 4;
+    static constexpr int PART = CONSUMERS * MB * PITCH * 4;    // two of them, in turn
+    static constexpr int OFF_CUM = OFF_PART + 2 * PART;        // tiles before each expert
+    static constexpr int OFF_BAR = OFF_CUM + (Q4_MAX_EXPERTS + 32) * 4;
+    static constexpr int OFF_MISC = OFF_BAR + 2 * STAGES * 8;
+    static constexpr int SMEM = OFF_MISC + 16 + 1024;
+    static_assert(STAGE % 1024 == 0 && SMEM <= 232448, "shared memory");
+};
 
-// Depth values x .. x + 31 of a row; those at or past `end` read 0 (the bytes may hold anything).
-__device__ __forceinline__ Chunk load_chunk(const uint8_t* row, int x, int end, bool on)
-{
-    Chunk c;
-    c.lo = c.hi = make_uint4(0, 0, 0, 0);
-    if (!on) return c;
-    if (x < end) c.lo = __ldg(reinterpret_cast<const uint4*>(row + x));
-    if (x + 16 < end) c.hi = __ldg(reinterpret_cast<const uint4*>(row + x + 16));
-    return c;
-}
-__device__ __forceinline__ void mask_word(uint32_t& w, int valid)        // valid bytes of a word
-{
-    if (valid <= 0) w = 0;
-    else if (valid < 4) w &= (1u << (8 * valid)) - 1u;
-}
-__device__ __forceinline__ void mask_chunk(Chunk& c, int valid)
-{
-    mask_word(c.lo.x, valid);      mask_word(c.lo.y, valid - 4);  mask_word(c.lo.z, valid - 8);  mask_word(c.lo.w, valid - 12);
-    mask_word(c.hi.x, valid - 16); mask_word(c.hi.y, valid - 20); mask_word(c.hi.z, valid - 24); mask_word(c.hi.w, valid - 28);
-}
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
@@ -46,119 +49,228 @@ __device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-// R: groups of 16 rows of Bt per block; NT: groups of 8 rows of A per pass.
-template <int R, int NT>
-__global__ void __launch_bounds__(NWARP * 32, R == 2 ? 2 : 3)
-gemm_f8_few_kernel(const GemmF8Params p)
+__device__ __forceinline__ void copy_scale(uint32_t dst, const float* src, bool in)
 {
-    constexpr int NB = 16 * R, MB = 8 * NT;
-    __shared__ float part[NWARP][MB][NB + 4];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * NB, e = blockIdx.y;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+
+struct FewTile { int e, n0, m0, rows; };
+
+// Tile t of the walk, by a whole warp: the expert whose tiles cover it (cum: tiles before each expert, E padded to
+// a multiple of 32 with the total), then row groups fastest, so that they share the weights in L2.
+template <int R>
+__device__ __forceinline__ FewTile few_tile(const GemmF8Params& p, uint32_t cum_s, int t, int lane)
+{
+    constexpr int NB = 16 * R;
+    FewTile f;
+    int lo = 0, hi = p.M;
+    f.e = 0;
+    int local = t;
+    if (p.mode == kExpertRows) {
+        const int blocks = (p.E + 31) / 32;
+        const int b = __popc(__ballot_sync(0xFFFFFFFFu, lane < blocks && lds32(cum_s + 4u * (uint32_t)(lane < blocks ? lane * 32 : 0)) <= t)) - 1;
+        const int c = lds32(cum_s + 4u * (uint32_t)(b * 32 + lane));
+        const int i = __popc(__ballot_sync(0xFFFFFFFFu, c <= t)) - 1;
+        f.e = b * 32 + i;
+        local = t - __shfl_sync(0xFFFFFFFFu, c, i);
+        lo = min(max(p.starts[f.e], 0), p.M);
+        hi = min(max(p.starts[f.e + 1], lo), p.M);
+    }
+    const int groups = (hi - lo + MB - 1) / MB, n = local / groups;
+    f.n0 = n * NB;
+    f.m0 = lo + (local - n * groups) * MB;
+    f.rows = min(MB, hi - f.m0);
+    return f;
+}
+
+template <int R>
+__global__ void __launch_bounds__((CONSUMERS + PRODUCERS) * 32, 1)
+gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmF8Params p)
+{
+    using C = FewCfg<R>;
+    constexpr int NB = C::NB;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t cum_s = sbase + C::OFF_CUM, bar0 = sbase + C::OFF_BAR, abort_flag = sbase + C::OFF_MISC;
+    auto bar_full  = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+    auto bar_empty = [&](int s) { return bar0 + 8u * (uint32_t)(C::STAGES + s); };
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int ntn = (p.N + NB - 1) / NB, nkb = (p.K + BLK - 1) / BLK;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(bar_full(s), 1 + 32);        // the copies' announcement, and each producer lane's scales
+            mbar_init(bar_empty(s), 1);
+        }
+        sts32(abort_flag, 0);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int m_lo = 0, m_hi = p.M;
-    int64_t brow = n0, sbrow = n0 / BLK;
+    int ntiles = (p.M + MB - 1) / MB * ntn;
     if (p.mode == kExpertRows) {
-        m_lo = min(max(p.starts[e], 0), p.M);
-        m_hi = min(max(p.starts[e + 1], m_lo), p.M);
-        brow += (int64_t)e * p.N;
-        sbrow += e * blocks_of(p.N);
-    }
-    const int nkb = (p.K + BLK - 1) / BLK;
-    const int rows_n = min(NB, p.N - n0);
-    const uint8_t* wrow = p.Bt + (brow + g) * p.ldb + t * 32;
-
-    for (int m0 = m_lo; m0 < m_hi; m0 += MB) {
-        const int rows_m = min(MB, m_hi - m0);
-        float acc[R][NT][4] = {};
-        const uint8_t* arow = p.A + (int64_t)(m0 + g) * p.lda + t * 32;
-#pragma unroll (R * NT == 1 ? 2 : 1)
-        for (int b = warp; b < nkb; b += NWARP) {
-            const int x = b * BLK, left = p.K - x - t * 32;       // depth values left from my first
-            Chunk w[R][2];
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    w[r][h] = load_chunk(wrow + (int64_t)(16 * r + 8 * h) * p.ldb + x, 0, left, 16 * r + 8 * h + g < rows_n);
-            Chunk a[NT];
-            float sa[NT][2], sb[R][2];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                a[j] = load_chunk(arow + (int64_t)(8 * j) * p.lda + x, 0, left, 8 * j + g < rows_m);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int m = 8 * j + 2 * t + c;
-                    sa[j][c] = m < rows_m ? __ldg(p.SA + b * p.ldsa + m0 + m) : 0.0f;
+        if (warp == 0) {
+            int at = 0;
+            for (int e0 = 0; e0 < p.E; e0 += 32) {
+                const int e = e0 + lane;
+                int s = 0;
+                if (e < p.E) {
+                    const int lo = min(max(p.starts[e], 0), p.M), hi = min(max(p.starts[e + 1], lo), p.M);
+                    s = (hi - lo + MB - 1) / MB * ntn;
                 }
-            }
+                const int own = s;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int n = 16 * r + 8 * h + g;
-                    sb[r][h] = n >= rows_n ? 0.0f : p.b_rows ? __ldg(p.SB + b * p.ldsb + n0 + n) : __ldg(p.SB + sbrow * p.ldsb + b);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(0xFFFFFFFFu, s, o);
+                    if (lane >= o) s += v;
                 }
-            if (x + BLK > p.K) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) { mask_chunk(w[r][0], left); mask_chunk(w[r][1], left); }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) mask_chunk(a[j], left);
+                // an expert without tiles repeats the next one's number and is never the last that is <= t
+                sts32(cum_s + 4u * (uint32_t)e, e < p.E ? at + s - own : INT32_MAX);
+                at += __shfl_sync(0xFFFFFFFFu, s, 31);
             }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (8 * j >= rows_m) break;
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    float d[4] = {};
-                    const Chunk& u = w[r][0];
-                    const Chunk& v = w[r][1];
-                    mma_e4m3(d, u.lo.x, v.lo.x, u.lo.y, v.lo.y, a[j].lo.x, a[j].lo.y);
-                    mma_e4m3(d, u.lo.z, v.lo.z, u.lo.w, v.lo.w, a[j].lo.z, a[j].lo.w);
-                    mma_e4m3(d, u.hi.x, v.hi.x, u.hi.y, v.hi.y, a[j].hi.x, a[j].hi.y);
-                    mma_e4m3(d, u.hi.z, v.hi.z, u.hi.w, v.hi.w, a[j].hi.z, a[j].hi.w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[r][j][i] = fmaf(d[i] * sb[r][i >> 1], sa[j][i & 1], acc[r][j][i]);
-                }
-            }
+            if (lane == 0) sts32(abort_flag + 4, at);
         }
+    }
+    __syncthreads();
+    if (p.mode == kExpertRows) ntiles = lds32(abort_flag + 4);
+
+    if (warp >= CONSUMERS) {
+        // ------------------------------------------------------------ producer
+        // a stage's waits, copies and arrivals take one warp about 500 clk, twice what its bytes take: four warps in turn
+        int it = 0;
+        for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
+            const FewTile f = few_tile<R>(p, cum_s, tile, lane);
+            const int64_t brow = (int64_t)f.e * p.N + f.n0;
+            const float* sb = p.b_rows ? p.SB + f.n0 + lane : p.SB + (f.e * blocks_of(p.N) + f.n0 / BLK) * p.ldsb;
+            const float* sa = p.SA + f.m0 + lane;
+            for (int b = 0; b < nkb; ++b, ++it) {
+                if ((it & (PRODUCERS - 1)) != warp - CONSUMERS) continue;
+                const int st = it % C::STAGES;
+                mbar_wait_suspend(bar_empty(st), ((uint32_t)(it / C::STAGES) & 1u) ^ 1u, abort_flag, p.status);
+                const uint32_t dst = sbase + st * C::STAGE, sc = sbase + C::OFF_SCALE + st * C::SCALE;
+                if (elect_one()) {
+                    mbar_expect_tx(bar_full(st), (uint32_t)C::STAGE);
+                    tma_load_2d(dst, &tmB, b * BLK, (int)brow, bar_full(st));
+                    tma_load_2d(dst + NB * BLK, &tmA, b * BLK, f.m0, bar_full(st));
+                }
+                __syncwarp();
+                if (lane < MB) copy_scale(sc + 4u * (uint32_t)lane, lane < f.rows ? sa + b * p.ldsa : p.SA, lane < f.rows);
+                if (p.b_rows) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+                    for (int i = 0; i < NB / 32; ++i)
+                        copy_scale(sc + 4u * (uint32_t)(MB + lane + 32 * i), f.n0 + lane + 32 * i < p.N ? sb + b * p.ldsb + 32 * i : p.SB,
+                                   f.n0 + lane + 32 * i < p.N);
+                } else if (lane == MB) {
+                    copy_scale(sc + 4u * MB, sb + b, true);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full(st)) : "memory");
+            }
+            if (lds32(abort_flag)) break;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
+    // ---------------------------------------------------------------- consumers
+    const int g = lane >> 2, t = lane & 3;
+    const uint32_t p0 = (uint32_t)(g * BLK + (((2 * t) ^ g) << 4)), p1 = (uint32_t)(g * BLK + (((2 * t + 1) ^ g) << 4));
+    int first = 0, buf = 0;                       // stage (over all tiles) of the tile's first block
+    for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x, first += nkb, buf ^= 1) {
+        const FewTile f = few_tile<R>(p, cum_s, tile, lane);
+        float acc[R][2][4] = {};
+        for (int b = warp; b < nkb; b += CONSUMERS) {
+            const int it = first + b, st = it % C::STAGES;
+            mbar_wait_suspend(bar_full(st), (uint32_t)(it / C::STAGES) & 1u, abort_flag, p.status);
+            const uint32_t ws = sbase + st * C::STAGE, as = ws + NB * BLK, sc = sbase + C::OFF_SCALE + st * C::SCALE;
+            uint4 a[2][2];
+            float sa[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                a[j][0] = lds128(as + 8 * j * BLK + p0);
+                a[j][1] = lds128(as + 8 * j * BLK + p1);
+                sa[j][0] = __int_as_float(lds32(sc + 4u * (uint32_t)(8 * j + 2 * t)));
+                sa[j][1] = __int_as_float(lds32(sc + 4u * (uint32_t)(8 * j + 2 * t + 1)));
+            }
+            const float sb = __int_as_float(lds32(sc + 4u * MB));
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const uint4 u0 = lds128(ws + 16 * r * BLK + p0), u1 = lds128(ws + 16 * r * BLK + p1);
+                const uint4 v0 = lds128(ws + (16 * r + 8) * BLK + p0), v1 = lds128(ws + (16 * r + 8) * BLK + p1);
+                float s0 = sb, s1 = sb;
+                if (p.b_rows) {
+                    s0 = __int_as_float(lds32(sc + 4u * (uint32_t)(MB + 16 * r + g)));
+                    s1 = __int_as_float(lds32(sc + 4u * (uint32_t)(MB + 16 * r + 8 + g)));
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (8 * j >= f.rows) break;
+                    float d[4] = {};
+                    mma_e4m3(d, u0.x, v0.x, u0.y, v0.y, a[j][0].x, a[j][0].y);
+                    mma_e4m3(d, u0.z, v0.z, u0.w, v0.w, a[j][0].z, a[j][0].w);
+                    mma_e4m3(d, u1.x, v1.x, u1.y, v1.y, a[j][1].x, a[j][1].y);
+                    mma_e4m3(d, u1.z, v1.z, u1.w, v1.w, a[j][1].z, a[j][1].w);
+                    acc[r][j][0] = fmaf(d[0] * s0, sa[j][0], acc[r][j][0]);
+                    acc[r][j][1] = fmaf(d[1] * s0, sa[j][1], acc[r][j][1]);
+                    acc[r][j][2] = fmaf(d[2] * s1, sa[j][0], acc[r][j][2]);
+                    acc[r][j][3] = fmaf(d[3] * s1, sa[j][1], acc[r][j][3]);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_empty(st));
+        }
+        // partial sums [warp][row of A][row of Bt]; the barrier of the next tile tells that these have been read
+        const uint32_t part = sbase + C::OFF_PART + (uint32_t)(buf * C::PART);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (8 * j >= f.rows) break;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[warp][8 * j + 2 * t + (i & 1)][16 * r + 8 * (i >> 1) + g] = acc[r][j][i];
-        __syncthreads();
-        for (int u = threadIdx.x; u < rows_m * NB; u += NWARP * 32) {
+                for (int i = 0; i < 4; ++i)
+                    sts32(part + 4u * (uint32_t)((warp * MB + 8 * j + 2 * t + (i & 1)) * C::PITCH + 16 * r + 8 * (i >> 1) + g),
+                          __float_as_int(acc[r][j][i]));
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        for (int u = threadIdx.x; u < f.rows * NB; u += CONSUMERS * 32) {
             const int m = u / NB, n = u % NB;
-            if (n >= rows_n) continue;
+            if (f.n0 + n >= p.N) continue;
             float v = 0.0f;
 #pragma unroll
-            for (int k = 0; k < NWARP; ++k) v += part[k][m][n];
-            const int64_t at = (int64_t)(m0 + m) * p.ldc + n0 + n;
+            for (int k = 0; k < CONSUMERS; ++k) v += __int_as_float(lds32(part + 4u * (uint32_t)((k * MB + m) * C::PITCH + n)));
+            const int64_t at = (int64_t)(f.m0 + m) * p.ldc + f.n0 + n;
             if (p.c_type == Q4_F32) static_cast<float*>(p.C)[at] = v;
             else if (p.c_type == Q4_BF16) static_cast<__nv_bfloat16*>(p.C)[at] = __float2bfloat16_rn(v);
             else static_cast<__half*>(p.C)[at] = __float2half_rn(v);
         }
-        __syncthreads();
     }
 }
 
-template <int R, int NT>
-static q4_status launch_few(const GemmF8Params& p, cudaStream_t st)
+template <int R>
+static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaStream_t st)
 {
+    using C = FewCfg<R>;
+    CUtensorMap a, b;
+    if (!make_byte_map(&a, p.A, p.lda, p.M, p.K, MB) ||
+        !make_byte_map(&b, p.Bt, p.ldb, (int)(p.mode == kExpertRows ? (int64_t)p.E * p.N : p.N), p.K, C::NB)) return Q4_ERR_CUDA;
+    static bool ready[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return Q4_ERR_CUDA;
+    if (!ready[dev]) {
+        if (cudaFuncSetAttribute(gemm_f8_few_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
+            return Q4_ERR_CUDA;
+        ready[dev] = true;
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((p.N + 16 * R - 1) / (16 * R)), (unsigned)(p.mode == kExpertRows ? p.E : 1));
-    cfg.blockDim = dim3(NWARP * 32);
+    cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
+    cfg.blockDim = dim3((CONSUMERS + PRODUCERS) * 32);
+    cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_few_kernel<R, NT>, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_few_kernel<R>, a, b, p);
     count_launch();
     return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
@@ -170,13 +282,17 @@ using namespace f8;
 bool gemm_f8_few_supported(const GemmF8Params& g)
 {
     if ((uintptr_t)g.A % 16 || (uintptr_t)g.Bt % 16 || g.lda % 16 || g.ldb % 16) return false;
+    if ((int64_t)g.N * (g.mode == kExpertRows ? g.E : 1) >= INT32_MAX - 512) return false;
     return g.mode == kExpertRows ? g.M <= 8 * (int64_t)g.E : g.mode == kDense && g.M <= 16;
 }
 
 q4_status launch_gemm_f8_few(const GemmF8Params& p, cudaStream_t st)
 {
-    if (p.mode == kExpertRows) return launch_few<2, 2>(p, st);
-    return p.M <= 8 ? launch_few<1, 1>(p, st) : launch_few<1, 2>(p, st);
+    const int sms = 2 * f8_pairs_of_device();
+    const int64_t groups = p.mode == kExpertRows ? (p.M + MB - 1) / MB + (p.E < p.M ? p.E : p.M) : (p.M + MB - 1) / MB;
+    // 64 columns per tile where the tiles still go round the SMs a few times; else 32
+    const int64_t t64 = groups * (((int64_t)p.N + 63) / 64), t32 = groups * (((int64_t)p.N + 31) / 32);
+    return t64 >= 4 * sms ? launch_few<4>(p, t64, sms, st) : launch_few<2>(p, t32, sms, st);
 }
 
 }  // namespace q4

@@ -655,19 +655,6 @@ static bool make_out_map(CUtensorMap* tm, void* base, int type, int64_t ldc, int
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static int pairs_of_device()
-{
-    static int per_dev[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 74;
-    if (!per_dev[dev]) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) n = 148;
-        per_dev[dev] = n / 2;
-    }
-    return per_dev[dev];
-}
-
 template <int HALVES, bool BROWS, bool SPLIT>
 static q4_status launch_pair(const PairParams& p, const CUtensorMap& a, const CUtensorMap& few, const CUtensorMap& b,
                              const CUtensorMap& c, int64_t clusters, cudaStream_t st)
@@ -705,6 +692,19 @@ static q4_status launch_pair(const PairParams& p, const CUtensorMap& a, const CU
 
 using namespace f8;
 
+int f8_pairs_of_device()
+{
+    static int per_dev[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 74;
+    if (!per_dev[dev]) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) n = 148;
+        per_dev[dev] = n / 2;
+    }
+    return per_dev[dev];
+}
+
 bool gemm_f8_pair_supported(const GemmF8Params& g)
 {
     // A's rows of a tile may pass M by up to a tile; the maps count rows in 32 bits
@@ -718,7 +718,7 @@ q4_status launch_gemm_f8_pair(const GemmF8Params& g, cudaStream_t st)
     p.g = g;
     p.tiles_m = (g.M + 255) / 256;
     const int64_t nkb = blocks_of(g.K);
-    const int pairs = pairs_of_device();
+    const int pairs = f8_pairs_of_device();
     const int64_t products = g.mode == kExpertDepth ? g.E : 1;
     const int64_t n256 = ((int64_t)g.N + 255) / 256, n128 = ((int64_t)g.N + 127) / 128;
     // row tiles: an expert's last one is its own
