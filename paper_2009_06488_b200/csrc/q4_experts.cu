@@ -258,7 +258,7 @@ __device__ __forceinline__ float reduce8(float (&d)[8], int lane)
 }
 
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, VEC ? 3 : 1)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
     using T = typename f8::Elem<TYPE>::T;

@@ -3,9 +3,9 @@
 //
 //   C[m][n] = sum over blocks b of 128 depth values of  SA[b][m] * SB(n, b) * sum_k a(m, k) b(n, k)
 //
-// One persistent CTA per SM walks tiles of 16 * R rows of Bt (output columns) by up to 16 rows of A of one
-// expert.  Four producer warps keep a ring of stages filled by TMA, a block of depth per stage: the tile's rows of Bt,
-// 16 rows of A (128-byte swizzle) and their scales (4-byte asynchronous copies), tile after tile without a
+// One persistent CTA per SM walks tiles of 16 * R rows of Bt (output columns) by up to MB (16 or 32) rows of A of one
+// expert.  Producer warps keep a ring of stages filled by TMA, a block of depth per stage: the tile's rows of Bt,
+// MB rows of A (128-byte swizzle) and their scales (4-byte asynchronous copies), tile after tile without a
 // break.  Eight consumer warps take the stages in turn: warp-level matrix instructions (16 x 8 x 32) with
 // Bt's rows as their 16 and the rows of A as their 8, scaled binary32 sums in registers, which are added over the
 // warps, in order, at the tile's end while the next tiles' stages arrive.
@@ -23,19 +23,27 @@ bool make_byte_map(CUtensorMap* tm, const uint8_t* base, int64_t ld, int rows, i
 
 namespace f8 {
 
-constexpr int CONSUMERS = 8, PRODUCERS = 4;
-constexpr int MB = 16;                    // rows of A per tile
+constexpr int CONSUMERS = 8;
 
-template <int R> struct FewCfg {
+// R: groups of 16 rows of Bt per tile; MB: rows of A per tile (16 or 32).
+template <int R, int MB> struct FewCfg {
     static constexpr int NB = 16 * R;                          // rows of Bt per tile
+    // A stage's waits, copies and arrivals take a producer warp about 500 clk, two to four times what its bytes
+    // take: four warps in turn, eight for the smallest stage (16384 x 4096: 17.5 -> 15.1 us; they cost
+    // the others registers: 64 experts 22 -> 23 us)
+    static constexpr int PRODUCERS = R == 2 && MB == 16 ? 8 : 4;
     static constexpr int STAGE = (NB + MB) * BLK;
-    static constexpr int STAGES = R == 4 ? 14 : 24;
-    static constexpr int OFF_SCALE = STAGES * STAGE;           // per stage: 16 SA, 64 SB
+    // Stage s is always filled by producer s % PRODUCERS and emptied by consumer s % CONSUMERS: a wait on a
+    // barrier's parity is only right for a warp that has seen the round before.
+    static constexpr int STAGES = R == 4 || MB == 32 ? 16 : 24;
+    static_assert(STAGES % PRODUCERS == 0 && STAGES % CONSUMERS == 0, "a stage belongs to one producer and one consumer");
+    static constexpr int OFF_SCALE = STAGES * STAGE;           // per stage: MB SA, 64 SB
     static constexpr int SCALE = (MB + 64) * 4;
     static constexpr int OFF_PART = OFF_SCALE + STAGES * SCALE;
     static constexpr int PITCH = NB + 4;
-    static constexpr int PART = CONSUMERS * MB * PITCH * 4;    // two of them, in turn
-    static constexpr int OFF_CUM = OFF_PART + 2 * PART;        // tiles before each expert
+    static constexpr int PART = CONSUMERS * MB * PITCH * 4;
+    static constexpr int PARTS = R == 4 ? 1 : 2;               // two take turns where they fit
+    static constexpr int OFF_CUM = OFF_PART + PARTS * PART;        // tiles before each expert
     static constexpr int OFF_BAR = OFF_CUM + (Q4_MAX_EXPERTS + 32) * 4;
     static constexpr int OFF_MISC = OFF_BAR + 2 * STAGES * 8;
     static constexpr int SMEM = OFF_MISC + 16 + 1024;
@@ -58,7 +66,7 @@ struct FewTile { int e, n0, m0, rows; };
 
 // Tile t of the walk, by a whole warp: the expert whose tiles cover it (cum: tiles before each expert, E padded to
 // a multiple of 32 with the total), then row groups fastest, so that they share the weights in L2.
-template <int R>
+template <int R, int MB>
 __device__ __forceinline__ FewTile few_tile(const GemmF8Params& p, uint32_t cum_s, int t, int lane)
 {
     constexpr int NB = 16 * R;
@@ -83,12 +91,12 @@ __device__ __forceinline__ FewTile few_tile(const GemmF8Params& p, uint32_t cum_
     return f;
 }
 
-template <int R>
-__global__ void __launch_bounds__((CONSUMERS + PRODUCERS) * 32, 1)
+template <int R, int MB>
+__global__ void __launch_bounds__((CONSUMERS + FewCfg<R, MB>::PRODUCERS) * 32, 1)
 gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmF8Params p)
 {
-    using C = FewCfg<R>;
-    constexpr int NB = C::NB;
+    using C = FewCfg<R, MB>;
+    constexpr int NB = C::NB, NT = MB / 8;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t cum_s = sbase + C::OFF_CUM, bar0 = sbase + C::OFF_BAR, abort_flag = sbase + C::OFF_MISC;
@@ -137,15 +145,14 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
     if (warp >= CONSUMERS) {
         // ------------------------------------------------------------ producer
-        // a stage's waits, copies and arrivals take one warp about 500 clk, twice what its bytes take: four warps in turn
         int it = 0;
         for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
-            const FewTile f = few_tile<R>(p, cum_s, tile, lane);
+            const FewTile f = few_tile<R, MB>(p, cum_s, tile, lane);
             const int64_t brow = (int64_t)f.e * p.N + f.n0;
             const float* sb = p.b_rows ? p.SB + f.n0 + lane : p.SB + (f.e * blocks_of(p.N) + f.n0 / BLK) * p.ldsb;
             const float* sa = p.SA + f.m0 + lane;
             for (int b = 0; b < nkb; ++b, ++it) {
-                if ((it & (PRODUCERS - 1)) != warp - CONSUMERS) continue;
+                if ((it & (C::PRODUCERS - 1)) != warp - CONSUMERS) continue;
                 const int st = it % C::STAGES;
                 mbar_wait_suspend(bar_empty(st), ((uint32_t)(it / C::STAGES) & 1u) ^ 1u, abort_flag, p.status);
                 const uint32_t dst = sbase + st * C::STAGE, sc = sbase + C::OFF_SCALE + st * C::SCALE;
@@ -161,7 +168,7 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     for (int i = 0; i < NB / 32; ++i)
                         copy_scale(sc + 4u * (uint32_t)(MB + lane + 32 * i), f.n0 + lane + 32 * i < p.N ? sb + b * p.ldsb + 32 * i : p.SB,
                                    f.n0 + lane + 32 * i < p.N);
-                } else if (lane == MB) {
+                } else if (lane == 0) {
                     copy_scale(sc + 4u * MB, sb + b, true);
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full(st)) : "memory");
@@ -176,16 +183,16 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const uint32_t p0 = (uint32_t)(g * BLK + (((2 * t) ^ g) << 4)), p1 = (uint32_t)(g * BLK + (((2 * t + 1) ^ g) << 4));
     int first = 0, buf = 0;                       // stage (over all tiles) of the tile's first block
     for (int tile = blockIdx.x; tile < ntiles; tile += gridDim.x, first += nkb, buf ^= 1) {
-        const FewTile f = few_tile<R>(p, cum_s, tile, lane);
-        float acc[R][2][4] = {};
-        for (int b = warp; b < nkb; b += CONSUMERS) {
+        const FewTile f = few_tile<R, MB>(p, cum_s, tile, lane);
+        float acc[R][NT][4] = {};
+        for (int b = (warp - first) & (CONSUMERS - 1); b < nkb; b += CONSUMERS) {
             const int it = first + b, st = it % C::STAGES;
             mbar_wait_suspend(bar_full(st), (uint32_t)(it / C::STAGES) & 1u, abort_flag, p.status);
             const uint32_t ws = sbase + st * C::STAGE, as = ws + NB * BLK, sc = sbase + C::OFF_SCALE + st * C::SCALE;
-            uint4 a[2][2];
-            float sa[2][2];
+            uint4 a[NT][2];
+            float sa[NT][2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < NT; ++j) {
                 a[j][0] = lds128(as + 8 * j * BLK + p0);
                 a[j][1] = lds128(as + 8 * j * BLK + p1);
                 sa[j][0] = __int_as_float(lds32(sc + 4u * (uint32_t)(8 * j + 2 * t)));
@@ -202,7 +209,7 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     s1 = __int_as_float(lds32(sc + 4u * (uint32_t)(MB + 16 * r + 8 + g)));
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < NT; ++j) {
                     if (8 * j >= f.rows) break;
                     float d[4] = {};
                     mma_e4m3(d, u0.x, v0.x, u0.y, v0.y, a[j][0].x, a[j][0].y);
@@ -219,9 +226,10 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             if (lane == 0) mbar_arrive(bar_empty(st));
         }
         // partial sums [warp][row of A][row of Bt]; the barrier of the next tile tells that these have been read
-        const uint32_t part = sbase + C::OFF_PART + (uint32_t)(buf * C::PART);
+        if (C::PARTS == 1) asm volatile("bar.sync 1, 256;" ::: "memory");       // the last tile's have been read
+        const uint32_t part = sbase + C::OFF_PART + (uint32_t)((C::PARTS == 1 ? 0 : buf) * C::PART);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < NT; ++j) {
             if (8 * j >= f.rows) break;
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -245,10 +253,10 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
 }
 
-template <int R>
+template <int R, int MB>
 static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaStream_t st)
 {
-    using C = FewCfg<R>;
+    using C = FewCfg<R, MB>;
     CUtensorMap a, b;
     if (!make_byte_map(&a, p.A, p.lda, p.M, p.K, MB) ||
         !make_byte_map(&b, p.Bt, p.ldb, (int)(p.mode == kExpertRows ? (int64_t)p.E * p.N : p.N), p.K, C::NB)) return Q4_ERR_CUDA;
@@ -256,7 +264,7 @@ static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaS
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return Q4_ERR_CUDA;
     if (!ready[dev]) {
-        if (cudaFuncSetAttribute(gemm_f8_few_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
+        if (cudaFuncSetAttribute(gemm_f8_few_kernel<R, MB>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
             return Q4_ERR_CUDA;
         ready[dev] = true;
     }
@@ -265,12 +273,12 @@ static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaS
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
-    cfg.blockDim = dim3((CONSUMERS + PRODUCERS) * 32);
+    cfg.blockDim = dim3((CONSUMERS + C::PRODUCERS) * 32);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_few_kernel<R>, a, b, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_few_kernel<R, MB>, a, b, p);
     count_launch();
     return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
@@ -279,20 +287,27 @@ static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaS
 
 using namespace f8;
 
+// Where it pays (measured, 148 SMs): by experts up to 8 rows per expert on average (64 experts of 2048 x 1024: 512
+// rows 34 against 43 us on the pair kernel, 1024 rows 55 against 43); one product up to 16 rows (4096 x 4096: 6.6
+// against 10.7 us), and up to 32 while its tiles go round the SMs twice at most (4096 x 4096 8.2 against 11.6 us,
+// 16384 x 4096 26 against 22 us): beyond, the warp-level matrix instructions bind.
 bool gemm_f8_few_supported(const GemmF8Params& g)
 {
     if ((uintptr_t)g.A % 16 || (uintptr_t)g.Bt % 16 || g.lda % 16 || g.ldb % 16) return false;
     if ((int64_t)g.N * (g.mode == kExpertRows ? g.E : 1) >= INT32_MAX - 512) return false;
-    return g.mode == kExpertRows ? g.M <= 8 * (int64_t)g.E : g.mode == kDense && g.M <= 16;
+    if (g.mode == kExpertRows) return g.M <= 8 * (int64_t)g.E;
+    return g.mode == kDense && (g.M <= 16 || (g.M <= 32 && ((int64_t)g.N + 31) / 32 <= 4 * f8_pairs_of_device()));
 }
 
 q4_status launch_gemm_f8_few(const GemmF8Params& p, cudaStream_t st)
 {
     const int sms = 2 * f8_pairs_of_device();
-    const int64_t groups = p.mode == kExpertRows ? (p.M + MB - 1) / MB + (p.E < p.M ? p.E : p.M) : (p.M + MB - 1) / MB;
-    // 64 columns per tile where the tiles still go round the SMs a few times; else 32
+    if (p.mode == kDense && p.M > 16) return launch_few<2, 32>(p, ((int64_t)p.N + 31) / 32, sms, st);
+    const int64_t groups = ((int64_t)p.M + 15) / 16 + (p.mode == kExpertRows ? (p.E < p.M ? p.E : p.M) : 0);
+    // 64 columns per tile where the tiles still go round the SMs a few times (half the stages' overhead per
+    // byte: 50 experts 22 against 27 us); else 32
     const int64_t t64 = groups * (((int64_t)p.N + 63) / 64), t32 = groups * (((int64_t)p.N + 31) / 32);
-    return t64 >= 4 * sms ? launch_few<4>(p, t64, sms, st) : launch_few<2>(p, t32, sms, st);
+    return t64 >= 4 * sms ? launch_few<4, 16>(p, t64, sms, st) : launch_few<2, 16>(p, t32, sms, st);
 }
 
 }  // namespace q4

@@ -688,6 +688,36 @@ static q4_status launch_pair(const PairParams& p, const CUtensorMap& a, const CU
     return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
 
+// Clusters of `size` CTAs of the split kernel that run at once on the current device.
+static int clusters_of_device(int size)
+{
+    static int per_dev[64][2] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    int& n = per_dev[dev][size == 8];
+    if (!n) {
+        using Cf = Cfg<1, false>;
+        auto kernel = gemm_f8_pair_kernel<1, false, true>;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)size;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)size);
+        cfg.blockDim = dim3(NTHREADS);
+        cfg.dynamicSmemBytes = Cf::SMEM;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cf::SMEM) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            n = -1;
+        }
+    }
+    return n;
+}
+
 }  // namespace f8
 
 using namespace f8;
@@ -724,9 +754,16 @@ q4_status launch_gemm_f8_pair(const GemmF8Params& g, cudaStream_t st)
     // row tiles: an expert's last one is its own
     const int64_t tm = g.mode == kExpertRows ? p.tiles_m + (g.E < g.M ? g.E : g.M) : p.tiles_m * products;
     const bool wide = g.N > 128 && tm * n256 >= pairs;
+    // Splitting the depth pays for its exchange (about 3.5 us) from 48 blocks, or 32 of the dearer ones with scales
+    // by row (100 x 4096 x 4096: 12.3 us whole, 13.2 in two parts), and only while all clusters run at
+    // once: a cluster lies within a GPC, so 33 of four CTAs and 15 of eight fit where 74 pairs do (2304 x 256 x
+    // 4097, 18 tiles: 16.9 us whole, 14.8 in two parts, 21.2 in four; 512 x 2304 x 2304, 36 tiles: 9.1 whole, 20.6
+    // in two; 1024^3: 5.9 and 9.3).
     int splits = 1;
-    if (!wide && g.mode == kDense)
-        while (splits < 4 && tm * n128 * splits * 2 <= pairs && nkb >= splits * 4) splits *= 2;
+    if (!wide && g.mode == kDense && nkb >= (g.b_rows ? 32 : 48)) {
+        if (tm * n128 <= clusters_of_device(4)) splits = 2;
+        if (tm * n128 <= clusters_of_device(8)) splits = 4;
+    }
     p.splits = splits;
     p.tiles_n = (int)(wide ? n256 : n128);
     const size_t es = type_size(g.c_type);
