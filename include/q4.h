@@ -455,8 +455,9 @@ int64_t   q4_expert_sort_rows(int32_t n, int32_t E, int32_t align);
  * sums in float32 and in the order of j, one rounding.  w [tokens][topk] float32 or NULL (= 1).
  *   q4_expert_gather        Xs[r] = w[source[r]] * X[source[r] / topk], zeros where source[r] < 0
  *   q4_expert_combine       Out[t] = sum_j w[t][j] * Y[slot[t][j]], dropped pairs left out
- *   q4_expert_combine_grad  dY[slot[t][j]] = w[t][j] * dOut[t], zeros in rows with source[r] < 0;
+ *   q4_expert_combine_grad  dY[r] = w[source[r]] * dOut[source[r] / topk], zeros where source[r] < 0;
  *                           dw[t][j] = sum_d dOut[t][d] * Y[slot[t][j]][d], 0 for dropped pairs
+ *                           (slot and source of one sort: source[slot[t][j]] = t * topk + j)
  * `rows` is the number of rows on the experts' side (Xs, Y, dY, source).  The gradient of the
  * unweighted gather is q4_expert_combine with w = NULL.
  */

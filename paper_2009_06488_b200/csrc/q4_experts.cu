@@ -4,7 +4,7 @@
 // Sort: a counting sort of n = tokens * topk expert numbers that keeps pairs of one expert in their
 // order.  Every warp owns a contiguous piece of the pairs; with base[warp][e] = the first row of expert
 // e that is the warp's, it walks its piece 32 pairs at a time, and a pair's row is base + the number of
-// lower lanes with the same expert (match).  The bases are a scan over experts (segments rounded up to
+// lower lanes with the same expert (ballots).  The bases are a scan over experts (segments rounded up to
 // `align`), over the chunks of other thread blocks (counted by a first kernel) and over the warps.  All
 // counts are integers: the result does not depend on any order of execution.
 // Bound: latency (two short kernels; one for up to kOneBlock pairs).
@@ -16,7 +16,8 @@
 namespace q4 {
 namespace experts {
 
-constexpr int NW = 16;                     // warps of a sort block
+constexpr int NW = 32;                     // warps of a sort block
+constexpr int KEEP = 4;                    // ids a lane keeps in registers (a block of kOneBlock pairs)
 constexpr int64_t kOneBlock = 4096;        // pairs per block; up to as many are sorted by one block
 constexpr int kMaxChunks = 128;
 
@@ -59,20 +60,20 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
     const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
     const int64_t piece = ((chunk + NW - 1) / NW + 31) / 32 * 32;
     const int64_t wlo = min(hi, lo + warp * piece), whi = min(hi, wlo + piece);
-    const bool kept = piece <= 8 * 32;     // a lane's ids stay in registers
+    const bool kept = piece <= KEEP * 32;     // a lane's ids stay in registers
 
     if (!hist) asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int i = threadIdx.x; i < (NW + 2) * E; i += blockDim.x) sm[i] = 0;
     __syncthreads();
-    int32_t mine[8];
+    int32_t mine[KEEP];
     if (kept) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < KEEP; ++k) {
             const int64_t i = wlo + k * 32 + lane;
             mine[k] = i < whi ? __ldg(ids + i) : -1;
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < KEEP; ++k)
             if (mine[k] >= 0 && mine[k] < E) atomicAdd(&base[warp * E + mine[k]], 1);
     } else {
 #pragma unroll 8
@@ -88,7 +89,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
         for (int u = threadIdx.x; u < parts * E; u += blockDim.x) {
             const int e = u % E, part = u / E;
             int b = 0, t = 0;
-#pragma unroll 8
+#pragma unroll 16
             for (int c = part; c < G; c += parts) {
                 const int h = hist[(int64_t)c * E + e];
                 t += h;
@@ -143,9 +144,15 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
         source[r] = -1;
     __syncthreads();
 
+    const int bits = 32 - __clz(E - 1);        // of an expert number (0 for E = 1)
     auto place = [&](int64_t i, int e) {
         if (e >= E || e < 0) e = -1;
-        const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
+        // lanes with my expert: one ballot per bit of its number (a match over 32 different numbers costs 32 rounds)
+        unsigned same = __ballot_sync(0xFFFFFFFFu, e >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const unsigned set = __ballot_sync(0xFFFFFFFFu, e >> b & 1);
+            same &= e >> b & 1 ? set : ~set;
+        }
         const int r = e >= 0 ? base[warp * E + e] + __popc(same & ((1u << lane) - 1u)) : -1;
         if (i < whi) {
             slot[i] = r;
@@ -157,7 +164,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
     };
     if (kept) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < KEEP; ++k)
             if (wlo + k * 32 < whi) place(wlo + k * 32 + lane, mine[k]);
     } else {
         for (int64_t i0 = wlo; i0 < whi; i0 += 32) place(i0 + lane, i0 + lane < whi ? __ldg(ids + i0 + lane) : -1);
@@ -195,36 +202,46 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     }
 }
 
-// Rows and weights of pairs j0 .. j0 + 7 of a token; -1 where there is none.
-__device__ __forceinline__ void pairs_of(const ExpertRowsParams& p, int64_t t, bool mine, int j0, int (&s)[8], float (&w)[8])
+// Row and weight of pair j0 + (lane & 7) of a token, -1 where there is none: every eight threads of a token hold
+// its next eight pairs between them.
+struct Pair { int s; float w; };
+__device__ __forceinline__ Pair pair_of(const ExpertRowsParams& p, int64_t t, bool mine, int j0, int lane)
+{
+    const int j = j0 + (lane & 7);
+    Pair q{-1, 1.0f};
+    if (mine && j < p.topk) {
+        q.s = __ldg(p.slot + t * p.topk + j);
+        if (p.w) q.w = __ldg(p.w + t * p.topk + j);
+    }
+    return q;
+}
+__device__ __forceinline__ void spread(const ExpertRowsParams& p, const Pair& q, int lane, int (&s)[8], float (&w)[8])
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const bool in = mine && j0 + j < p.topk;
-        s[j] = in ? __ldg(p.slot + t * p.topk + j0 + j) : -1;
-        w[j] = in && p.w ? __ldg(p.w + t * p.topk + j0 + j) : 1.0f;
+        s[j] = __shfl_sync(0xFFFFFFFFu, q.s, (lane & 24) + j);
+        w[j] = __shfl_sync(0xFFFFFFFFu, q.w, (lane & 24) + j);
+        if (s[j] >= p.rows) s[j] = -1;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) if (s[j] >= p.rows) s[j] = -1;
 }
 
+// 16-bit types: four blocks per SM have 128 KB of rows in flight.
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, VEC && TYPE != Q4_F32 ? 4 : 1)
 combine_kernel(const ExpertRowsParams p, int tx_bits)
 {
     using T = typename f8::Elem<TYPE>::T;
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
     const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
-    if (t >= p.tokens) return;
-    const int c = (blockIdx.y * TX + tx) * 8;
-    if (c >= p.D) return;
-    const int n = min(8, p.D - c);
+    const int c = (blockIdx.y * TX + tx) * 8, lane = threadIdx.x & 31;
+    const bool mine = t < p.tokens;
+    const int n = mine ? max(0, min(8, p.D - c)) : 0;
     float acc[8] = {};
     for (int j0 = 0; j0 < p.topk; j0 += 8) {
         int s[8];
         float w[8];
         Eight<T> v[8];
-        pairs_of(p, t, true, j0, s, w);
+        spread(p, pair_of(p, t, mine, j0, lane), lane, s, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             f8::load8<VEC>(v[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
@@ -234,6 +251,7 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j].get(i), acc[i]);
     }
+    if (n == 0) return;
     Eight<T> o;
     f8::pack8(o, acc);
     f8::store8<VEC>(static_cast<T*>(p.out) + t * p.ldo + c, n, o);
@@ -257,8 +275,11 @@ __device__ __forceinline__ float reduce8(float (&d)[8], int lane)
     return d[0] + __shfl_xor_sync(0xFFFFFFFFu, d[0], 16);
 }
 
+// By tokens: a token's gradient is read once, its rows wherever they lie.  (By rows of the experts' side, read and
+// written front to back with the gradients from L2, 4096 x 8 x 2048 takes 68 us instead of 60: the streams push the
+// gradients out of L2.  Rows that happen to lie in token order take 48: the rest is the scattered writes.)
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256, VEC ? 3 : 1)
+__global__ void __launch_bounds__(256, !VEC ? 1 : TYPE == Q4_F32 ? 2 : 3)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
     using T = typename f8::Elem<TYPE>::T;
@@ -276,50 +297,56 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
         return;
     }
     __shared__ float part[8][8];
-    const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
-    const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
-    const bool mine = t < p.tokens;
-    const T* g = static_cast<const T*>(p.X) + (mine ? t * p.ldx : 0);
-    for (int j0 = 0; j0 < p.topk; j0 += 8) {
-        int s[8];
-        float w[8], dot[8] = {};
-        pairs_of(p, t, mine, j0, s, w);
-        for (int c = tx * 8; mine && c < p.D; c += TX * 8) {
-            const int n = min(8, p.D - c);
-            Eight<T> d, y[8];
-            f8::load8<VEC>(d, g + c, n);
+    const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
+    // a block walks groups of TY tokens; the next group's pairs are loaded before this one's rows
+    int64_t t = (int64_t)blockIdx.x * TY + ty;
+    const int64_t step = (int64_t)token_blocks * TY;
+    Pair ahead = pair_of(p, t, t < p.tokens, 0, lane);
+    for (int64_t group = (int64_t)blockIdx.x * TY; group < p.tokens; group += step, t += step) {
+        const bool mine = t < p.tokens;
+        const T* g = static_cast<const T*>(p.X) + (mine ? t * p.ldx : 0);
+        for (int j0 = 0; j0 < p.topk; j0 += 8) {
+            int s[8];
+            float w[8], dot[8] = {};
+            spread(p, ahead, lane, s, w);
+            ahead = j0 + 8 < p.topk ? pair_of(p, t, mine, j0 + 8, lane) : pair_of(p, t + step, t + step < p.tokens, 0, lane);
+            for (int c = tx * 8; mine && c < p.D; c += TX * 8) {
+                const int n = min(8, p.D - c);
+                Eight<T> d, y[8];
+                f8::load8<VEC>(d, g + c, n);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                f8::load8<VEC>(y[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
+                for (int j = 0; j < 8; ++j)
+                    f8::load8<VEC>(y[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (s[j] < 0) continue;
-                float o[8];
+                for (int j = 0; j < 8; ++j) {
+                    if (s[j] < 0) continue;
+                    float o[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dot[j] = fmaf(d.get(i), y[j].get(i), dot[j]);
-                    o[i] = w[j] * d.get(i);
+                    for (int i = 0; i < 8; ++i) {
+                        dot[j] = fmaf(d.get(i), y[j].get(i), dot[j]);
+                        o[i] = w[j] * d.get(i);
+                    }
+                    Eight<T> e;
+                    f8::pack8(e, o);
+                    f8::store8<VEC>(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, e);
                 }
-                Eight<T> e;
-                f8::pack8(e, o);
-                f8::store8<VEC>(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, e);
             }
-        }
-        if (TX >= 32) {
-            const float sum = reduce8(dot, lane);
-            if (lane < 8) part[warp][lane] = sum;
-            __syncthreads();
-            if (tx < 8) {
-                float all = 0.0f;
-                for (int k = 0; k < TX / 32; ++k) all += part[warp + k][tx];
-                if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = all;
-            }
-            __syncthreads();
-        } else {
+            if (TX >= 32) {
+                const float sum = reduce8(dot, lane);
+                if (lane < 8) part[warp][lane] = sum;
+                __syncthreads();
+                if (tx < 8) {
+                    float all = 0.0f;
+                    for (int k = 0; k < TX / 32; ++k) all += part[warp + k][tx];
+                    if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = all;
+                }
+                __syncthreads();
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                for (int o = TX >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
-                if (tx == 0 && mine && j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
+                for (int j = 0; j < 8; ++j) {
+                    for (int o = TX >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
+                    if (tx == 0 && mine && j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
+                }
             }
         }
     }
@@ -379,6 +406,7 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
         if (err != cudaSuccess) return err;
     }
     cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(NW * 32);
     const cudaError_t err = cudaLaunchKernelEx(&cfg, place_kernel, ids, n, E, align, chunk,
                                                (const int32_t*)(g > 1 ? hist : nullptr), starts, source, rows, slot);
     count_launch();
@@ -406,7 +434,8 @@ cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st)
 cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t st)
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
-    const int tb = (int)(((int64_t)p.tokens + ty - 1) / ty);
+    const int64_t groups = ((int64_t)p.tokens + ty - 1) / ty;
+    const int tb = (int)(groups < 3 * 148 ? groups : 3 * 148);           // resident at once
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
     Q4_ROWS_LAUNCH(combine_grad_kernel, grid, (p, b, tb));
     count_launch();

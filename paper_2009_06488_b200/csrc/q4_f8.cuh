@@ -99,7 +99,7 @@ __device__ __forceinline__ void store8(T* p, int n, const Eight<T>& e)
         if (n > 0) {
 #pragma unroll
             for (int k = 0; k < Eight<T>::NW / 4; ++k)
-                reinterpret_cast<uint4*>(p)[k] = make_uint4(e.w[4 * k], e.w[4 * k + 1], e.w[4 * k + 2], e.w[4 * k + 3]);
+                __stcs(reinterpret_cast<uint4*>(p) + k, make_uint4(e.w[4 * k], e.w[4 * k + 1], e.w[4 * k + 2], e.w[4 * k + 3]));
         }
     } else {
 #pragma unroll

@@ -48,8 +48,13 @@ __device__ __forceinline__ void scale_of(uint32_t a, int pow2, float& s, float& 
         inv = __fdiv_rn(448.0f, m);
         return;
     }
-    if (a <= 0x7F800000u) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
-    inv = __fdiv_rn(1.0f, s);
+    if (a > 0x7F800000u) {                                      // NaN
+        inv = s;
+        return;
+    }
+    const uint32_t up = (__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u;
+    s = __uint_as_float(up);
+    inv = a == 0x7F800000u ? 0.0f : __uint_as_float(0x7F000000u - up);      // exponents of inverses add up to 254
 }
 // two codes, `lo` in the low byte
 __device__ __forceinline__ uint32_t cvt2(float lo, float hi)
@@ -116,17 +121,33 @@ quantize_kernel(const QuantizeParams p)
     }
 
     if (p.Q) {
+        // Maxima of my RT rows over the 16 threads that span them: each step hands half of the rows to the
+        // neighbour, so that thread cx ends with row cx % RT and takes that row's scale alone (a scale costs about
+        // forty instructions; every thread taking all of its rows' was a third of the kernel's).
+        float inv_mine = binv;
+        if (!BLOCKS) {
+            uint32_t a[RT];
+#pragma unroll
+            for (int i = 0; i < RT; ++i) a[i] = max_of(v[i]);
+#pragma unroll
+            for (int w = RT / 2; w; w >>= 1) {
+                const bool up = cx & w;
+#pragma unroll
+                for (int i = 0; i < RT / 2; ++i) {
+                    if (i >= w) break;
+                    const uint32_t give = up ? a[i] : a[i + w], keep = up ? a[i + w] : a[i];
+                    a[i] = max(keep, __shfl_xor_sync(0xFFFFFFFFu, give, w));
+                }
+            }
+#pragma unroll
+            for (int o = RT; o < 16; o <<= 1) a[0] = max(a[0], __shfl_xor_sync(0xFFFFFFFFu, a[0], o));
+            float s;
+            scale_of(a[0], p.pow2, s, inv_mine);
+            if (cx < RT) row_scale[ry * RT + cx] = s;
+        }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            float inv = binv;
-            if (!BLOCKS) {
-                uint32_t a = max_of(v[i]);
-#pragma unroll
-                for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
-                float s;
-                scale_of(a, p.pow2, s, inv);
-                if (cx == 0) row_scale[ry * RT + i] = s;
-            }
+            const float inv = BLOCKS ? binv : __shfl_sync(0xFFFFFFFFu, inv_mine, (lane & 16) + i);
             if (r0 + i < p.rows && nc > 0) {
                 uint32_t q[2];
 #pragma unroll
@@ -203,8 +224,11 @@ quantize_kernel(const QuantizeParams p)
             const int c = u >> 3, h = u & 7;                    // 16 codes of column c, from row 16 h
             const int n = (int)min((int64_t)16, p.rows - (rt0 + 16 * h));
             if (cb * BLK + c >= p.cols || n <= 0) continue;
-            const uint2 lo = *reinterpret_cast<const uint2*>(&tile[c * BLK + (((2 * h) ^ (c >> 3)) << 3)]);
-            const uint2 hi = *reinterpret_cast<const uint2*>(&tile[c * BLK + (((2 * h + 1) ^ (c >> 3)) << 3)]);
+            // pieces 2 h and 2 h + 1 lie together, in either order
+            const uint4 two = *reinterpret_cast<const uint4*>(&tile[c * BLK + ((h ^ (c >> 4)) << 4)]);
+            const bool turned = (c >> 3) & 1;
+            const uint2 lo = turned ? make_uint2(two.z, two.w) : make_uint2(two.x, two.y);
+            const uint2 hi = turned ? make_uint2(two.x, two.y) : make_uint2(two.z, two.w);
             uint8_t* dst = p.Qt + (int64_t)(cb * BLK + c) * p.ldqt + rt0 + 16 * h;
             if (n == 16 && p.qt_vec) {
                 *reinterpret_cast<uint4*>(dst) = make_uint4(lo.x, lo.y, hi.x, hi.y);
@@ -221,9 +245,11 @@ template <int TYPE, bool VEC>
 static void launch_typed(const QuantizeParams& p, bool blocks, cudaStream_t st)
 {
     // column blocks vary fastest: neighbouring tiles read neighbouring pieces of the same rows
-    const unsigned tiles = (unsigned)(blocks_of(p.cols) * (blocks || p.Qt ? blocks_of(p.rows) : (p.rows + 31) / 32));
+    const int64_t t128 = blocks_of(p.cols) * blocks_of(p.rows);
+    const bool large = blocks || p.Qt || t128 >= 4 * 148;
+    const unsigned tiles = (unsigned)(large ? t128 : blocks_of(p.cols) * (((int64_t)p.rows + 31) / 32));
     if (blocks) quantize_kernel<TYPE, 8, true, VEC><<<tiles, 256, 0, st>>>(p);
-    else if (p.Qt) quantize_kernel<TYPE, 8, false, VEC><<<tiles, 256, 0, st>>>(p);
+    else if (large) quantize_kernel<TYPE, 8, false, VEC><<<tiles, 256, 0, st>>>(p);
     else quantize_kernel<TYPE, 2, false, VEC><<<tiles, 256, 0, st>>>(p);
 }
 
