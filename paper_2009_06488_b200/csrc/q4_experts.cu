@@ -2,11 +2,11 @@
 // order, and the weighted sum back to token order with its gradient.
 //
 // Sort: a counting sort of n = tokens * topk expert numbers that keeps pairs of one expert in their
-// order.  Every warp owns a contiguous piece of the pairs; with base[warp][e] = the first row of expert
-// e that is the warp's, it walks its piece 32 pairs at a time, and a pair's row is base + the number of
-// lower lanes with the same expert (ballots).  The bases are a scan over experts (segments rounded up to
-// `align`), over the chunks of other thread blocks (counted by a first kernel) and over the warps.  All
-// counts are integers: the result does not depend on any order of execution.
+// order.  Every warp owns a contiguous piece of the pairs and walks it 32 pairs at a time; a pair's place among its
+// block's pairs is the block's pairs of earlier experts + the expert's pairs of earlier warps and rounds + the
+// number of lower lanes with the same expert (ballots).  Its row adds the expert's first row (segments rounded up
+// to `align`) and the expert's pairs in the chunks of earlier blocks (counted by a first kernel).  Rows are written
+// from the block's order, in runs.  All counts are integers: the result does not depend on any order of execution.
 // Bound: latency (two short kernels; one for up to kOneBlock pairs).
 //
 // Rows: a row's D values are spread over up to 256 threads, 8 (16 bytes of a 16-bit type) each; a token's
@@ -45,6 +45,35 @@ count_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int64_t chun
     for (int e = threadIdx.x; e < E; e += blockDim.x) hist[(int64_t)blockIdx.x * E + e] = cnt[e];
 }
 
+// Inclusive sum over the lanes of a warp.
+__device__ __forceinline__ int scan32(int v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+
+// Shared memory of place_kernel, in ints.  A row of `base` is an expert's counts per warp, one int longer than
+// the warps: lanes over warps as well as lanes over experts touch different banks.
+struct PlaceLayout {
+    int base, total, before, first, local, delta, sums, order, all;
+    __host__ __device__ explicit PlaceLayout(int E)
+    {
+        base = 0;
+        total = E * (NW + 1);
+        before = total + E;
+        first = before + E;            // [E + 1]
+        local = first + E + 1;         // [E] block's pairs before an expert's
+        delta = local + E;             // [E] row of a block's pair minus its place in the block's order
+        sums = delta + E;              // [2][32]
+        order = sums + 64;             // [kOneBlock] the block's pairs in expert order
+        all = order + (int)kOneBlock;
+    }
+};
+
 // Launched while count_kernel runs (programmatic serialization): what needs only the ids comes first.
 __global__ void __launch_bounds__(NW * 32)
 place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t align, int64_t chunk,
@@ -52,19 +81,17 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
              int32_t rows, int32_t* __restrict__ slot)
 {
     extern __shared__ int32_t sm[];
-    int32_t* base = sm;                    // [NW][E]: counts of a warp's piece, then its next row
-    int32_t* total = sm + NW * E;          // [E] pairs of an expert
-    int32_t* before = total + E;           // [E] of them in earlier chunks
-    int32_t* first = before + E;           // [E + 1] first row of an expert
+    const PlaceLayout L(E);
+    int32_t *base = sm + L.base, *total = sm + L.total, *before = sm + L.before, *first = sm + L.first;
+    int32_t *local = sm + L.local, *delta = sm + L.delta, *sums = sm + L.sums, *order = sm + L.order;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
     const int64_t piece = ((chunk + NW - 1) / NW + 31) / 32 * 32;
     const int64_t wlo = min(hi, lo + warp * piece), whi = min(hi, wlo + piece);
-    const bool kept = piece <= KEEP * 32;     // a lane's ids stay in registers
+    const bool kept = piece <= KEEP * 32;  // a lane's ids stay in registers, the block's order in shared memory
 
     if (!hist) asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int i = threadIdx.x; i < (NW + 2) * E; i += blockDim.x) sm[i] = 0;
-    __syncthreads();
+    for (int i = threadIdx.x; i < L.first; i += NW * 32) sm[i] = 0;
     int32_t mine[KEEP];
     if (kept) {
 #pragma unroll
@@ -72,100 +99,127 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
             const int64_t i = wlo + k * 32 + lane;
             mine[k] = i < whi ? __ldg(ids + i) : -1;
         }
+    }
+    __syncthreads();
+    if (kept) {
 #pragma unroll
         for (int k = 0; k < KEEP; ++k)
-            if (mine[k] >= 0 && mine[k] < E) atomicAdd(&base[warp * E + mine[k]], 1);
+            if (mine[k] >= 0 && mine[k] < E) atomicAdd(&base[mine[k] * (NW + 1) + warp], 1);
     } else {
 #pragma unroll 8
         for (int64_t i = wlo + lane; i < whi; i += 32) {
             const int e = __ldg(ids + i);
-            if (e >= 0 && e < E) atomicAdd(&base[warp * E + e], 1);
+            if (e >= 0 && e < E) atomicAdd(&base[e * (NW + 1) + warp], 1);
+        }
+    }
+    __syncthreads();
+    // the block's pairs of an expert before each warp's, and all of them
+    for (int e = warp; e < E; e += NW) {
+        const int c = base[e * (NW + 1) + lane], s = scan32(c, lane);
+        base[e * (NW + 1) + lane] = s - c;
+        if (lane == 31) {
+            local[e] = s;
+            if (!hist) total[e] = s;
         }
     }
     if (hist) {
         asm volatile("griddepcontrol.wait;" ::: "memory");
-        // thread (e, part) sums a part of the chunks: as many parts as the block has threads for
-        const int parts = max(1, (int)blockDim.x / E), G = (int)gridDim.x;
-        for (int u = threadIdx.x; u < parts * E; u += blockDim.x) {
-            const int e = u % E, part = u / E;
-            int b = 0, t = 0;
-#pragma unroll 16
+        // thread (four experts, part) sums a part of the chunks: as many parts as the block has threads for
+        const int G = (int)gridDim.x, quads = E / 4, parts = quads ? max(1, NW * 32 / quads) : 1;
+        const bool vec = E % 4 == 0 && (uintptr_t)hist % 16 == 0;
+        for (int u = threadIdx.x; vec && u < parts * quads; u += NW * 32) {
+            const int part = u / quads, q = u - part * quads;
+            int4 b = make_int4(0, 0, 0, 0), t = b;
+#pragma unroll 4
             for (int c = part; c < G; c += parts) {
-                const int h = hist[(int64_t)c * E + e];
+                const int4 h = *reinterpret_cast<const int4*>(hist + (int64_t)c * E + 4 * q);
+                const bool early = c < (int)blockIdx.x;
+                t.x += h.x; t.y += h.y; t.z += h.z; t.w += h.w;
+                b.x += early ? h.x : 0; b.y += early ? h.y : 0; b.z += early ? h.z : 0; b.w += early ? h.w : 0;
+            }
+            atomicAdd(&total[4 * q], t.x); atomicAdd(&total[4 * q + 1], t.y); atomicAdd(&total[4 * q + 2], t.z); atomicAdd(&total[4 * q + 3], t.w);
+            atomicAdd(&before[4 * q], b.x); atomicAdd(&before[4 * q + 1], b.y); atomicAdd(&before[4 * q + 2], b.z); atomicAdd(&before[4 * q + 3], b.w);
+        }
+        for (int k = threadIdx.x; !vec && k < E; k += NW * 32) {
+            int b = 0, t = 0;
+#pragma unroll 8
+            for (int c = 0; c < G; ++c) {
+                const int h = hist[(int64_t)c * E + k];
                 t += h;
                 b += c < (int)blockIdx.x ? h : 0;
             }
-            atomicAdd(&total[e], t);
-            atomicAdd(&before[e], b);
-        }
-    } else {
-        __syncthreads();
-        for (int e = threadIdx.x; e < E; e += blockDim.x) {
-            int t = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) t += base[w * E + e];
-            total[e] = t;
+            total[k] = t;
+            before[k] = b;
         }
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __syncthreads();
-    if (warp == 0) {
-        int at = 0;
-        for (int e0 = 0; e0 < E; e0 += 32) {
-            const int e = e0 + lane;
-            const int t = e < E ? (total[e] + align - 1) / align * align : 0;
-            int s = t;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(0xFFFFFFFFu, s, o);
-                if (lane >= o) s += u;
-            }
-            if (e < E) first[e] = at + s - t;
-            at += __shfl_sync(0xFFFFFFFFu, s, 31);
-        }
-        if (lane == 0) first[E] = at;
+    // over the experts: warp w scans experts 32 w .., then adds the sums of the warps before it
+    const int e = warp * 32 + lane;
+    const int seg = e < E ? (total[e] + align - 1) / align * align : 0, cnt = e < E ? local[e] : 0;
+    int seg_to = scan32(seg, lane), cnt_to = scan32(cnt, lane);
+    if (lane == 31) {
+        sums[warp] = seg_to;
+        sums[32 + warp] = cnt_to;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x) {
-        int at = first[e] + before[e];
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const int c = base[w * E + e];
-            base[w * E + e] = at;
-            at += c;
-        }
+    const int s0 = sums[lane], s1 = sums[32 + lane];
+    const int t0 = scan32(s0, lane), t1 = scan32(s1, lane);
+    seg_to += __shfl_sync(0xFFFFFFFFu, t0 - s0, warp);
+    cnt_to += __shfl_sync(0xFFFFFFFFu, t1 - s1, warp);
+    const int in_block = __shfl_sync(0xFFFFFFFFu, t1, 31);
+    if (e < E) {
+        first[e] = seg_to - seg;
+        local[e] = cnt_to - cnt;
+        delta[e] = seg_to - seg + before[e] - (cnt_to - cnt);
+        if (e == E - 1) first[E] = seg_to;
     }
+    __syncthreads();
     if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= E; e += blockDim.x) starts[e] = first[e];
+        for (int k = threadIdx.x; k <= E; k += NW * 32) starts[k] = first[k];
     // rows that no pair takes: behind each expert's pairs, and behind the last segment
-    for (int e = (int)blockIdx.x + warp * (int)gridDim.x; e < E; e += NW * (int)gridDim.x)
-        for (int r = first[e] + total[e] + lane; r < first[e + 1]; r += 32) if (r < rows) source[r] = -1;
-    for (int64_t r = (int64_t)first[E] + blockIdx.x * blockDim.x + threadIdx.x; r < rows; r += (int64_t)gridDim.x * blockDim.x)
+    // (a block per expert where there are as many, else a warp)
+    const bool by_block = (int)gridDim.x >= E;
+    const int step = by_block ? NW * 32 : 32, from = by_block ? (int)threadIdx.x : lane;
+    for (int k = (int)blockIdx.x + (by_block ? 0 : warp * (int)gridDim.x); k < E; k += (by_block ? 1 : NW) * (int)gridDim.x)
+        for (int r = first[k] + total[k] + from; r < first[k + 1]; r += step) if (r < rows) source[r] = -1;
+    for (int64_t r = (int64_t)first[E] + blockIdx.x * (NW * 32) + threadIdx.x; r < rows; r += (int64_t)gridDim.x * (NW * 32))
         source[r] = -1;
-    __syncthreads();
 
     const int bits = 32 - __clz(E - 1);        // of an expert number (0 for E = 1)
-    auto place = [&](int64_t i, int e) {
-        if (e >= E || e < 0) e = -1;
+    auto place = [&](int64_t i, int x) {
+        if (x >= E || x < 0) x = -1;
         // lanes with my expert: one ballot per bit of its number (a match over 32 different numbers costs 32 rounds)
-        unsigned same = __ballot_sync(0xFFFFFFFFu, e >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const unsigned set = __ballot_sync(0xFFFFFFFFu, e >> b & 1);
-            same &= e >> b & 1 ? set : ~set;
+        unsigned same = __ballot_sync(0xFFFFFFFFu, x >= 0);
+#pragma unroll
+        for (int b = 0; b < 10; ++b) {
+            if (b >= bits) break;
+            const bool one = x & (1 << b);
+            const unsigned set = __ballot_sync(0xFFFFFFFFu, one);
+            same &= one ? set : ~set;
         }
-        const int r = e >= 0 ? base[warp * E + e] + __popc(same & ((1u << lane) - 1u)) : -1;
-        if (i < whi) {
-            slot[i] = r;
-            if (e >= 0 && r < rows) source[r] = (int32_t)i;
+        int r = -1;
+        if (x >= 0) {
+            const int k = local[x] + base[x * (NW + 1) + warp] + __popc(same & ((1u << lane) - 1u));
+            r = k + delta[x];
+            // the rows of the block's order are runs: written one by one, a warp's 32 would be 32 sectors
+            if (kept) order[k] = x << 16 | (int)(i - lo);
+            else if (r < rows) source[r] = (int32_t)i;
         }
+        if (i < whi) slot[i] = r;
         __syncwarp();
-        if (e >= 0 && (int)(__ffs(same) - 1) == lane) base[warp * E + e] += __popc(same);
+        if (x >= 0 && (int)(__ffs(same) - 1) == lane) base[x * (NW + 1) + warp] += __popc(same);
         __syncwarp();
     };
     if (kept) {
 #pragma unroll
         for (int k = 0; k < KEEP; ++k)
             if (wlo + k * 32 < whi) place(wlo + k * 32 + lane, mine[k]);
+        __syncthreads();
+        for (int k = threadIdx.x; k < in_block; k += NW * 32) {
+            const int v = order[k], r = k + delta[v >> 16];
+            if (r < rows) source[r] = (int32_t)lo + (v & 0xFFFF);
+        }
     } else {
         for (int64_t i0 = wlo; i0 < whi; i0 += 32) place(i0 + lane, i0 + lane < whi ? __ldg(ids + i0 + lane) : -1);
     }
@@ -384,7 +438,7 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
 {
     const int g = chunks_of(n);
     const int64_t chunk = ((int64_t)n + g - 1) / g;
-    const size_t smem = ((size_t)(NW + 3) * E + 1) * 4;
+    const size_t smem = (size_t)PlaceLayout(E).all * 4;
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
