@@ -233,6 +233,7 @@ template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256)
 gather_kernel(const ExpertRowsParams p, int tx_bits)
 {
+    f8::wait_for_predecessor();
     using T = typename f8::Elem<TYPE>::T;
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
     const int64_t r = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
@@ -284,6 +285,7 @@ template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256, VEC && TYPE != Q4_F32 ? 4 : 1)
 combine_kernel(const ExpertRowsParams p, int tx_bits)
 {
+    f8::wait_for_predecessor();
     using T = typename f8::Elem<TYPE>::T;
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
     const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
@@ -336,6 +338,7 @@ template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256, !VEC ? 1 : TYPE == Q4_F32 ? 2 : 3)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
+    f8::wait_for_predecessor();
     using T = typename f8::Elem<TYPE>::T;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if ((int)blockIdx.x >= token_blocks) {
@@ -417,15 +420,11 @@ static int tx_bits_of(int D)
 
 using namespace experts;
 
-#define Q4_ROWS_LAUNCH(kernel, grid, args)                                                          \
-    do {                                                                                            \
-        if (p.type == Q4_F32) p.vec ? kernel<Q4_F32, true><<<grid, 256, 0, st>>> args               \
-                                    : kernel<Q4_F32, false><<<grid, 256, 0, st>>> args;             \
-        else if (p.type == Q4_BF16) p.vec ? kernel<Q4_BF16, true><<<grid, 256, 0, st>>> args        \
-                                          : kernel<Q4_BF16, false><<<grid, 256, 0, st>>> args;      \
-        else p.vec ? kernel<Q4_F16, true><<<grid, 256, 0, st>>> args                                \
-                   : kernel<Q4_F16, false><<<grid, 256, 0, st>>> args;                              \
-    } while (0)
+// The instance of a row kernel for the call's type and alignment.
+#define Q4_ROWS_LAUNCH(kernel, grid, ...)                                                                        \
+    (p.type == Q4_F32    ? f8::launch(p.vec ? kernel<Q4_F32, true> : kernel<Q4_F32, false>, grid, 256, 0, st, __VA_ARGS__)    \
+     : p.type == Q4_BF16 ? f8::launch(p.vec ? kernel<Q4_BF16, true> : kernel<Q4_BF16, false>, grid, 256, 0, st, __VA_ARGS__)  \
+                         : f8::launch(p.vec ? kernel<Q4_F16, true> : kernel<Q4_F16, false>, grid, 256, 0, st, __VA_ARGS__))
 
 size_t expert_sort_ws_bytes(int64_t n, int32_t E)
 {
@@ -444,45 +443,26 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
         if (e != cudaSuccess) return e;
     }
     int32_t* hist = static_cast<int32_t*>(ws);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)g);
-    cfg.blockDim = dim3(512);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
     if (g > 1) {
-        cfg.dynamicSmemBytes = (size_t)E * 4;
-        const cudaError_t err = cudaLaunchKernelEx(&cfg, count_kernel, ids, n, E, chunk, hist);
-        count_launch();
+        const cudaError_t err = f8::launch(count_kernel, (unsigned)g, 512, (size_t)E * 4, st, ids, n, E, chunk, hist);
         if (err != cudaSuccess) return err;
     }
-    cfg.dynamicSmemBytes = smem;
-    cfg.blockDim = dim3(NW * 32);
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, place_kernel, ids, n, E, align, chunk,
-                                               (const int32_t*)(g > 1 ? hist : nullptr), starts, source, rows, slot);
-    count_launch();
-    return err;
+    return f8::launch(place_kernel, (unsigned)g, NW * 32, smem, st, ids, n, E, align, chunk,
+                      (const int32_t*)(g > 1 ? hist : nullptr), starts, source, rows, slot);
 }
 
 cudaError_t launch_expert_gather(const ExpertRowsParams& p, cudaStream_t st)
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const unsigned grid = (unsigned)(((int64_t)p.rows + ty - 1) / ty);
-    Q4_ROWS_LAUNCH(gather_kernel, grid, (p, b));
-    count_launch();
-    return cudaGetLastError();
+    return Q4_ROWS_LAUNCH(gather_kernel, grid, p, b);
 }
 
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, cudaStream_t st)
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const dim3 grid((unsigned)(((int64_t)p.tokens + ty - 1) / ty), (unsigned)((p.D + (8 << b) - 1) / (8 << b)));
-    Q4_ROWS_LAUNCH(combine_kernel, grid, (p, b));
-    count_launch();
-    return cudaGetLastError();
+    return Q4_ROWS_LAUNCH(combine_kernel, grid, p, b);
 }
 
 cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t st)
@@ -491,9 +471,7 @@ cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t s
     const int64_t groups = ((int64_t)p.tokens + ty - 1) / ty;
     const int tb = (int)(groups < 3 * 148 ? groups : 3 * 148);           // resident at once
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
-    Q4_ROWS_LAUNCH(combine_grad_kernel, grid, (p, b, tb));
-    count_launch();
-    return cudaGetLastError();
+    return Q4_ROWS_LAUNCH(combine_grad_kernel, grid, p, b, tb);
 }
 
 }  // namespace q4

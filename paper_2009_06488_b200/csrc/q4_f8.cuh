@@ -107,6 +107,31 @@ __device__ __forceinline__ void store8(T* p, int n, const Eight<T>& e)
     }
 }
 
+// Launch with programmatic stream serialization: the kernel's start overlaps its predecessor's end; it calls
+// wait_for_predecessor() before it touches memory.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A... args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    count_launch();
+    return e;
+}
+__device__ __forceinline__ void wait_for_predecessor()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 inline size_t type_size(int type) { return type == Q4_F32 ? 4 : 2; }
 
 struct QuantizeParams {

@@ -114,8 +114,7 @@ gemm_f8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    wait_for_predecessor();
     int ntiles = (p.M + MB - 1) / MB * ntn;
     if (p.mode == kExpertRows) {
         if (warp == 0) {
@@ -268,18 +267,8 @@ static q4_status launch_few(const GemmF8Params& p, int64_t tiles, int sms, cudaS
             return Q4_ERR_CUDA;
         ready[dev] = true;
     }
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(tiles < sms ? tiles : sms));
-    cfg.blockDim = dim3((CONSUMERS + C::PRODUCERS) * 32);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_few_kernel<R, MB>, a, b, p);
-    count_launch();
+    const cudaError_t e = launch(gemm_f8_few_kernel<R, MB>, (unsigned)(tiles < sms ? tiles : sms), (CONSUMERS + C::PRODUCERS) * 32,
+                                 C::SMEM, st, a, b, p);
     return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
 

@@ -77,6 +77,7 @@ quantize_kernel(const QuantizeParams p)
     __shared__ float row_scale[TR];
     __shared__ __align__(16) uint8_t tile[RT == 8 ? BLK * BLK : 16];
 
+    wait_for_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
     const int ncb = (p.cols + BLK - 1) / BLK;
@@ -242,26 +243,25 @@ quantize_kernel(const QuantizeParams p)
 }
 
 template <int TYPE, bool VEC>
-static void launch_typed(const QuantizeParams& p, bool blocks, cudaStream_t st)
+static cudaError_t launch_typed(const QuantizeParams& p, bool blocks, cudaStream_t st)
 {
     // column blocks vary fastest: neighbouring tiles read neighbouring pieces of the same rows
     const int64_t t128 = blocks_of(p.cols) * blocks_of(p.rows);
     const bool large = blocks || p.Qt || t128 >= 4 * 148;
     const unsigned tiles = (unsigned)(large ? t128 : blocks_of(p.cols) * (((int64_t)p.rows + 31) / 32));
-    if (blocks) quantize_kernel<TYPE, 8, true, VEC><<<tiles, 256, 0, st>>>(p);
-    else if (large) quantize_kernel<TYPE, 8, false, VEC><<<tiles, 256, 0, st>>>(p);
-    else quantize_kernel<TYPE, 2, false, VEC><<<tiles, 256, 0, st>>>(p);
+    if (blocks) return launch(quantize_kernel<TYPE, 8, true, VEC>, tiles, 256, 0, st, p);
+    if (large) return launch(quantize_kernel<TYPE, 8, false, VEC>, tiles, 256, 0, st, p);
+    return launch(quantize_kernel<TYPE, 2, false, VEC>, tiles, 256, 0, st, p);
 }
 
 }  // namespace f8
 
 cudaError_t launch_f8_quantize(const f8::QuantizeParams& p, int x_type, bool blocks, cudaStream_t st)
 {
-    if (x_type == Q4_F32) p.x_vec ? f8::launch_typed<Q4_F32, true>(p, blocks, st) : f8::launch_typed<Q4_F32, false>(p, blocks, st);
-    else if (x_type == Q4_BF16) p.x_vec ? f8::launch_typed<Q4_BF16, true>(p, blocks, st) : f8::launch_typed<Q4_BF16, false>(p, blocks, st);
-    else p.x_vec ? f8::launch_typed<Q4_F16, true>(p, blocks, st) : f8::launch_typed<Q4_F16, false>(p, blocks, st);
-    count_launch();
-    return cudaGetLastError();
+    using namespace f8;
+    if (x_type == Q4_F32) return p.x_vec ? launch_typed<Q4_F32, true>(p, blocks, st) : launch_typed<Q4_F32, false>(p, blocks, st);
+    if (x_type == Q4_BF16) return p.x_vec ? launch_typed<Q4_BF16, true>(p, blocks, st) : launch_typed<Q4_BF16, false>(p, blocks, st);
+    return p.x_vec ? launch_typed<Q4_F16, true>(p, blocks, st) : launch_typed<Q4_F16, false>(p, blocks, st);
 }
 
 }  // namespace q4
