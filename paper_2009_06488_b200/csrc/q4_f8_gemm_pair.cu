@@ -10,6 +10,7 @@
 //   warp 0       TMA producer    per block: the CTA's 128 rows of A and its half of the tile's rows of Bt, 128 bytes
 //                                each, 128-byte swizzle; rows past the end of the segment are not loaded
 //   warps 1, 2   MMA issuers     (leader CTA) four 32-deep steps per block and 128 columns
+//   warp 3       places          of the tiles, found ahead for the accumulators
 //   warps 4..11  accumulators    each thread one row and BN / 2 columns; then scaled sums out through swizzled
 //                                staging slices and TMA stores (whole 32-row groups) or 16-byte stores (ragged ones)
 //
@@ -36,6 +37,7 @@ constexpr int NTHREADS = 12 * 32;
 // Registers: the block is launched with 384 x 168 = 64512; warps 0..3 give back to 56 each, the accumulators
 // take 224 (128 x 56 + 256 x 224 = 64512).
 constexpr int REGS_ISSUE = 56, REGS_ACC = 224;
+constexpr int TI_RING = 3;               // tiles whose places are staged for the accumulators
 constexpr int SLICE = 4096;              // staging slice of an accumulator warp: 32 rows x 128 bytes
 
 template <int HALVES, bool BROWS> struct Cfg {
@@ -46,8 +48,9 @@ template <int HALVES, bool BROWS> struct Cfg {
     static constexpr int STAGES = HALVES == 2 ? (BROWS ? 4 : 5) : 6;
     static constexpr int OFF_SLICE = STAGES * STAGE;
     static constexpr int OFF_SB = OFF_SLICE + 8 * 2 * SLICE;   // [set][buffer][4 blocks][CW] scales of Bt's rows
-    static constexpr int OFF_BAR = OFF_SB + (BROWS ? 2 * 2 * 4 * CW * 4 : 0);
-    static constexpr int NBAR = 2 * STAGES + 8;
+    static constexpr int OFF_TI = OFF_SB + (BROWS ? 2 * 2 * 4 * CW * 4 : 0);    // places of tiles
+    static constexpr int OFF_BAR = OFF_TI + TI_RING * 32;
+    static constexpr int NBAR = 2 * STAGES + 8 + 2 * TI_RING + 2;
     static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
     static constexpr int SMEM = OFF_MISC + 16 + 1024;          // + slack to align the base
     static_assert(STAGE % 1024 == 0 && SMEM <= 232448, "shared memory");
@@ -225,6 +228,9 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     auto bar_empty  = [&](int s) { return bar0 + 8u * (uint32_t)(C::STAGES + s); };
     auto bar_tfull  = [&](int a) { return bar0 + 8u * (uint32_t)(2 * C::STAGES + a); };
     auto bar_tempty = [&](int a) { return bar0 + 8u * (uint32_t)(2 * C::STAGES + 4 + a); };  // used in the leader
+    auto bar_ifull  = [&](uint32_t i) { return bar0 + 8u * (2 * C::STAGES + 8 + i); };           // a tile's place is staged
+    auto bar_iempty = [&](uint32_t i) { return bar0 + 8u * (2 * C::STAGES + 8 + TI_RING + i); };
+    auto bar_set    = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::STAGES + 8 + 2 * TI_RING + i); };   // a set's warps meet (BROWS)
     const uint32_t tmem_slot = sbase + C::OFF_MISC;
     const uint32_t abort_flag = sbase + C::OFF_MISC + 4;
 
@@ -244,6 +250,12 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             mbar_init(bar_tfull(a), 1);
             mbar_init(bar_tempty(a), HALVES == 2 ? 8 : 16);   // accumulator warps of both CTAs that read the slot
         }
+        for (uint32_t i = 0; i < TI_RING; ++i) {
+            mbar_init(bar_ifull(i), 1);
+            mbar_init(bar_iempty(i), 8);     // accumulator warps
+        }
+        mbar_init(bar_set(0), 4);
+        mbar_init(bar_set(1), 4);
         sts32(abort_flag, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
@@ -364,60 +376,81 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         tc_fence_after();
         if (warp == 1)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
-    } else if (warp < 4) {
+    } else if (warp == 3) {
+        // ------------------------------------------------------------ places of tiles, for the accumulators
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
+        Walk<BN> walk(p, lane);
+        uint32_t ti = 0, ph = 0;
+        for (int tile = cluster_id;; tile += nclusters) {
+            const bool more = walk.get(tile, t);
+            if (more) share(t);
+            mbar_wait_suspend(bar_iempty(ti), ph ^ 1u, abort_flag, g.status);
+            const bool last = !more || lds32(abort_flag);
+            if (lane == 0) {
+                const uint32_t at = sbase + C::OFF_TI + ti * 32u;
+                sts128(at, make_uint4((uint32_t)t.m0, (uint32_t)t.m_end, (uint32_t)t.n0, last ? 0xFFFFFFFFu : (uint32_t)t.nkb));
+                sts128(at + 16u, make_uint4((uint32_t)(t.k0 / ROWB), (uint32_t)t.sbrow, (uint32_t)t.crow, (uint32_t)(t.crow >> 32)));
+                mbar_arrive(bar_ifull(ti));
+            }
+            __syncwarp();
+            if (last) break;
+            if (++ti == TI_RING) { ti = 0; ph ^= 1u; }
+        }
+        __syncwarp();
         cluster_sync_all();
         if (SPLIT) cluster_sync_all();
     } else {
         // ------------------------------------------------------------ accumulators
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ACC));
-        Walk<BN> walk(p, lane);
         const int lg = warp & 3, set = warp >= 8 ? 1 : 0;
         const uint32_t tempty_leader = map_to_cta(bar_tempty(0), leader);
         const uint32_t slices = sbase + C::OFF_SLICE + (uint32_t)((warp - 4) * 2 * SLICE);
         const uint32_t sb_s = sbase + C::OFF_SB + (uint32_t)(set * 2 * 4 * CW * 4);
         const int st_id = lg * 32 + lane;                 // thread of the set
-        uint32_t used = 0;
-        // what I need of a tile
-        int c0, rows, nkb, row;                           // first column, valid rows from my warp's first, blocks, my row of A
-        bool live;
-        int64_t crow;                                     // C row of my warp's first
-        const float *sa_at, *sb_at;
-        float sa[4], sb[4];
-        auto enter = [&]() {
-            share(t);
-            const int m0 = t.m0 + (int)rank * TMC + lg * 32;
-            c0 = t.n0 + set * CW;
-            rows = t.m_end - m0;
-            row = m0 + lane;
-            live = rows > 0 && c0 < g.N;
-            nkb = HALVES == 2 && set == 1 && g.N - t.n0 <= 128 ? 0 : t.nkb;     // nothing is multiplied in my half
-            crow = t.crow + (int)rank * TMC + lg * 32;
-            const int64_t kb0 = t.k0 / ROWB;
-            sa_at = g.SA + kb0 * g.ldsa + row;
-            sb_at = g.SB + (BROWS ? kb0 * g.ldsb : (t.sbrow + (HALVES == 2 ? set : 0)) * g.ldsb + kb0);
+        uint32_t used = 0, ti = 0, tph = 0;
+        uint32_t met = 0;
+        auto meet = [&]() {                                // the set's four warps; bounded like every wait
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_set(set));
+            mbar_wait(bar_set(set), met, abort_flag, g.status);
+            met ^= 1u;
         };
+        // the tile whose scales are loaded: this one, or from its last round on the next
+        int f_c0 = 0, f_rows = 0, f_nkb = -1, nkb = -1;  // first column, valid rows from my warp's first, blocks (-1: no tile)
+        const float *sa_at = nullptr, *sb_at = nullptr;
+        float sa[4], sb[4];
         // scales of blocks b0 .. b0 + 3, loaded a round of four blocks ahead
         auto fetch = [&](int b0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool in = b0 + i < nkb;
-                sa[i] = load_ahead(sa_at + (b0 + i) * g.ldsa, in && rows > lane);
+                const bool in = b0 + i < f_nkb;
+                sa[i] = load_ahead(sa_at + (b0 + i) * g.ldsa, in && f_rows > lane);
                 if (!BROWS) {
-                    sb[i] = load_ahead(sb_at + b0 + i, in && c0 < g.N);
+                    sb[i] = load_ahead(sb_at + b0 + i, in && f_c0 < g.N);
                 } else if (i < 4 * CW / 128) {
-                    const int el = i * 128 + st_id, kb = el / CW, n = c0 + el % CW;
-                    sb[i] = load_ahead(sb_at + (b0 + kb) * g.ldsb + n, b0 + kb < nkb && n < g.N);
+                    const int el = i * 128 + st_id, kb = el / CW, n = f_c0 + el % CW;
+                    sb[i] = load_ahead(sb_at + (b0 + kb) * g.ldsb + n, b0 + kb < f_nkb && n < g.N);
                 }
             }
         };
-        int tile = cluster_id;
-        bool more = walk.get(tile, t);
-        if (more) {
-            enter();
+        // the next tile's place and its first scales
+        auto next = [&](uint32_t i, uint32_t ph) {
+            mbar_wait(bar_ifull(i), ph, abort_flag, g.status);
+            const uint4 x = lds128(sbase + C::OFF_TI + i * 32u), y = lds128(sbase + C::OFF_TI + i * 32u + 16u);
+            const int m0 = (int)x.x + (int)rank * TMC + lg * 32;
+            f_nkb = lds32(abort_flag) ? -1 : (int)x.w;
+            if (f_nkb < 0) return;
+            f_c0 = (int)x.z + set * CW;
+            f_rows = (int)x.y - m0;
+            if (HALVES == 2 && set == 1 && g.N - (int)x.z <= 128) f_nkb = 0;     // nothing is multiplied in my half
+            sa_at = g.SA + (int64_t)y.x * g.ldsa + m0 + lane;
+            sb_at = g.SB + (BROWS ? (int64_t)y.x * g.ldsb : ((int64_t)y.y + (HALVES == 2 ? set : 0)) * g.ldsb + y.x);
             fetch(0);
-        }
-        while (more) {
+        };
+        next(0, 0);
+        while ((nkb = f_nkb) >= 0) {
+            const bool live = f_rows > 0 && f_c0 < g.N;
+            const uint32_t ti_next = ti + 1 == TI_RING ? 0 : ti + 1, tph_next = ti + 1 == TI_RING ? tph ^ 1u : tph;
             unsigned long long acc[CW / 2];
 #pragma unroll
             for (int i = 0; i < CW / 2; ++i) acc[i] = 0;
@@ -431,9 +464,10 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     // two buffers: a warp that writes one has passed the barrier behind which all read the other
 #pragma unroll
                     for (int i = 0; i < 4 * CW / 128; ++i) sts32(sb_buf + 4u * (uint32_t)(i * 128 + st_id), __float_as_int(sb[i]));
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory");
+                    meet();
                 }
-                fetch(b0 + 4);
+                if (b0 + 4 < nkb) fetch(b0 + 4);
+                else next(ti_next, tph_next);
                 const int n = min(4, nkb - b0);
 #pragma unroll 1
                 for (int i = 0; i < n; ++i) {
@@ -481,7 +515,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     s[0] = s[1]; s[1] = s[2]; s[2] = s[3];
                 }
             }
-            if (BROWS && nkb > 0) asm volatile("bar.sync %0, 128;" ::"r"(1 + set) : "memory");  // buffers free for the next tile
+            if (BROWS && nkb > 0) meet();                 // buffers free for the next tile
 
             if (SPLIT) {
                 // partial tile [128 rows][BN + 4] over the ring, which nothing reads or fills any more: this pair's
@@ -495,41 +529,40 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     sts128(part + 16u * (uint32_t)i, v);
                 }
             }
-            // the next tile and its first scales, which arrive while this one is stored
-            const int c0_now = c0, rows_now = rows;
-            const int64_t crow_now = crow;
-            const bool store = !SPLIT && live;
-            more = walk.get(tile += nclusters, t);
-            if (more) {
-                enter();
-                fetch(0);
-            }
-            if (store) {
+            if (nkb == 0) next(ti_next, tph_next);
+            const uint4 x = lds128(sbase + C::OFF_TI + ti * 32u), y = lds128(sbase + C::OFF_TI + ti * 32u + 16u);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_iempty(ti));
+            ti = ti_next;
+            tph = tph_next;
+            if (!SPLIT && live) {
+                const int c0 = (int)x.z + set * CW, rows = (int)x.y - ((int)x.x + (int)rank * TMC + lg * 32);
+                const int64_t crow = (int64_t)((uint64_t)y.w << 32 | y.z) + (int)rank * TMC + lg * 32;     // C row of my warp's first
                 const int es = g.c_type == Q4_F32 ? 4 : 2, per = 128 / es;      // columns per slice
                 // slices q0, q0 + 1 to memory
                 auto flush = [&](int q0) {
                     // a store clips rows and columns at the matrix's end, columns in pieces of 16 bytes only
-                    const bool whole = p.c_vec && rows_now >= 32;
+                    const bool whole = p.c_vec && rows >= 32;
                     fence_async_smem();
                     __syncwarp();
 #pragma unroll 1
                     for (int q = q0; q < q0 + 2; ++q) {
                         const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
-                        const int nc = c0_now + q * per;
+                        const int nc = c0 + q * per;
                         if (q >= CW / per || nc >= g.N) break;
                         if (whole && (nc + per <= g.N || g.N * es % 16 == 0)) {
                             if (lane == 0) {
-                                tma_store_2d(&tmC, slice, nc, (int)crow_now);
+                                tma_store_2d(&tmC, slice, nc, (int)crow);
                                 bulk_commit();
                             }
                             continue;
                         }
 #pragma unroll 1
-                        for (int it = 0; it < 8 && it * 4 < rows_now; ++it) {
+                        for (int it = 0; it < 8 && it * 4 < rows; ++it) {
                             const int rr = it * 4 + (lane >> 3), ch = lane & 7, col = nc + ch * (16 / es);
                             const uint4 v = lds128(slice + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)));
-                            if (rr >= rows_now || col >= g.N) continue;
-                            uint8_t* dst = static_cast<uint8_t*>(g.C) + ((crow_now + rr) * g.ldc + col) * es;
+                            if (rr >= rows || col >= g.N) continue;
+                            uint8_t* dst = static_cast<uint8_t*>(g.C) + ((crow + rr) * g.ldc + col) * es;
                             const int have = min(16 / es, g.N - col);
                             if (p.c_vec && have == 16 / es) {
                                 *reinterpret_cast<uint4*>(dst) = v;
@@ -550,7 +583,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 if (g.c_type == Q4_F32) {
 #pragma unroll
                     for (int q0 = 0; q0 < CW / 32; q0 += 2) {
-                        if (c0_now + q0 * 32 < g.N) {
+                        if (c0 + q0 * 32 < g.N) {
                             if (lane == 0) bulk_wait_read();           // earlier stores have read my slices
                             __syncwarp();
 #pragma unroll
@@ -583,7 +616,6 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     flush(0);
                 }
             }
-            if (!BROWS && lds32(abort_flag)) break;      // with BROWS the set's warps stay together (named barrier)
         }
         if (lane == 0) bulk_wait_read();       // my TMA stores have read their slices; their writes complete with the grid
         __syncwarp();
@@ -591,6 +623,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         cluster_sync_all();      // every partial tile is written; my tensor-memory loads are done
         if (SPLIT) {
             // one tile per cluster: CTA `split` of a rank adds its 128 / splits rows of all partial tiles, in order
+            Walk<BN> walk(p, lane);
             if (walk.get(cluster_id, t)) {
                 for (int r = split * TMC / splits + warp - 4; r < (split + 1) * TMC / splits; r += 8) {
                     const int row = t.m0 + (int)rank * TMC + r, col = t.n0 + lane * 4;
