@@ -481,32 +481,28 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                                             (uint32_t)(slot * 128 + (HALVES == 2 ? 0 : set * CW));
                         const uint32_t sbits = __float_as_uint(s[0]);
                         const unsigned long long ss = pack_f2(sbits, sbits);
-                        uint32_t r[2][16];
-                        tc_ld16(ta, r[0]);
-                        tc_wait_ld16(r[0]);
 #pragma unroll
                         for (int c = 0; c < CW / 16; ++c) {
-                            uint32_t (&now)[16] = r[c & 1];
-                            if (c + 1 < CW / 16) {
-                                tc_ld16(ta + (uint32_t)(16 * (c + 1)), r[(c + 1) & 1]);
-                            } else {
+                            uint32_t r[16];
+                            tc_ld16(ta + (uint32_t)(16 * c), r);
+                            tc_wait_ld16(r);
+                            if (c + 1 == CW / 16) {
                                 // my loads of the slot are complete: it may be overwritten
                                 tc_fence_before();
                                 __syncwarp();
                                 if (lane == 0) mbar_arrive_cluster_relaxed(tempty);
                             }
-                            if (BROWS) {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
+                            for (int j = 0; j < 4; ++j) {
+                                if (BROWS) {
                                     const uint4 q = lds128(sb_buf + 4u * (uint32_t)(i * CW + 16 * c + 4 * j));
-                                    fma_f2(acc[8 * c + 2 * j], mul_f2(pack_f2(now[4 * j], now[4 * j + 1]), pack_f2(q.x, q.y)), ss);
-                                    fma_f2(acc[8 * c + 2 * j + 1], mul_f2(pack_f2(now[4 * j + 2], now[4 * j + 3]), pack_f2(q.z, q.w)), ss);
+                                    fma_f2(acc[8 * c + 2 * j], mul_f2(pack_f2(r[4 * j], r[4 * j + 1]), pack_f2(q.x, q.y)), ss);
+                                    fma_f2(acc[8 * c + 2 * j + 1], mul_f2(pack_f2(r[4 * j + 2], r[4 * j + 3]), pack_f2(q.z, q.w)), ss);
+                                } else {
+                                    fma_f2(acc[8 * c + 2 * j], pack_f2(r[4 * j], r[4 * j + 1]), ss);
+                                    fma_f2(acc[8 * c + 2 * j + 1], pack_f2(r[4 * j + 2], r[4 * j + 3]), ss);
                                 }
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) fma_f2(acc[8 * c + j], pack_f2(now[2 * j], now[2 * j + 1]), ss);
                             }
-                            if (c + 1 < CW / 16) tc_wait_ld16(r[(c + 1) & 1]);
                         }
                     } else {
                         __syncwarp();
