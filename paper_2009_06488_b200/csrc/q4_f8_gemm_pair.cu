@@ -536,13 +536,13 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 const int64_t crow = (int64_t)((uint64_t)y.w << 32 | y.z) + (int)rank * TMC + lg * 32;     // C row of my warp's first
                 const int es = g.c_type == Q4_F32 ? 4 : 2, per = 128 / es;      // columns per slice
                 // slices q0, q0 + 1 to memory
-                auto flush = [&](int q0) {
+                auto flush = [&](int q0, int q1) {
                     // a store clips rows and columns at the matrix's end, columns in pieces of 16 bytes only
                     const bool whole = p.c_vec && rows >= 32;
                     fence_async_smem();
                     __syncwarp();
 #pragma unroll 1
-                    for (int q = q0; q < q0 + 2; ++q) {
+                    for (int q = q0; q < q1; ++q) {
                         const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
                         const int nc = c0 + q * per;
                         if (q >= CW / per || nc >= g.N) break;
@@ -577,19 +577,24 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 };
                 const uint32_t mine = slices + (uint32_t)(lane * 128), sw = (uint32_t)(lane & 7);
                 if (g.c_type == Q4_F32) {
+                    // the first two slices together, then one at a time as the older one has been read (a slice
+                    // that goes out without a bulk store is the warp's last, or all of them do)
 #pragma unroll
-                    for (int q0 = 0; q0 < CW / 32; q0 += 2) {
+                    for (int q0 = 0; q0 < CW / 32; q0 += q0 ? 1 : 2) {
                         if (c0 + q0 * 32 < g.N) {
-                            if (lane == 0) bulk_wait_read();           // earlier stores have read my slices
+                            if (lane == 0) {
+                                if (q0) bulk_wait_read_but_one();
+                                else bulk_wait_read();                 // the previous tile's
+                            }
                             __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
+                            for (int j = 0; j < (q0 ? 8 : 16); ++j) {
                                 uint4 v;
                                 unpack_f2(acc[16 * q0 + 2 * j], v.x, v.y);
                                 unpack_f2(acc[16 * q0 + 2 * j + 1], v.z, v.w);
-                                sts128(mine + (uint32_t)((j >> 3) * SLICE) + ((((uint32_t)j & 7u) ^ sw) << 4), v);
+                                sts128(mine + (uint32_t)(((q0 + (j >> 3)) & 1) * SLICE) + ((((uint32_t)j & 7u) ^ sw) << 4), v);
                             }
-                            flush(q0);
+                            flush(q0, q0 ? q0 + 1 : 2);
                         }
                     }
                 } else {
@@ -609,7 +614,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                         sts128(mine + (uint32_t)((j >> 3) * SLICE) + ((((uint32_t)j & 7u) ^ sw) << 4),
                                make_uint4(w[0], w[1], w[2], w[3]));
                     }
-                    flush(0);
+                    flush(0, 2);
                 }
             }
         }
