@@ -67,7 +67,7 @@ __device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d) { r
 
 // VEC: every row of X begins on a multiple of 16 bytes and cols is a multiple of 8.
 template <int TYPE, int RT, bool BLOCKS, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, !VEC || RT == 2 ? 1 : TYPE == Q4_F32 ? 2 : 4)
 quantize_kernel(const QuantizeParams p)
 {
     using T = typename Elem<TYPE>::T;
@@ -86,22 +86,29 @@ quantize_kernel(const QuantizeParams p)
     const int c0 = cb * BLK + cx * 8;
     const int nc = min(8, max(0, p.cols - c0));
 
+    // the tile lies inside: no conditions in the loops (a tenth of the kernel's instructions, and issue binds it)
+    const bool whole = (int64_t)(rb + 1) * TR <= p.rows && (cb + 1) * BLK <= p.cols;
     Eight<T> v[RT];
-    int64_t from[RT];
-    if (p.source) {
-        // a thread of each row fetches its number
-        int s = -1;
-        if (cx < RT && r0 + cx < p.rows) s = __ldg(p.source + r0 + cx);
-        const int64_t r = s >= 0 && s / p.topk < p.x_rows ? s / p.topk : -1;
+    if (whole && !p.source) {
+        const T* src = static_cast<const T*>(p.X) + r0 * p.ldx + c0;
 #pragma unroll
-        for (int i = 0; i < RT; ++i) from[i] = __shfl_sync(0xFFFFFFFFu, r, (lane & 16) + i);
+        for (int i = 0; i < RT; ++i) load8<VEC>(v[i], src + i * p.ldx, 8);
     } else {
+        int64_t from = -1;
+        if (cx < RT && r0 + cx < p.rows) {
+            // a thread of each row finds where it comes from
+            from = r0 + cx;
+            if (p.source) {
+                const int s = __ldg(p.source + from);
+                from = s >= 0 && s / p.topk < p.x_rows ? s / p.topk : -1;
+            }
+        }
 #pragma unroll
-        for (int i = 0; i < RT; ++i) from[i] = r0 + i < p.rows ? r0 + i : -1;
+        for (int i = 0; i < RT; ++i) {
+            const int64_t r = __shfl_sync(0xFFFFFFFFu, from, (lane & 16) + i);
+            load8<VEC>(v[i], static_cast<const T*>(p.X) + (r >= 0 ? r * p.ldx + c0 : 0), r >= 0 ? nc : 0);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-        load8<VEC>(v[i], static_cast<const T*>(p.X) + (from[i] >= 0 ? from[i] * p.ldx + c0 : 0), from[i] >= 0 ? nc : 0);
 
     float binv = 0.0f;
     if (BLOCKS) {
@@ -146,20 +153,26 @@ quantize_kernel(const QuantizeParams p)
             scale_of(a[0], p.pow2, s, inv_mine);
             if (cx < RT) row_scale[ry * RT + cx] = s;
         }
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
+        auto row_codes = [&](int i) {
             const float inv = BLOCKS ? binv : __shfl_sync(0xFFFFFFFFu, inv_mine, (lane & 16) + i);
-            if (r0 + i < p.rows && nc > 0) {
-                uint32_t q[2];
+            return make_uint2(cvt4(v[i].get(0) * inv, v[i].get(1) * inv, v[i].get(2) * inv, v[i].get(3) * inv),
+                              cvt4(v[i].get(4) * inv, v[i].get(5) * inv, v[i].get(6) * inv, v[i].get(7) * inv));
+        };
+        uint8_t* dst = p.Q + r0 * p.ldq + c0;
+        if (whole && p.q_vec) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    q[k] = cvt4(v[i].get(4 * k) * inv, v[i].get(4 * k + 1) * inv, v[i].get(4 * k + 2) * inv, v[i].get(4 * k + 3) * inv);
-                uint8_t* dst = p.Q + (r0 + i) * p.ldq + c0;
+            for (int i = 0; i < RT; ++i, dst += p.ldq) *reinterpret_cast<uint2*>(dst) = row_codes(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < RT; ++i, dst += p.ldq) {
+                const uint2 q = row_codes(i);
+                if (r0 + i >= p.rows) continue;
                 if (nc == 8 && p.q_vec) {
-                    *reinterpret_cast<uint2*>(dst) = make_uint2(q[0], q[1]);
+                    *reinterpret_cast<uint2*>(dst) = q;
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) if (j < nc) dst[j] = (uint8_t)((q[j >> 2] >> (8 * (j & 3))) & 0xFFu);
+                    for (int j = 0; j < 8; ++j)
+                        if (j < nc) dst[j] = (uint8_t)(((j < 4 ? q.x : q.y) >> (8 * (j & 3))) & 0xFFu);
                 }
             }
         }
@@ -218,19 +231,19 @@ quantize_kernel(const QuantizeParams p)
             *reinterpret_cast<uint2*>(&tile[(cx * 8 + j) * BLK + ((ry ^ cx) << 3)]) = make_uint2(q[0], q[1]);
         }
         __syncthreads();
-        const int64_t rt0 = (int64_t)rb * BLK;
+        const int h = threadIdx.x & 7;
+        const int64_t rt0 = (int64_t)rb * BLK + 16 * h;
+        const int n = (int)min((int64_t)16, p.rows - rt0);
+        uint8_t* dst = p.Qt + (int64_t)(cb * BLK + (int)(threadIdx.x >> 3)) * p.ldqt + rt0;
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int u = it * 256 + threadIdx.x;
-            const int c = u >> 3, h = u & 7;                    // 16 codes of column c, from row 16 h
-            const int n = (int)min((int64_t)16, p.rows - (rt0 + 16 * h));
+        for (int it = 0; it < 4; ++it, dst += 32 * p.ldqt) {
+            const int c = it * 32 + (int)(threadIdx.x >> 3);    // 16 codes of column c, from row 16 h
             if (cb * BLK + c >= p.cols || n <= 0) continue;
             // pieces 2 h and 2 h + 1 lie together, in either order
             const uint4 two = *reinterpret_cast<const uint4*>(&tile[c * BLK + ((h ^ (c >> 4)) << 4)]);
             const bool turned = (c >> 3) & 1;
             const uint2 lo = turned ? make_uint2(two.z, two.w) : make_uint2(two.x, two.y);
             const uint2 hi = turned ? make_uint2(two.x, two.y) : make_uint2(two.z, two.w);
-            uint8_t* dst = p.Qt + (int64_t)(cb * BLK + c) * p.ldqt + rt0 + 16 * h;
             if (n == 16 && p.qt_vec) {
                 *reinterpret_cast<uint4*>(dst) = make_uint4(lo.x, lo.y, hi.x, hi.y);
             } else {
