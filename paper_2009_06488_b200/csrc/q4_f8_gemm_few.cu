@@ -11,7 +11,9 @@
 // warps, in order, at the tile's end while the next tiles' stages arrive.
 // The order of depth values inside a block is free as long as both operands share it: lane (g, t) takes
 // 16-byte pieces 2 t and 2 t + 1 of its rows, which the swizzle spreads over all banks.
-// Bound: HBM.  The tensor memory kernel would drain a 128-row accumulator per block for a handful of rows.
+// Bound: HBM; the tensor memory kernel would drain a 128-row accumulator per block for a handful of rows.
+// 64 experts of 2048 x 1024, 16 tokens x 8: 22 us = 5.4 TB/s of weights (pair kernel 34 us); one token through
+// 4096 x 4096: 5.9 us in a graph, of which the weights take 2.6.
 #include <cuda.h>
 
 #include "q4_f8.cuh"

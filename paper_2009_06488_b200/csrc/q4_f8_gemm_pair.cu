@@ -17,6 +17,15 @@
 // Tensor memory holds four slots of 128 columns.  With HALVES = 2 each column half has two of them and its own
 // four accumulating warps, so a half's drain (and the two hand-offs around it) has three quarters of the
 // two blocks' tensor time; one slot of 256 columns per block would leave it half.
+//
+// Bound: the drain.  A block of a wide tile is 512 clk of tensor time; the accumulators need about 750 for it
+// (eight loads of 16 columns, each followed by its multiply-adds, 460 clk for the two warps of a scheduler; the
+// wait, the scales and the release the rest).  What was tried beside it: sixteen accumulating warps of 64 columns
+// (issue slots bind: 4096^3 72 to 78 us), 32-column loads (they slow the products beside them: 87 us), a second
+// buffer (the loads of one warp do not overlap its arithmetic: no change), waiting for the next block before the
+// last multiply-adds (70 us), a warp that multiplies the scales for all (76 us).  In long runs the power cap binds:
+// 8192^3 448 us = 2.46 PFLOP/s in a short region, 524 us = 2.10 PFLOP/s at about 1.4 GHz in a long one.
+//
 // With SPLIT the cluster is 2 * splits CTAs that share one tile's depth; their partial tiles are added in
 // order through distributed shared memory (problems of few tiles).
 #include <cuda.h>
@@ -787,7 +796,13 @@ q4_status launch_gemm_f8_pair(const GemmF8Params& g, cudaStream_t st)
     const int64_t n256 = ((int64_t)g.N + 255) / 256, n128 = ((int64_t)g.N + 127) / 128;
     // row tiles: an expert's last one is its own
     const int64_t tm = g.mode == kExpertRows ? p.tiles_m + (g.E < g.M ? g.E : g.M) : p.tiles_m * products;
-    const bool wide = g.N > 128 && tm * n256 >= pairs;
+    // Tile width: clocks of the busiest pair, from measured ones per block (780 wide, 480 narrow) and tile (2500).
+    // 2048^3 (64 wide tiles, one round; 128 narrow, two) 13.0 against 13.9 us, 1024 x 4096 x 4096 19.4 against 21.8,
+    // 4096^3 64 against 71; 512 x 2304 x 2304 takes narrow tiles, all in one round either way.
+    const int64_t per = g.mode == kExpertDepth ? (nkb + g.E - 1) / g.E : nkb;
+    const int64_t t_wide = (tm * n256 + pairs - 1) / pairs * (per * 780 + 2500);
+    const int64_t t_narrow = (tm * n128 + pairs - 1) / pairs * (per * 480 + 2500);
+    const bool wide = g.N > 128 && t_wide <= t_narrow;
     // Splitting the depth pays for its exchange (about 3.5 us) from 48 blocks, or 32 of the dearer ones with scales
     // by row (100 x 4096 x 4096: 12.3 us whole, 13.2 in two parts), and only while all clusters run at
     // once: a cluster lies within a GPC, so 33 of four CTAs and 15 of eight fit where 74 pairs do (2304 x 256 x
