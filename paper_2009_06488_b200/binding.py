@@ -1,4 +1,4 @@
-"""ctypes binding of the q4 CUDA library: same names as the C ABI in ``include/q4.h``.
+"""Binding of the q4 CUDA library (ctypes, and a C++ module): same names as the C ABI in ``include/q4.h``.
 
 Argument marshalling only -- tensors in, pointers and sizes out.  Every step of the
 path runs in the library's kernels; there is no CPU fallback, and importing this
@@ -25,6 +25,7 @@ if not os.path.exists(LIB_PATH):
         "(python -m paper_2009_06488_b200.build); there is no CPU fallback")
 
 _lib = ctypes.CDLL(LIB_PATH)
+from . import _q4_torch as _t  # noqa: E402  (links to the library just loaded)
 
 (Q4_OK, Q4_ERR_INVALID_ARG, Q4_ERR_ALIGNMENT, Q4_ERR_RANGE, Q4_ERR_WORKSPACE,
  Q4_ERR_UNSUPPORTED, Q4_ERR_CUDA, Q4_ERR_DEVICE_TIMEOUT, Q4_ERR_STATIC_SCRATCH, Q4_ERR_WEIGHT_IMAGE) = range(10)
@@ -441,116 +442,35 @@ def q4_conv2d_channels(X, Wt, d: ConvDesc, za: int, zb, mult, shift, zo: int, cl
     return Y
 
 
-_TYPE = {torch.float32: Q4_F32, torch.bfloat16: Q4_BF16, torch.float16: Q4_F16}
-_CODE = (torch.float8_e4m3fn, torch.uint8)
-
-
-def _gpu(first, *others) -> int:
-    """The CUDA device that all of the tensors (None left out) are on."""
-    d = first.get_device()
-    if d < 0:
-        raise ValueError("CUDA tensors are needed")
-    for t in others:
-        if t is not None and t.get_device() != d:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
-    return d
-
-
-def _need(t, name: str, dtypes, rows: int, cols: int) -> int:
-    """Checks a 2-D tensor of at least rows x cols elements with contiguous rows; its pitch in elements."""
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be one of {tuple(dtypes)}, not {t.dtype}")
-    shape = t.shape
-    if len(shape) != 2 or shape[0] < rows or shape[1] < cols:
-        raise ValueError(f"{name} must be 2-D and at least {rows} x {cols}, not {tuple(shape)}")
-    pitch, step = t.stride()
-    if step != 1 and shape[1] > 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    return pitch if shape[0] > 1 or pitch > shape[1] else shape[1]
-
-
-def _need_flat(t, name: str, dtype, n: int):
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.numel() < n or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and hold at least {n} elements")
-    return t.data_ptr()
-
-
-def _blocks(n: int) -> int:
-    return (n + 127) // 128
-
-
-_raw_stream = torch._C._cuda_getCurrentRawStream      # device -> cudaStream_t, without making a Stream object
-
-
-_F32 = (torch.float32,)
-
+# The calls below are marshalled by _q4_torch (C++): their checks in Python took longer than the smallest kernels.
 
 def q4_f8_quantize(X, Q=None, S=None, Qt=None, St=None, blocks: bool = False, pow2: bool = False, source=None,
                    topk: int = 1):
     """e4m3 codes and scales per 128 columns of a row (or per 128 x 128 block) of X, straight (Q, S)
     and/or transposed (Qt, St); codes are float8_e4m3fn or uint8 tensors.  With ``source`` (int32, one
     entry per output row) row r is made from X's row source[r] // topk; see include/q4.h."""
-    ldx = _need(X, "X", _TYPE, 0, 0)
-    x_rows, cols = X.shape
-    rows = x_rows if source is None else source.numel()
-    if (Q is None) != (S is None) or (Qt is None) != (St is None) or (Q is None and Qt is None):
-        raise ValueError("codes come with their scales: give Q and S, Qt and St, or both pairs")
-    device = _gpu(X, Q, S, Qt, St, source)
-    q = s = qt = st = None
-    ldq = lds = ldqt = ldst = 0
-    if Q is not None:
-        ldq = _need(Q, "Q", _CODE, rows, cols)
-        lds = _need(S, "S", _F32, *((_blocks(rows), _blocks(cols)) if blocks else (_blocks(cols), rows)))
-        q, s = Q.data_ptr(), S.data_ptr()
-    if Qt is not None:
-        ldqt = _need(Qt, "Qt", _CODE, cols, rows)
-        ldst = _need(St, "St", _F32, *((_blocks(cols), _blocks(rows)) if blocks else (_blocks(rows), cols)))
-        qt, st = Qt.data_ptr(), St.data_ptr()
-    src = None if source is None else _need_flat(source, "source", torch.int32, rows)
-    _check(_lib.q4_f8_quantize(X.data_ptr(), _TYPE[X.dtype], ldx, rows, cols, src, topk, x_rows,
-                               (Q4_F8_BLOCKS if blocks else 0) | (Q4_F8_POW2 if pow2 else 0),
-                               q, ldq, s, lds, qt, ldqt, st, ldst, _raw_stream(device)), "q4_f8_quantize")
+    _check(_t.f8_quantize(X, Q, S, Qt, St, source, topk, (Q4_F8_BLOCKS if blocks else 0) | (Q4_F8_POW2 if pow2 else 0)),
+           "q4_f8_quantize")
 
 
 def q4_gemm_f8(A, SA, Bt, SB, C, M: int, N: int, K: int, b_rows: bool = False):
     """C = A Bt^T of e4m3 codes with their scales: SA [ceil(K/128), M]; SB [ceil(N/128), ceil(K/128)], or
     [ceil(K/128), N] with b_rows; C float32, bfloat16 or float16.  See include/q4.h."""
-    device = _gpu(A, SA, Bt, SB, C)
-    kb = _blocks(K)
-    lda, ldb, ldc = _need(A, "A", _CODE, M, K), _need(Bt, "Bt", _CODE, N, K), _need(C, "C", _TYPE, M, N)
-    ldsa = _need(SA, "SA", _F32, kb, M)
-    ldsb = _need(SB, "SB", _F32, kb, N) if b_rows else _need(SB, "SB", _F32, _blocks(N), kb)
-    _check(_lib.q4_gemm_f8(A.data_ptr(), lda, SA.data_ptr(), ldsa, Bt.data_ptr(), ldb, SB.data_ptr(), ldsb,
-                           Q4_F8_B_ROWS if b_rows else 0, C.data_ptr(), _TYPE[C.dtype], ldc, M, N, K,
-                           _raw_stream(device)), "q4_gemm_f8")
+    _check(_t.gemm_f8(A, SA, Bt, SB, C, M, N, K, Q4_F8_B_ROWS if b_rows else 0), "q4_gemm_f8")
     return C
 
 
 def q4_gemm_f8_experts(A, SA, Bt, SB, starts, C, M: int, N: int, K: int):
     """Rows starts[e] .. starts[e + 1] of A times expert e's weights (rows e * N .. of Bt, scales in rows
     e * ceil(N/128) .. of SB); rows of C outside every segment stay untouched.  See include/q4.h."""
-    device = _gpu(A, SA, Bt, SB, starts, C)
-    E, kb = starts.numel() - 1, _blocks(K)
-    lda, ldb, ldc = _need(A, "A", _CODE, M, K), _need(Bt, "Bt", _CODE, E * N, K), _need(C, "C", _TYPE, M, N)
-    ldsa, ldsb = _need(SA, "SA", _F32, kb, M), _need(SB, "SB", _F32, E * _blocks(N), kb)
-    _check(_lib.q4_gemm_f8_experts(A.data_ptr(), lda, SA.data_ptr(), ldsa, Bt.data_ptr(), ldb, SB.data_ptr(), ldsb,
-                                   _need_flat(starts, "starts", torch.int32, 1), E, C.data_ptr(), _TYPE[C.dtype], ldc,
-                                   M, N, K, _raw_stream(device)), "q4_gemm_f8_experts")
+    _check(_t.gemm_f8_experts(A, SA, Bt, SB, starts, C, M, N, K, 0), "q4_gemm_f8_experts")
     return C
 
 
 def q4_gemm_f8_experts_wgrad(A, SA, Bt, SB, starts, C, M: int, N: int, K: int):
     """Rows e * M .. of C = A[:, seg e] Bt[:, seg e]^T over depth segments that begin on multiples of 128;
     SA [ceil(K/128), M], SB [ceil(K/128), N].  See include/q4.h."""
-    device = _gpu(A, SA, Bt, SB, starts, C)
-    E, kb = starts.numel() - 1, _blocks(K)
-    lda, ldb, ldc = _need(A, "A", _CODE, M, K), _need(Bt, "Bt", _CODE, N, K), _need(C, "C", _TYPE, E * M, N)
-    ldsa, ldsb = _need(SA, "SA", _F32, kb, M), _need(SB, "SB", _F32, kb, N)
-    _check(_lib.q4_gemm_f8_experts_wgrad(A.data_ptr(), lda, SA.data_ptr(), ldsa, Bt.data_ptr(), ldb, SB.data_ptr(), ldsb,
-                                         _need_flat(starts, "starts", torch.int32, 1), E, C.data_ptr(), _TYPE[C.dtype],
-                                         ldc, M, N, K, _raw_stream(device)), "q4_gemm_f8_experts_wgrad")
+    _check(_t.gemm_f8_experts(A, SA, Bt, SB, starts, C, M, N, K, 1), "q4_gemm_f8_experts_wgrad")
     return C
 
 
@@ -564,65 +484,25 @@ def q4_expert_sort_rows(n: int, E: int, align: int) -> int:
 
 def q4_expert_sort(ids, E: int, align: int, starts, source, slot, ws=None):
     """Stable sort of expert numbers: starts [E + 1], source [rows], slot (as ids); all int32.  See include/q4.h."""
-    device = _gpu(ids, starts, source, slot, ws)
-    n = ids.numel()
-    if ws is not None and not ws.is_contiguous():
-        raise ValueError("ws must be contiguous")
-    _check(_lib.q4_expert_sort(_need_flat(ids, "ids", torch.int32, n), n, E, align,
-                               _need_flat(starts, "starts", torch.int32, E + 1),
-                               _need_flat(source, "source", torch.int32, 0), source.numel(),
-                               _need_flat(slot, "slot", torch.int32, n),
-                               None if ws is None else ws.data_ptr(),
-                               0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(device)), "q4_expert_sort")
-
-
-def _pairs(w, tokens: int, topk: int):
-    return None if w is None else _need_flat(w, "w", torch.float32, tokens * topk)
-
-
-def _one_type(first, *others):
-    for t in others:
-        if t.dtype != first.dtype or t.shape[1] != first.shape[1]:
-            raise ValueError("rows of one type and width are needed")
+    _check(_t.expert_sort(ids, E, align, starts, source, slot, ws), "q4_expert_sort")
 
 
 def q4_expert_gather(X, source, topk: int, Xs, w=None):
     """Xs[r] = w[source[r]] * X[source[r] // topk], zeros where source[r] < 0; see include/q4.h."""
-    device = _gpu(X, source, Xs, w)
-    (tokens, D), rows = X.shape, source.numel()
-    ldx, ldxs = _need(X, "X", _TYPE, 0, 0), _need(Xs, "Xs", _TYPE, rows, D)
-    _one_type(X, Xs)
-    _check(_lib.q4_expert_gather(X.data_ptr(), ldx, _TYPE[X.dtype], D, tokens, topk,
-                                 _need_flat(source, "source", torch.int32, rows), rows, _pairs(w, tokens, topk),
-                                 Xs.data_ptr(), ldxs, _raw_stream(device)), "q4_expert_gather")
+    _check(_t.expert_gather(X, source, topk, Xs, w), "q4_expert_gather")
     return Xs
 
 
 def q4_expert_combine(Y, slot, w, Out):
     """Out[t] = sum_j w[t, j] * Y[slot[t, j]] (w None: ones); slot int32 [tokens, topk]; see include/q4.h."""
-    device = _gpu(Y, slot, w, Out)
-    (tokens, topk), (rows, D) = slot.shape, Y.shape
-    ldy, ldo = _need(Y, "Y", _TYPE, 0, 0), _need(Out, "Out", _TYPE, tokens, D)
-    _one_type(Y, Out)
-    _check(_lib.q4_expert_combine(Y.data_ptr(), ldy, _TYPE[Y.dtype], D, rows,
-                                  _need_flat(slot, "slot", torch.int32, 0), _pairs(w, tokens, topk), tokens, topk,
-                                  Out.data_ptr(), ldo, _raw_stream(device)), "q4_expert_combine")
+    _check(_t.expert_combine(Y, slot, w, Out), "q4_expert_combine")
     return Out
 
 
 def q4_expert_combine_grad(dOut, Y, slot, w, source, dY, dw):
     """Gradient of q4_expert_combine: dY[slot[t, j]] = w[t, j] * dOut[t] (zeros in rows of no pair) and
     dw[t, j] = <dOut[t], Y[slot[t, j]]>; see include/q4.h."""
-    device = _gpu(dOut, Y, slot, w, source, dY, dw)
-    (tokens, topk), (rows, D) = slot.shape, Y.shape
-    ldd, ldy = _need(dOut, "dOut", _TYPE, tokens, D), _need(Y, "Y", _TYPE, 0, 0)
-    lddy = _need(dY, "dY", _TYPE, rows, D)
-    _one_type(Y, dOut, dY)
-    _check(_lib.q4_expert_combine_grad(dOut.data_ptr(), ldd, Y.data_ptr(), ldy, _TYPE[Y.dtype], D, rows,
-                                       _need_flat(source, "source", torch.int32, rows),
-                                       _need_flat(slot, "slot", torch.int32, 0), _pairs(w, tokens, topk), tokens, topk,
-                                       dY.data_ptr(), lddy, _need_flat(dw, "dw", torch.float32, tokens * topk),
-                                       _raw_stream(device)), "q4_expert_combine_grad")
+    _check(_t.expert_combine_grad(dOut, Y, slot, w, source, dY, dw), "q4_expert_combine_grad")
 
 
 def q4_row_sums(P, rows: int, K: int, sums):

@@ -1,4 +1,5 @@
-"""Builds the CUDA library (csrc/*.cu -> libq4.so next to this file) for sm_100a.
+"""Builds the CUDA library (csrc/*.cu -> libq4.so next to this file) for sm_100a, and the module that
+hands torch tensors to it (csrc/q4_torch.cpp -> _q4_torch.so).
 
 nvcc cross-compiles without a GPU.  The library links the CUDA runtime statically
 and obtains the one driver entry point it needs at run time, so it loads on a
@@ -14,6 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libq4.so")
+TORCH_SRC = os.path.join(CSRC, "q4_torch.cpp")
+TORCH_LIB = os.path.join(HERE, "_q4_torch.so")      # tensors to the C ABI; links to libq4.so beside it
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-cudart", "static"]
@@ -59,7 +62,27 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *objs])
         os.replace(tmp, LIB)
+    if force or not os.path.exists(TORCH_LIB) or \
+            os.path.getmtime(TORCH_LIB) < max(os.path.getmtime(TORCH_SRC), os.path.getmtime(os.path.join(INCLUDE, "q4.h"))):
+        build_torch()
     return LIB
+
+
+def build_torch() -> None:
+    """The marshalling module (host code only: g++ with torch's headers)."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = TORCH_LIB + f".tmp{os.getpid()}"
+    subprocess.check_call(
+        ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-I", INCLUDE, "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
+         "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+         "-isystem", os.environ.get("CUDA_HOME", "/usr/local/cuda") + "/include", "-o", tmp, TORCH_SRC,
+         "-L", HERE, "-l:libq4.so", "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+         "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, TORCH_LIB)
 
 
 if __name__ == "__main__":

@@ -731,23 +731,23 @@ static q4_status launch_pair(const PairParams& p, const CUtensorMap& a, const CU
     return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
 
-// Clusters of `size` CTAs of the split kernel that run at once on the current device.
-static int clusters_of_device(int size)
+// Clusters of `splits` pairs of the split kernel that run at once on the current device (splits 2..4).
+static int clusters_of_device(int splits)
 {
-    static int per_dev[64][2] = {};
+    static int per_dev[64][5] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    int& n = per_dev[dev][size == 8];
+    int& n = per_dev[dev][splits];
     if (!n) {
         using Cf = Cfg<1, false>;
         auto kernel = gemm_f8_pair_kernel<1, false, true>;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)size;
+        attr[0].val.clusterDim.x = (unsigned)(2 * splits);
         attr[0].val.clusterDim.y = 1;
         attr[0].val.clusterDim.z = 1;
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)size);
+        cfg.gridDim = dim3((unsigned)(2 * splits));
         cfg.blockDim = dim3(NTHREADS);
         cfg.dynamicSmemBytes = Cf::SMEM;
         cfg.attrs = attr;
@@ -804,15 +804,14 @@ q4_status launch_gemm_f8_pair(const GemmF8Params& g, cudaStream_t st)
     const int64_t t_narrow = (tm * n128 + pairs - 1) / pairs * (per * 480 + 2500);
     const bool wide = g.N > 128 && t_wide <= t_narrow;
     // Splitting the depth pays for its exchange (about 3.5 us) from 48 blocks, or 32 of the dearer ones with scales
-    // by row (100 x 4096 x 4096: 12.3 us whole, 13.2 in two parts), and only while all clusters run at
-    // once: a cluster lies within a GPC, so 33 of four CTAs and 15 of eight fit where 74 pairs do (2304 x 256 x
-    // 4097, 18 tiles: 16.9 us whole, 14.8 in two parts, 21.2 in four; 512 x 2304 x 2304, 36 tiles: 9.1 whole, 20.6
-    // in two; 1024^3: 5.9 and 9.3).
+    // by row (100 x 4096 x 4096: 12.3 us whole, 13.2 in two parts), and only while all clusters run at once: a
+    // cluster lies within a GPC, so 33 of four CTAs, 22 of six and 15 of eight fit where 74 pairs do (2304 x 256 x
+    // 4097, 18 tiles: 16.9 us whole, 14.8 in two parts, 13.4 in three, 21.2 in four; 512 x 2304 x 2304, 36 tiles:
+    // 9.1 whole, 20.6 in two).
     int splits = 1;
-    if (!wide && g.mode == kDense && nkb >= (g.b_rows ? 32 : 48)) {
-        if (tm * n128 <= clusters_of_device(4)) splits = 2;
-        if (tm * n128 <= clusters_of_device(8)) splits = 4;
-    }
+    if (!wide && g.mode == kDense && nkb >= (g.b_rows ? 32 : 48))
+        for (int k = 2; k <= 4; ++k)
+            if (tm * n128 <= clusters_of_device(k)) splits = k;
     p.splits = splits;
     p.tiles_n = (int)(wide ? n256 : n128);
     const size_t es = type_size(g.c_type);

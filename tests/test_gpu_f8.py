@@ -177,6 +177,23 @@ def test_product_matches_the_oracle(q4, M, N, K, b_rows, out):
     assert q4.q4_last_device_status() == q4.Q4_OK
 
 
+@pytest.mark.parametrize("M,N,K", [(130, 200, 6150), (300, 1000, 6300), (520, 1200, 6200), (40, 300, 8200), (700, 1200, 6200)])
+@pytest.mark.parametrize("b_rows", [False, True])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_long_products_of_few_tiles(q4, M, N, K, b_rows, out):
+    """Few tiles and a long depth, which may be shared by several CTA pairs (2, 16, 30, 3 and 30 tiles)."""
+    import torch
+    (a, sa), (b, sb) = operands(M + K, M, K, False), operands(N + K + 1, N, K, not b_rows)
+    want, mag = f8.product(a, sa, b, sb, b_rows)
+    A, B, SA, SB = placed(a, up16(K)), placed(b, up16(K) + 32), placed(sa), placed(sb)
+    for pad in (8, 3):
+        C = torch.full((M + 1, N + pad), 7.0, dtype=types()[out], device="cuda")
+        q4.q4_gemm_f8(A, SA, B, SB, C, M, N, K, b_rows=b_rows)
+        check(C[:M, :N], want, mag, K, out)
+        assert (C[M:] == 7).all() and (C[:, N:] == 7).all()
+    assert q4.q4_last_device_status() == q4.Q4_OK
+
+
 @pytest.mark.parametrize("off,pitch", [(3, 0), (0, 5)])
 @pytest.mark.parametrize("M,N,K", [(1, 70, 300), (130, 70, 300)])
 def test_product_of_unaligned_operands(q4, M, N, K, off, pitch):
