@@ -237,23 +237,27 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     using T = typename f8::Elem<TYPE>::T;
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1);
     const int64_t r = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
-    if (r >= p.rows) return;
-    const int pair = p.source[r], t = pair / p.topk;
+    const bool mine = r < p.rows;
+    if (VEC && !mine) return;
+    const int pair = mine ? p.source[r] : -1, t = pair / p.topk;
     const bool on = pair >= 0 && t < p.tokens;
     const float w = on && p.w ? p.w[pair] : 1.0f;
     const T* src = static_cast<const T*>(p.X) + (on ? t * p.ldx : 0);
-    T* dst = static_cast<T*>(p.out) + r * p.ldo;
-    for (int c = tx * 8; c < p.D; c += TX * 8) {
-        const int n = min(8, p.D - c);
-        Eight<T> v;
-        f8::load8<VEC>(v, src + c, on ? n : 0);
+    T* dst = static_cast<T*>(p.out) + (mine ? r * p.ldo : 0);
+    const f8::Span in = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D);
+    const bool first = f8::first_of(tx), last = f8::last_of(tx, TX);
+    for (int c0 = 0; c0 < p.D; c0 += TX * 8) {             // whole warps
+        const int c = c0 + tx * 8, left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
+        f8::Coming<VEC, T> x;
+        x.load(src + c, on ? n : 0, in);
+        Eight<T> v = x.get(on ? n : 0);
         if (p.w) {
             float f[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = v.get(i) * w;
             f8::pack8(v, f);
         }
-        f8::store8<VEC>(dst + c, n, v);
+        f8::store8<VEC>(dst + c, left, v, first, last);
     }
 }
 
@@ -282,7 +286,7 @@ __device__ __forceinline__ void spread(const ExpertRowsParams& p, const Pair& q,
 
 // 16-bit types: four blocks per SM have 128 KB of rows in flight.
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256, VEC && TYPE != Q4_F32 ? 4 : 1)
+__global__ void __launch_bounds__(256, VEC && TYPE == Q4_F32 ? 1 : 4)
 combine_kernel(const ExpertRowsParams p, int tx_bits)
 {
     f8::wait_for_predecessor();
@@ -291,26 +295,32 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const int64_t t = (int64_t)blockIdx.x * (256 >> tx_bits) + (threadIdx.x >> tx_bits);
     const int c = (blockIdx.y * TX + tx) * 8, lane = threadIdx.x & 31;
     const bool mine = t < p.tokens;
-    const int n = mine ? max(0, min(8, p.D - c)) : 0;
+    const int left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
+    const f8::Span in = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
+    constexpr int JN = VEC ? 8 : 2;                  // rows in flight
     float acc[8] = {};
     for (int j0 = 0; j0 < p.topk; j0 += 8) {
         int s[8];
         float w[8];
-        Eight<T> v[8];
         spread(p, pair_of(p, t, mine, j0, lane), lane, s, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            f8::load8<VEC>(v[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
+        for (int h = 0; h < 8; h += JN) {
+            f8::Coming<VEC, T> v[JN];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (s[j] >= 0)                          // a dropped pair's weight may be anything
+            for (int j = h; j < h + JN; ++j)
+                v[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, in);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], v[j].get(i), acc[i]);
+            for (int j = h; j < h + JN; ++j) {
+                if (s[j] < 0) continue;             // a dropped pair's weight may be anything
+                const Eight<T> y = v[j - h].get(n);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], y.get(i), acc[i]);
+            }
+        }
     }
-    if (n == 0) return;
     Eight<T> o;
     f8::pack8(o, acc);
-    f8::store8<VEC>(static_cast<T*>(p.out) + t * p.ldo + c, n, o);
+    f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || mine ? t * p.ldo + c : 0), left, o, f8::first_of(tx), f8::last_of(tx, TX));
 }
 
 // Sums of eight values over the 32 lanes of a warp; lane l < 8 returns the sum of value l.  Each step
@@ -335,7 +345,7 @@ __device__ __forceinline__ float reduce8(float (&d)[8], int lane)
 // written front to back with the gradients from L2, 4096 x 8 x 2048 takes 68 us instead of 60: the streams push the
 // gradients out of L2.  Rows that happen to lie in token order take 48: the rest is the scattered writes.)
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256, !VEC ? 1 : TYPE == Q4_F32 ? 2 : 3)
+__global__ void __launch_bounds__(256, VEC && TYPE != Q4_F32 ? 3 : 2)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
     f8::wait_for_predecessor();
@@ -349,13 +359,19 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
         zero.zero();
         for (unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0); none; none &= none - 1) {
             T* dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
-            for (int c = lane * 8; c < p.D; c += 256) f8::store8<VEC>(dst + c, min(8, p.D - c), zero);
+            for (int c0 = 0; c0 < p.D; c0 += 256) {
+                const int c = c0 + lane * 8;
+                f8::store8<VEC>(dst + c, p.D - c, zero, lane == 0, lane == 31);
+            }
         }
         return;
     }
+    constexpr int JN = VEC ? 8 : 4;                  // rows in flight
     __shared__ float part[8][8];
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
     // a block walks groups of TY tokens; the next group's pairs are loaded before this one's rows
+    const f8::Span gs = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D), ys = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
+    const bool first = f8::first_of(tx), last = f8::last_of(tx, TX);
     int64_t t = (int64_t)blockIdx.x * TY + ty;
     const int64_t step = (int64_t)token_blocks * TY;
     Pair ahead = pair_of(p, t, t < p.tokens, 0, lane);
@@ -367,25 +383,33 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
             float w[8], dot[8] = {};
             spread(p, ahead, lane, s, w);
             ahead = j0 + 8 < p.topk ? pair_of(p, t, mine, j0 + 8, lane) : pair_of(p, t + step, t + step < p.tokens, 0, lane);
-            for (int c = tx * 8; mine && c < p.D; c += TX * 8) {
-                const int n = min(8, p.D - c);
-                Eight<T> d, y[8];
-                f8::load8<VEC>(d, g + c, n);
+            // (rows of any alignment: whole warps go on together)
+            for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
+                const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
+                f8::Coming<VEC, T> dc;
+                dc.load(g + c, n, gs);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    f8::load8<VEC>(y[j], static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0);
+                for (int h = 0; h < 8; h += JN) {
+                    f8::Coming<VEC, T> yc[JN];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (s[j] < 0) continue;
-                    float o[8];
+                    for (int j = h; j < h + JN; ++j)
+                        yc[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, ys);
+                    const Eight<T> d = dc.get(n);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dot[j] = fmaf(d.get(i), y[j].get(i), dot[j]);
-                        o[i] = w[j] * d.get(i);
+                    for (int j = h; j < h + JN; ++j) {
+                        if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
+                        const Eight<T> y = yc[j - h].get(n);
+                        float o[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            dot[j] = fmaf(d.get(i), y.get(i), dot[j]);
+                            o[i] = w[j] * d.get(i);
+                        }
+                        Eight<T> e;
+                        f8::pack8(e, o);
+                        f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e,
+                                        first, last);
                     }
-                    Eight<T> e;
-                    f8::pack8(e, o);
-                    f8::store8<VEC>(static_cast<T*>(p.out) + s[j] * p.ldo + c, n, e);
                 }
             }
             if (TX >= 32) {

@@ -71,12 +71,48 @@ template <typename H> __device__ __forceinline__ void pack8(Eight<H>& e, const f
     for (int i = 0; i < 4; ++i) e.w[i] = pack2(v[2 * i], v[2 * i + 1], (const H*)nullptr);
 }
 
-// VEC: all eight exist (n = 8, or 0 for none) at an address that is a multiple of 16 bytes; else `n` of
-// them (0..8) are read one by one.  What does not exist reads 0.  The data is streamed: read once.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(Eight<T>& e, const T* p, int n)
+// Bytes off .. off + 15 of the 32 bytes a, b (0 <= off < 16).
+__device__ __forceinline__ uint4 cut16(const uint4& a, const uint4& b, int off)
 {
-    if constexpr (VEC) {
+    const bool two = off & 8, one = off & 4;
+    const uint32_t s0 = two ? a.z : a.x, s1 = two ? a.w : a.y, s2 = two ? b.x : a.z, s3 = two ? b.y : a.w, s4 = two ? b.z : b.x,
+                   s5 = two ? b.w : b.y;
+    const uint32_t t0 = one ? s1 : s0, t1 = one ? s2 : s1, t2 = one ? s3 : s2, t3 = one ? s4 : s3, t4 = one ? s5 : s4;
+    const unsigned sh = 8u * ((unsigned)off & 3u);
+    return make_uint4(__funnelshift_r(t0, t1, sh), __funnelshift_r(t1, t2, sh), __funnelshift_r(t2, t3, sh), __funnelshift_r(t3, t4, sh));
+}
+
+// Rows that need not begin on multiples of 16 bytes are read in the aligned pieces that hold their values, and
+// cut afterwards.  A piece may hold bytes of a row's neighbours, never bytes outside the matrix's first and last value:
+// such a piece is read value by value.
+struct Span { uintptr_t lo, hi; };
+template <typename T> __device__ __forceinline__ Span span_of(const void* base, int64_t rows, int64_t ld, int cols)
+{
+    return {(uintptr_t)base, (uintptr_t)base + (uintptr_t)(rows > 0 ? ((rows - 1) * ld + cols) * (int64_t)sizeof(T) : 0)};
+}
+template <typename T> __device__ __noinline__ uint4 piece_by_values(uintptr_t at, uintptr_t lo, uintptr_t hi)
+{
+    unsigned long long w[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+        for (int i = 0; i < 8; i += (int)sizeof(T)) {
+            const uintptr_t v = at + 8 * h + i;
+            if (v < lo || v >= hi) continue;
+            if (sizeof(T) == 4) w[h] |= (unsigned long long)*reinterpret_cast<const uint32_t*>(v) << (8 * i);
+            else w[h] |= (unsigned long long)*reinterpret_cast<const uint16_t*>(v) << (8 * i);
+        }
+    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+}
+
+// Eight values on their way.  VEC: all eight exist (n = 8, or 0 for none) at an address that is a multiple of 16
+// bytes; else n of them (0..8) anywhere.  What does not exist reads 0.
+template <bool VEC, typename T> struct Coming;
+template <typename T> struct Coming<true, T> {
+    Eight<T> e;
+    // The data is streamed: read once.
+    __device__ __forceinline__ void load(const T* p, int n, const Span&)
+    {
         e.zero();
         if (n > 0) {
 #pragma unroll
@@ -85,25 +121,90 @@ __device__ __forceinline__ void load8(Eight<T>& e, const T* p, int n)
                              : "=r"(e.w[4 * k]), "=r"(e.w[4 * k + 1]), "=r"(e.w[4 * k + 2]), "=r"(e.w[4 * k + 3])
                              : "l"(reinterpret_cast<const uint4*>(p) + k));
         }
-    } else {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
-        pack8(e, v);                               // exact: the values are of the type
     }
-}
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* p, int n, const Eight<T>& e)
-{
-    if constexpr (VEC) {
-        if (n > 0) {
+    __device__ __forceinline__ const Eight<T>& get(int) const { return e; }
+};
+template <typename T> struct Coming<false, T> {
+    static constexpr int G = Eight<T>::NW / 4 + 1;
+    uint4 g[G];
+    int off;
+    __device__ __forceinline__ void load(const T* p, int n, const Span& in)
+    {
+        off = (int)((uintptr_t)p & 15);
+        const uintptr_t first = (uintptr_t)p - off;
 #pragma unroll
-            for (int k = 0; k < Eight<T>::NW / 4; ++k)
+        for (int k = 0; k < G; ++k) {
+            const uintptr_t at = first + 16 * k;
+            const bool need = n > 0 && 16 * k < off + n * (int)sizeof(T), inside = at >= in.lo && at + 16 <= in.hi;
+            asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                         "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                         "@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                         : "=&r"(g[k].x), "=&r"(g[k].y), "=&r"(g[k].z), "=&r"(g[k].w) : "l"(at), "r"((int)(need && inside)));
+            if (need && !inside) g[k] = piece_by_values<T>(at, in.lo, in.hi);
+        }
+    }
+    __device__ __forceinline__ Eight<T> get(int n) const
+    {
+        Eight<T> e;
+#pragma unroll
+        for (int k = 0; k + 1 < G; ++k) {
+            const uint4 c = cut16(g[k], g[k + 1], off);
+            e.w[4 * k] = c.x;
+            e.w[4 * k + 1] = c.y;
+            e.w[4 * k + 2] = c.z;
+            e.w[4 * k + 3] = c.w;
+        }
+        if (n < 8) {
+#pragma unroll
+            for (int k = 0; k < Eight<T>::NW; ++k) {
+                if (sizeof(T) == 4) e.w[k] = k < n ? e.w[k] : 0;
+                else e.w[k] = 2 * k + 1 < n ? e.w[k] : 2 * k < n ? e.w[k] & 0xFFFFu : 0;
+            }
+        }
+        return e;
+    }
+};
+
+// Place tx of the TX threads that share a row, TX a power of two: whether the warp's lane before / behind holds its neighbours.
+__device__ __forceinline__ bool first_of(int tx) { return (tx & 31) == 0; }
+__device__ __forceinline__ bool last_of(int tx, int TX) { return ((tx + 1) & (min(TX, 32) - 1)) == 0; }
+
+// The first `left` (any number; at most 8) of a lane's eight values to p.  VEC as above.  Else: called by whole warps; lane + 1
+// holds the row's next eight unless `last` (of the row's lanes, or of the warp), lane - 1 the eight before unless `first`.
+// Aligned pieces of 16 bytes are put together with the lane before; what is left at the ends is written by values.
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, int left, const Eight<T>& e, bool first, bool last)
+{
+    constexpr int NW = Eight<T>::NW, ES = (int)sizeof(T);
+    if constexpr (VEC) {
+        if (left > 0) {
+#pragma unroll
+            for (int k = 0; k < NW / 4; ++k)
                 __stcs(reinterpret_cast<uint4*>(p) + k, make_uint4(e.w[4 * k], e.w[4 * k + 1], e.w[4 * k + 2], e.w[4 * k + 3]));
         }
     } else {
+        const int off = (int)((uintptr_t)p & 15);
+        uint4 s[NW / 4 + 1];
+        s[0] = make_uint4(__shfl_up_sync(0xFFFFFFFFu, e.w[NW - 4], 1), __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 3], 1),
+                          __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 2], 1), __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 1], 1));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = from_f<T>(e.get(i));
+        for (int k = 0; k < NW / 4; ++k) s[k + 1] = make_uint4(e.w[4 * k], e.w[4 * k + 1], e.w[4 * k + 2], e.w[4 * k + 3]);
+        unsigned done = 0;                         // pieces that are written whole, the last one by the next lane
+#pragma unroll
+        for (int k = 0; k < NW / 4; ++k) {
+            if (min(left, 8) * ES < 16 * (k + 1) - off || (k == 0 && off && first)) continue;
+            done |= 1u << k;
+            const uint4 v = off ? cut16(s[k], s[k + 1], 16 - off) : s[k + 1];
+            __stcs(reinterpret_cast<uint4*>((uintptr_t)p - off) + k, v);
+        }
+        if (!last && min(left - 8, 8) * ES >= 16 - off) done |= 1u << (NW / 4);
+        if (done == (2u << (NW / 4)) - 1u || (off == 0 && done == (1u << (NW / 4)) - 1u)) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i >= left || (done >> ((off + i * ES) >> 4) & 1u)) continue;
+            if (ES == 4) reinterpret_cast<uint32_t*>(p)[i] = e.w[i % NW];
+            else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(e.w[i >> 1] >> (16 * (i & 1)));
+        }
     }
 }
 

@@ -106,6 +106,12 @@ __device__ __forceinline__ unsigned long long mul_f2(unsigned long long a, unsig
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
     return v;
 }
+__device__ __forceinline__ uint32_t lds16(uint32_t a)
+{
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint4 lds128_cluster(uint32_t a)
 {
     uint4 v;
@@ -544,45 +550,53 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 const int c0 = (int)x.z + set * CW, rows = (int)x.y - ((int)x.x + (int)rank * TMC + lg * 32);
                 const int64_t crow = (int64_t)((uint64_t)y.w << 32 | y.z) + (int)rank * TMC + lg * 32;     // C row of my warp's first
                 const int es = g.c_type == Q4_F32 ? 4 : 2, per = 128 / es;      // columns per slice
-                // slices q0, q0 + 1 to memory
+                // slices q0 .. q1 - 1 to memory
                 auto flush = [&](int q0, int q1) {
-                    // a store clips rows and columns at the matrix's end, columns in pieces of 16 bytes only
-                    const bool whole = p.c_vec && rows >= 32;
                     fence_async_smem();
                     __syncwarp();
-#pragma unroll 1
-                    for (int q = q0; q < q1; ++q) {
-                        const uint32_t slice = slices + (uint32_t)((q & 1) * SLICE);
+                    int q = q0;
+                    q1 = min(q1, CW / per);
+                    // a store clips rows and columns at the matrix's end, columns in pieces of 16 bytes only
+                    for (; p.c_vec && rows >= 32 && q < q1; ++q) {
                         const int nc = c0 + q * per;
-                        if (q >= CW / per || nc >= g.N) break;
-                        if (whole && (nc + per <= g.N || g.N * es % 16 == 0)) {
-                            if (lane == 0) {
-                                tma_store_2d(&tmC, slice, nc, (int)crow);
-                                bulk_commit();
-                            }
-                            continue;
+                        if (nc >= g.N || (nc + per > g.N && g.N * es % 16 != 0)) break;
+                        if (lane == 0) {
+                            tma_store_2d(&tmC, slices + (uint32_t)((q & 1) * SLICE), nc, (int)crow);
+                            bulk_commit();
                         }
-#pragma unroll 1
-                        for (int it = 0; it < 8 && it * 4 < rows; ++it) {
-                            const int rr = it * 4 + (lane >> 3), ch = lane & 7, col = nc + ch * (16 / es);
-                            const uint4 v = lds128(slice + (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4)));
-                            if (rr >= rows || col >= g.N) continue;
-                            uint8_t* dst = static_cast<uint8_t*>(g.C) + ((crow + rr) * g.ldc + col) * es;
-                            const int have = min(16 / es, g.N - col);
-                            if (p.c_vec && have == 16 / es) {
-                                *reinterpret_cast<uint4*>(dst) = v;
-                            } else {
-                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    if (j >= have) break;
-                                    if (es == 4) { if (j < 4) reinterpret_cast<uint32_t*>(dst)[j] = w[j & 3]; }
-                                    else reinterpret_cast<uint16_t*>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-                                }
-                            }
-                        }
-                        __syncwarp();
                     }
+                    const int nc = c0 + q * per, bytes = min((q1 - q) * 128, (g.N - nc) * es);
+                    if (bytes <= 0) return;
+                    // the rest in aligned pieces of 16 bytes, each cut from two of the slices', ...
+                    uint8_t* const dst = static_cast<uint8_t*>(g.C) + (crow * g.ldc + nc) * es;
+                    const int64_t pitch = g.ldc * es;
+                    const int lg_pieces = q1 - q > 1 ? 4 : 3, n = min(rows, 32);
+                    auto piece = [&](int r, int c) {
+                        return slices + (uint32_t)(((q + (c >> 3)) & 1) * SLICE + r * 128) + (uint32_t)(((c ^ r) & 7) << 4);
+                    };
+#pragma unroll 4
+                    for (int i = lane; i < n << lg_pieces; i += 32) {
+                        const int r = i >> lg_pieces, c = i & ((1 << lg_pieces) - 1);
+                        uint8_t* const at = dst + r * pitch;
+                        const int head = (int)(-(intptr_t)at & 15), off = head + 16 * c;
+                        if (off + 16 > bytes) continue;
+                        uint4 v = lds128(piece(r, c));
+                        if (head) v = f8::cut16(v, lds128(piece(r, c + 1)), head);
+                        *reinterpret_cast<uint4*>(at + off) = v;
+                    }
+                    // ... and what is left at either end by values, a row's by eight lanes
+#pragma unroll 2
+                    for (int r = lane >> 3; r < n; r += 4) {
+                        uint8_t* const at = dst + r * pitch;
+                        const int head = min((int)(-(intptr_t)at & 15), bytes), tail = (bytes - head) & 15;
+                        for (int k = (lane & 7) * es; k < head + tail; k += 8 * es) {
+                            const int off = k < head ? k : bytes - tail + k - head;
+                            const uint32_t from = piece(r, off >> 4) + (uint32_t)(off & 15);
+                            if (es == 4) *reinterpret_cast<int*>(at + off) = lds32(from);
+                            else *reinterpret_cast<uint16_t*>(at + off) = (uint16_t)lds16(from);
+                        }
+                    }
+                    __syncwarp();
                 };
                 const uint32_t mine = slices + (uint32_t)(lane * 128), sw = (uint32_t)(lane & 7);
                 if (g.c_type == Q4_F32) {

@@ -71,7 +71,7 @@ __device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d) { r
 
 // VEC: every row of X begins on a multiple of 16 bytes and cols is a multiple of 8.
 template <int TYPE, int RT, bool BLOCKS, bool VEC>
-__global__ void __launch_bounds__(256, !VEC || RT == 2 ? 1 : TYPE == Q4_F32 ? 2 : 4)
+__global__ void __launch_bounds__(256, RT == 2 ? 1 : !VEC || TYPE == Q4_F32 ? 2 : 4)
 quantize_kernel(const QuantizeParams p)
 {
     using T = typename Elem<TYPE>::T;
@@ -92,11 +92,15 @@ quantize_kernel(const QuantizeParams p)
 
     // the tile lies inside: no conditions in the loops (a tenth of the kernel's instructions, and issue binds it)
     const bool whole = (int64_t)(rb + 1) * TR <= p.rows && (cb + 1) * BLK <= p.cols;
+    Coming<VEC, T> x[RT];
     Eight<T> v[RT];
+    const Span in = span_of<T>(p.X, p.x_rows, p.ldx, p.cols);
     if (whole && !p.source) {
         const T* src = static_cast<const T*>(p.X) + r0 * p.ldx + c0;
 #pragma unroll
-        for (int i = 0; i < RT; ++i) load8<VEC>(v[i], src + i * p.ldx, 8);
+        for (int i = 0; i < RT; ++i) x[i].load(src + i * p.ldx, 8, in);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) v[i] = x[i].get(8);
     } else {
         int64_t from = -1;
         if (cx < RT && r0 + cx < p.rows) {
@@ -110,8 +114,10 @@ quantize_kernel(const QuantizeParams p)
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int64_t r = __shfl_sync(0xFFFFFFFFu, from, (lane & 16) + i);
-            load8<VEC>(v[i], static_cast<const T*>(p.X) + (r >= 0 ? r * p.ldx + c0 : 0), r >= 0 ? nc : 0);
+            x[i].load(static_cast<const T*>(p.X) + (r >= 0 ? r * p.ldx + c0 : 0), r >= 0 ? nc : 0, in);
         }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) v[i] = x[i].get(nc);
     }
 
     float binv = 0.0f;
