@@ -245,11 +245,10 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     const T* src = static_cast<const T*>(p.X) + (on ? t * p.ldx : 0);
     T* dst = static_cast<T*>(p.out) + (mine ? r * p.ldo : 0);
     const f8::Span in = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D);
-    const bool first = f8::first_of(tx), last = f8::last_of(tx, TX);
     for (int c0 = 0; c0 < p.D; c0 += TX * 8) {             // whole warps
         const int c = c0 + tx * 8, left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
         f8::Coming<VEC, T> x;
-        x.load(src + c, on ? n : 0, in);
+        x.load(src + c, on ? n : 0, c >= 8 && left >= 16, in);
         Eight<T> v = x.get(on ? n : 0);
         if (p.w) {
             float f[8];
@@ -257,7 +256,7 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
             for (int i = 0; i < 8; ++i) f[i] = v.get(i) * w;
             f8::pack8(v, f);
         }
-        f8::store8<VEC>(dst + c, left, v, first, last);
+        f8::store8<VEC>(dst + c, left, v, tx, TX);
     }
 }
 
@@ -297,6 +296,7 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const bool mine = t < p.tokens;
     const int left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
     const f8::Span in = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
+    const bool inner = c >= 8 && left >= 16;
     constexpr int JN = VEC ? 8 : 2;                  // rows in flight
     float acc[8] = {};
     for (int j0 = 0; j0 < p.topk; j0 += 8) {
@@ -308,7 +308,7 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
             f8::Coming<VEC, T> v[JN];
 #pragma unroll
             for (int j = h; j < h + JN; ++j)
-                v[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, in);
+                v[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, in);
 #pragma unroll
             for (int j = h; j < h + JN; ++j) {
                 if (s[j] < 0) continue;             // a dropped pair's weight may be anything
@@ -320,7 +320,7 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     }
     Eight<T> o;
     f8::pack8(o, acc);
-    f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || mine ? t * p.ldo + c : 0), left, o, f8::first_of(tx), f8::last_of(tx, TX));
+    f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || mine ? t * p.ldo + c : 0), left, o, tx, TX);
 }
 
 // Sums of eight values over the 32 lanes of a warp; lane l < 8 returns the sum of value l.  Each step
@@ -361,7 +361,7 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
             T* dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
             for (int c0 = 0; c0 < p.D; c0 += 256) {
                 const int c = c0 + lane * 8;
-                f8::store8<VEC>(dst + c, p.D - c, zero, lane == 0, lane == 31);
+                f8::store8<VEC>(dst + c, p.D - c, zero, lane, 32);
             }
         }
         return;
@@ -371,7 +371,6 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
     // a block walks groups of TY tokens; the next group's pairs are loaded before this one's rows
     const f8::Span gs = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D), ys = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
-    const bool first = f8::first_of(tx), last = f8::last_of(tx, TX);
     int64_t t = (int64_t)blockIdx.x * TY + ty;
     const int64_t step = (int64_t)token_blocks * TY;
     Pair ahead = pair_of(p, t, t < p.tokens, 0, lane);
@@ -386,14 +385,15 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
             // (rows of any alignment: whole warps go on together)
             for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
                 const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
+                const bool inner = c >= 8 && left >= 16;
                 f8::Coming<VEC, T> dc;
-                dc.load(g + c, n, gs);
+                dc.load(g + c, n, inner, gs);
 #pragma unroll
                 for (int h = 0; h < 8; h += JN) {
                     f8::Coming<VEC, T> yc[JN];
 #pragma unroll
                     for (int j = h; j < h + JN; ++j)
-                        yc[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, ys);
+                        yc[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, ys);
                     const Eight<T> d = dc.get(n);
 #pragma unroll
                     for (int j = h; j < h + JN; ++j) {
@@ -408,7 +408,7 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
                         Eight<T> e;
                         f8::pack8(e, o);
                         f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e,
-                                        first, last);
+                                        tx, TX);
                     }
                 }
             }

@@ -111,7 +111,7 @@ template <bool VEC, typename T> struct Coming;
 template <typename T> struct Coming<true, T> {
     Eight<T> e;
     // The data is streamed: read once.
-    __device__ __forceinline__ void load(const T* p, int n, const Span&)
+    __device__ __forceinline__ void load(const T* p, int n, bool, const Span&)
     {
         e.zero();
         if (n > 0) {
@@ -128,18 +128,26 @@ template <typename T> struct Coming<false, T> {
     static constexpr int G = Eight<T>::NW / 4 + 1;
     uint4 g[G];
     int off;
-    __device__ __forceinline__ void load(const T* p, int n, const Span& in)
+    // `inner`: the row has eight values more on either side, so that no piece needs a check.
+    __device__ __forceinline__ void load(const T* p, int n, bool inner, const Span& in)
     {
         off = (int)((uintptr_t)p & 15);
-        const uintptr_t first = (uintptr_t)p - off;
+        const uintptr_t at0 = (uintptr_t)p - off;
+#pragma unroll
+        for (int k = 0; k < G; ++k) g[k] = make_uint4(0, 0, 0, 0);
+        if (inner) {
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+                asm volatile("{\n\t.reg .pred q;\n\tsetp.gt.s32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                             : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at0 + 16 * k), "r"(n));
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < G; ++k) {
-            const uintptr_t at = first + 16 * k;
+            const uintptr_t at = at0 + 16 * k;
             const bool need = n > 0 && 16 * k < off + n * (int)sizeof(T), inside = at >= in.lo && at + 16 <= in.hi;
-            asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-                         "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
-                         "@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-                         : "=&r"(g[k].x), "=&r"(g[k].y), "=&r"(g[k].z), "=&r"(g[k].w) : "l"(at), "r"((int)(need && inside)));
+            asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                         : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at), "r"((int)(need && inside)));
             if (need && !inside) g[k] = piece_by_values<T>(at, in.lo, in.hi);
         }
     }
@@ -165,15 +173,11 @@ template <typename T> struct Coming<false, T> {
     }
 };
 
-// Place tx of the TX threads that share a row, TX a power of two: whether the warp's lane before / behind holds its neighbours.
-__device__ __forceinline__ bool first_of(int tx) { return (tx & 31) == 0; }
-__device__ __forceinline__ bool last_of(int tx, int TX) { return ((tx + 1) & (min(TX, 32) - 1)) == 0; }
-
-// The first `left` (any number; at most 8) of a lane's eight values to p.  VEC as above.  Else: called by whole warps; lane + 1
-// holds the row's next eight unless `last` (of the row's lanes, or of the warp), lane - 1 the eight before unless `first`.
+// The first `left` (any number; at most 8) of a lane's eight values to p.  VEC as above.  Else: called by whole warps; the
+// lane is place tx of the TX (a power of two) that share a row, each with the eight values behind the lane before.
 // Aligned pieces of 16 bytes are put together with the lane before; what is left at the ends is written by values.
 template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* p, int left, const Eight<T>& e, bool first, bool last)
+__device__ __forceinline__ void store8(T* p, int left, const Eight<T>& e, int tx, int TX)
 {
     constexpr int NW = Eight<T>::NW, ES = (int)sizeof(T);
     if constexpr (VEC) {
@@ -184,6 +188,7 @@ __device__ __forceinline__ void store8(T* p, int left, const Eight<T>& e, bool f
         }
     } else {
         const int off = (int)((uintptr_t)p & 15);
+        const bool first = (tx & 31) == 0, last = ((tx + 1) & (min(TX, 32) - 1)) == 0;    // of the warp's part of the row
         uint4 s[NW / 4 + 1];
         s[0] = make_uint4(__shfl_up_sync(0xFFFFFFFFu, e.w[NW - 4], 1), __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 3], 1),
                           __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 2], 1), __shfl_up_sync(0xFFFFFFFFu, e.w[NW - 1], 1));
@@ -196,6 +201,16 @@ __device__ __forceinline__ void store8(T* p, int left, const Eight<T>& e, bool f
             done |= 1u << k;
             const uint4 v = off ? cut16(s[k], s[k + 1], 16 - off) : s[k + 1];
             __stcs(reinterpret_cast<uint4*>((uintptr_t)p - off) + k, v);
+        }
+        if (ES == 2 && TX >= 32 && left - 8 * (31 - (tx & 31)) >= 16) {
+            // one row, which goes on behind the warp: the 16 bytes at its ends by eight lanes
+            if (off == 0) return;
+            const int lane = tx & 31, k = lane & 7, from = 2 * k < 16 - off ? 0 : 31;
+            const uint32_t w0 = __shfl_sync(0xFFFFFFFFu, e.w[0], from), w1 = __shfl_sync(0xFFFFFFFFu, e.w[1], from),
+                           w2 = __shfl_sync(0xFFFFFFFFu, e.w[2], from), w3 = __shfl_sync(0xFFFFFFFFu, e.w[3], from);
+            const uint32_t w = k & 4 ? (k & 2 ? w3 : w2) : (k & 2 ? w1 : w0);
+            if (lane < 8) reinterpret_cast<uint16_t*>(p)[8 * (from - lane) + k] = (uint16_t)(w >> (16 * (k & 1)));
+            return;
         }
         if (!last && min(left - 8, 8) * ES >= 16 - off) done |= 1u << (NW / 4);
         if (done == (2u << (NW / 4)) - 1u || (off == 0 && done == (1u << (NW / 4)) - 1u)) return;
