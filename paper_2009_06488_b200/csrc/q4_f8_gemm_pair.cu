@@ -106,18 +106,17 @@ __device__ __forceinline__ unsigned long long mul_f2(unsigned long long a, unsig
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
     return v;
 }
-__device__ __forceinline__ uint32_t lds16(uint32_t a)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint4 lds128_cluster(uint32_t a)
 {
     uint4 v;
     asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
 
 // A load that stays where it is written (the compiler would move a plain one down to its use, a round of four
@@ -275,6 +274,12 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
+    if (warp == 0 && elect_one()) {
+        prefetch_map(&tmA);
+        prefetch_map(&tmAfew);
+        prefetch_map(&tmB);
+        if (p.c_vec) prefetch_map(&tmC);
+    }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(tmem_slot), "r"(512u) : "memory");
@@ -284,8 +289,9 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     cluster_sync_all();              // barriers of all CTAs are initialised past this point
     tc_fence_after();
     const uint32_t tmem_base = (uint32_t)lds32(tmem_slot);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // Before a warp's first access to global memory.  What does not need any comes before it: it overlaps the end of the
+    // kernel before, the places of a dense product's first tile with it.
+    const bool dense = g.mode == kDense;
 
     // the share of a tile's depth blocks that this pair sums
     auto share = [&](Tile& t) {
@@ -299,12 +305,14 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     Tile t;
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
-        Walk<BN> walk(p, lane);
         // ------------------------------------------------------------ TMA producer
+        if (!dense) wait_for_predecessor();
+        Walk<BN> walk(p, lane);
         const uint32_t full_leader = map_to_cta(bar_full(0), leader);
         uint32_t st = 0, ph = 0;
         Tile next;
         bool more = walk.get(cluster_id, next);
+        if (dense) wait_for_predecessor();
         for (int tile = cluster_id; more;) {
             t = next;
             share(t);
@@ -343,6 +351,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
         if (rank == 0) {
             const int who = warp - 1;
+            if (!dense) wait_for_predecessor();
             Walk<BN> walk(p, lane);
             const uint16_t both = (uint16_t)(3u << leader);
             const uint64_t desc0 = make_kmajor_sw128_desc(sbase);
@@ -394,6 +403,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     } else if (warp == 3) {
         // ------------------------------------------------------------ places of tiles, for the accumulators
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
+        if (!dense) wait_for_predecessor();
         Walk<BN> walk(p, lane);
         uint32_t ti = 0, ph = 0;
         for (int tile = cluster_id;; tile += nclusters) {
@@ -417,6 +427,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     } else {
         // ------------------------------------------------------------ accumulators
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ACC));
+        wait_for_predecessor();
         const int lg = warp & 3, set = warp >= 8 ? 1 : 0;
         const uint32_t tempty_leader = map_to_cta(bar_tempty(0), leader);
         const uint32_t slices = sbase + C::OFF_SLICE + (uint32_t)((warp - 4) * 2 * SLICE);
@@ -574,26 +585,48 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     auto piece = [&](int r, int c) {
                         return slices + (uint32_t)(((q + (c >> 3)) & 1) * SLICE + r * 128) + (uint32_t)(((c ^ r) & 7) << 4);
                     };
-#pragma unroll 4
-                    for (int i = lane; i < n << lg_pieces; i += 32) {
-                        const int r = i >> lg_pieces, c = i & ((1 << lg_pieces) - 1);
-                        uint8_t* const at = dst + r * pitch;
-                        const int head = (int)(-(intptr_t)at & 15), off = head + 16 * c;
-                        if (off + 16 > bytes) continue;
-                        uint4 v = lds128(piece(r, c));
-                        if (head) v = f8::cut16(v, lds128(piece(r, c + 1)), head);
-                        *reinterpret_cast<uint4*>(at + off) = v;
+                    // (four at a time: loads, then stores; every address lies in the warp's two slices)
+                    const int total = n << lg_pieces, head0 = (int)(-(intptr_t)dst & 15), skew = (int)(pitch & 15);
+#pragma unroll 1
+                    for (int i0 = lane; i0 < total; i0 += 128) {
+                        uint4 x[4], y[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int i = i0 + 32 * u, r = i >> lg_pieces & 31, c = i & ((1 << lg_pieces) - 1);
+                            x[u] = lds128(piece(r, c));
+                            y[u] = lds128(piece(r, c + 1));
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int i = i0 + 32 * u, r = i >> lg_pieces, c = i & ((1 << lg_pieces) - 1);
+                            const int head = (head0 - r * skew) & 15, off = head + 16 * c;
+                            if (i < total && off + 16 <= bytes)
+                                *reinterpret_cast<uint4*>(dst + r * pitch + off) = f8::cut16(x[u], y[u], head);
+                        }
                     }
                     // ... and what is left at either end by values, a row's by eight lanes
-#pragma unroll 2
-                    for (int r = lane >> 3; r < n; r += 4) {
-                        uint8_t* const at = dst + r * pitch;
-                        const int head = min((int)(-(intptr_t)at & 15), bytes), tail = (bytes - head) & 15;
-                        for (int k = (lane & 7) * es; k < head + tail; k += 8 * es) {
-                            const int off = k < head ? k : bytes - tail + k - head;
-                            const uint32_t from = piece(r, off >> 4) + (uint32_t)(off & 15);
-                            if (es == 4) *reinterpret_cast<int*>(at + off) = lds32(from);
-                            else *reinterpret_cast<uint16_t*>(at + off) = (uint16_t)lds16(from);
+                    const int ends = bytes & 15 ? 30 : head0 | skew ? 16 : 0;
+#pragma unroll 1
+                    for (int k = (lane & 7) * es; k < ends; k += 8 * es) {
+#pragma unroll 1
+                        for (int r0 = lane >> 3; r0 < n; r0 += 16) {
+                            uint32_t v[4];
+                            int off[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const int r = r0 + 4 * u, head = min((head0 - r * skew) & 15, bytes), tail = (bytes - head) & 15;
+                                off[u] = k < head ? k : bytes - tail + k - head;
+                                if (r >= n || k >= head + tail) off[u] = -1;
+                                const uint32_t from = piece(r & 31, max(off[u], 0) >> 4) + (uint32_t)(off[u] & 15);
+                                v[u] = (uint32_t)lds32(from & ~3u) >> (8 * (from & 2u));
+                            }
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                uint8_t* const at = dst + (r0 + 4 * u) * pitch + off[u];
+                                if (off[u] < 0) continue;
+                                if (es == 4) *reinterpret_cast<uint32_t*>(at) = v[u];
+                                else *reinterpret_cast<uint16_t*>(at) = (uint16_t)v[u];
+                            }
                         }
                     }
                     __syncwarp();
