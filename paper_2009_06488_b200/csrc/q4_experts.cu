@@ -18,8 +18,9 @@ namespace experts {
 
 constexpr int NW = 32;                     // warps of a sort block
 constexpr int KEEP = 4;                    // ids a lane keeps in registers (a block of kOneBlock pairs)
-constexpr int64_t kOneBlock = 4096;        // pairs per block; up to as many are sorted by one block
+constexpr int64_t kOneBlock = 4096;        // pairs per block; up to as many are placed by one block
 constexpr int kMaxChunks = 128;
+constexpr int64_t kRowsPerBlock = 2048;    // rows without a pair per further block
 
 static int chunks_of(int64_t n)
 {
@@ -85,7 +86,8 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
     int32_t *base = sm + L.base, *total = sm + L.total, *before = sm + L.before, *first = sm + L.first;
     int32_t *local = sm + L.local, *delta = sm + L.delta, *sums = sm + L.sums, *order = sm + L.order;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t lo = blockIdx.x * chunk, hi = min((int64_t)n, lo + chunk);
+    // without counts of chunks every block sorts all pairs, and all but the first only for the rows that no pair takes
+    const int64_t lo = hist ? blockIdx.x * chunk : 0, hi = min((int64_t)n, lo + chunk);
     const int64_t piece = ((chunk + NW - 1) / NW + 31) / 32 * 32;
     const int64_t wlo = min(hi, lo + warp * piece), whi = min(hi, wlo + piece);
     const bool kept = piece <= KEEP * 32;  // a lane's ids stay in registers, the block's order in shared memory
@@ -185,6 +187,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
         for (int r = first[k] + total[k] + from; r < first[k + 1]; r += step) if (r < rows) source[r] = -1;
     for (int64_t r = (int64_t)first[E] + blockIdx.x * (NW * 32) + threadIdx.x; r < rows; r += (int64_t)gridDim.x * (NW * 32))
         source[r] = -1;
+    if (!hist && blockIdx.x > 0) return;
 
     const int bits = 32 - __clz(E - 1);        // of an expert number (0 for E = 1)
     auto place = [&](int64_t i, int x) {
@@ -260,12 +263,12 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     }
 }
 
-// Row and weight of pair j0 + (lane & 7) of a token, -1 where there is none: every eight threads of a token hold
-// its next eight pairs between them.
+// Row and weight of pair j0 + lane % J of a token, -1 where there is none: every J threads of a token hold its next J
+// pairs between them.
 struct Pair { int s; float w; };
-__device__ __forceinline__ Pair pair_of(const ExpertRowsParams& p, int64_t t, bool mine, int j0, int lane)
+template <int J> __device__ __forceinline__ Pair pair_of(const ExpertRowsParams& p, int64_t t, bool mine, int j0, int lane)
 {
-    const int j = j0 + (lane & 7);
+    const int j = j0 + lane % J;
     Pair q{-1, 1.0f};
     if (mine && j < p.topk) {
         q.s = __ldg(p.slot + t * p.topk + j);
@@ -273,12 +276,12 @@ __device__ __forceinline__ Pair pair_of(const ExpertRowsParams& p, int64_t t, bo
     }
     return q;
 }
-__device__ __forceinline__ void spread(const ExpertRowsParams& p, const Pair& q, int lane, int (&s)[8], float (&w)[8])
+template <int J> __device__ __forceinline__ void spread(const ExpertRowsParams& p, const Pair& q, int lane, int (&s)[J], float (&w)[J])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        s[j] = __shfl_sync(0xFFFFFFFFu, q.s, (lane & 24) + j);
-        w[j] = __shfl_sync(0xFFFFFFFFu, q.w, (lane & 24) + j);
+    for (int j = 0; j < J; ++j) {
+        s[j] = __shfl_sync(0xFFFFFFFFu, q.s, lane / J * J + j);
+        w[j] = __shfl_sync(0xFFFFFFFFu, q.w, lane / J * J + j);
         if (s[j] >= p.rows) s[j] = -1;
     }
 }
@@ -297,25 +300,25 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const int left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
     const f8::Span in = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
     const bool inner = c >= 8 && left >= 16;
-    constexpr int JN = VEC ? 8 : 2;                  // rows in flight
+    // Rows in flight.  Unaligned ones take two pieces each and code that has to be fetched once per block: two at a time with four
+    // blocks per SM 44 us for 4096 x 8 x 2047 (four and three 46, eight and two 56; aligned rows 24).
+    constexpr int J = VEC ? 8 : 2;
     float acc[8] = {};
-    for (int j0 = 0; j0 < p.topk; j0 += 8) {
-        int s[8];
-        float w[8];
-        spread(p, pair_of(p, t, mine, j0, lane), lane, s, w);
+#pragma unroll 1
+    for (int j0 = 0; j0 < p.topk; j0 += J) {
+        int s[J];
+        float w[J];
+        f8::Coming<VEC, T> v[J];
+        spread(p, pair_of<J>(p, t, mine, j0, lane), lane, s, w);
 #pragma unroll
-        for (int h = 0; h < 8; h += JN) {
-            f8::Coming<VEC, T> v[JN];
+        for (int j = 0; j < J; ++j)
+            v[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, in);
 #pragma unroll
-            for (int j = h; j < h + JN; ++j)
-                v[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, in);
+        for (int j = 0; j < J; ++j) {
+            if (s[j] < 0) continue;                 // a dropped pair's weight may be anything
+            const Eight<T> y = v[j].get(n);
 #pragma unroll
-            for (int j = h; j < h + JN; ++j) {
-                if (s[j] < 0) continue;             // a dropped pair's weight may be anything
-                const Eight<T> y = v[j - h].get(n);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], y.get(i), acc[i]);
-            }
+            for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], y.get(i), acc[i]);
         }
     }
     Eight<T> o;
@@ -345,7 +348,7 @@ __device__ __forceinline__ float reduce8(float (&d)[8], int lane)
 // written front to back with the gradients from L2, 4096 x 8 x 2048 takes 68 us instead of 60: the streams push the
 // gradients out of L2.  Rows that happen to lie in token order take 48: the rest is the scattered writes.)
 template <int TYPE, bool VEC>
-__global__ void __launch_bounds__(256, VEC && TYPE != Q4_F32 ? 3 : 2)
+__global__ void __launch_bounds__(256, VEC && TYPE == Q4_F32 ? 2 : 3)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
     f8::wait_for_predecessor();
@@ -353,70 +356,68 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if ((int)blockIdx.x >= token_blocks) {
         // rows that belong to no pair get zeros: 32 rows per warp
+        constexpr int PV = 16 / (int)sizeof(T);
         const int64_t r0 = ((int64_t)blockIdx.x - token_blocks) * 256 + warp * 32;
         const int pair = r0 + lane < p.rows ? p.source[r0 + lane] : 0;
-        Eight<T> zero;
-        zero.zero();
         for (unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0); none; none &= none - 1) {
-            T* dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
-            for (int c0 = 0; c0 < p.D; c0 += 256) {
-                const int c = c0 + lane * 8;
-                f8::store8<VEC>(dst + c, p.D - c, zero, lane, 32);
-            }
+            T* const dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
+            const int head = min((int)(-(uintptr_t)dst & 15) / (int)sizeof(T), p.D), body = (p.D - head) / PV;
+            for (int k = lane; k < body; k += 32) __stcs(reinterpret_cast<uint4*>(dst + head) + k, make_uint4(0, 0, 0, 0));
+            const int rest = p.D - body * PV;              // values before and behind the pieces of 16 bytes
+            if (lane < rest) dst[lane < head ? lane : lane + body * PV] = f8::from_f<T>(0.0f);
         }
         return;
     }
-    constexpr int JN = VEC ? 8 : 4;                  // rows in flight
+    // Rows in flight.  Unaligned: two with three blocks per SM 121 us for 4096 x 8 x 2047 (four and two 143, one and four 184;
+    // aligned rows 59): issue binds, a row's cut and put-together pieces are three times an aligned one's instructions.
+    constexpr int J = VEC ? 8 : 2;
     __shared__ float part[8][8];
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
     // a block walks groups of TY tokens; the next group's pairs are loaded before this one's rows
     const f8::Span gs = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D), ys = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
     int64_t t = (int64_t)blockIdx.x * TY + ty;
     const int64_t step = (int64_t)token_blocks * TY;
-    Pair ahead = pair_of(p, t, t < p.tokens, 0, lane);
+    Pair ahead = pair_of<J>(p, t, t < p.tokens, 0, lane);
     for (int64_t group = (int64_t)blockIdx.x * TY; group < p.tokens; group += step, t += step) {
         const bool mine = t < p.tokens;
         const T* g = static_cast<const T*>(p.X) + (mine ? t * p.ldx : 0);
-        for (int j0 = 0; j0 < p.topk; j0 += 8) {
-            int s[8];
-            float w[8], dot[8] = {};
+#pragma unroll 1
+        for (int j0 = 0; j0 < p.topk; j0 += J) {
+            int s[J];
+            float w[J], dot[8] = {};
             spread(p, ahead, lane, s, w);
-            ahead = j0 + 8 < p.topk ? pair_of(p, t, mine, j0 + 8, lane) : pair_of(p, t + step, t + step < p.tokens, 0, lane);
+            ahead = j0 + J < p.topk ? pair_of<J>(p, t, mine, j0 + J, lane) : pair_of<J>(p, t + step, t + step < p.tokens, 0, lane);
             // (rows of any alignment: whole warps go on together)
             for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
                 const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
                 const bool inner = c >= 8 && left >= 16;
                 f8::Coming<VEC, T> dc;
                 dc.load(g + c, n, inner, gs);
+                f8::Coming<VEC, T> yc[J];
 #pragma unroll
-                for (int h = 0; h < 8; h += JN) {
-                    f8::Coming<VEC, T> yc[JN];
+                for (int j = 0; j < J; ++j)
+                    yc[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, ys);
+                const Eight<T> d = dc.get(n);
 #pragma unroll
-                    for (int j = h; j < h + JN; ++j)
-                        yc[j - h].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, ys);
-                    const Eight<T> d = dc.get(n);
+                for (int j = 0; j < J; ++j) {
+                    if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
+                    const Eight<T> y = yc[j].get(n);
+                    float o[8];
 #pragma unroll
-                    for (int j = h; j < h + JN; ++j) {
-                        if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
-                        const Eight<T> y = yc[j - h].get(n);
-                        float o[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            dot[j] = fmaf(d.get(i), y.get(i), dot[j]);
-                            o[i] = w[j] * d.get(i);
-                        }
-                        Eight<T> e;
-                        f8::pack8(e, o);
-                        f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e,
-                                        tx, TX);
+                    for (int i = 0; i < 8; ++i) {
+                        dot[j] = fmaf(d.get(i), y.get(i), dot[j]);
+                        o[i] = w[j] * d.get(i);
                     }
+                    Eight<T> e;
+                    f8::pack8(e, o);
+                    f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e, tx, TX);
                 }
             }
             if (TX >= 32) {
                 const float sum = reduce8(dot, lane);
                 if (lane < 8) part[warp][lane] = sum;
                 __syncthreads();
-                if (tx < 8) {
+                if (tx < J) {
                     float all = 0.0f;
                     for (int k = 0; k < TX / 32; ++k) all += part[warp + k][tx];
                     if (mine && j0 + tx < p.topk) p.dw[t * p.topk + j0 + tx] = all;
@@ -424,7 +425,7 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
                 __syncthreads();
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < J; ++j) {
                     for (int o = TX >> 1; o; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
                     if (tx == 0 && mine && j0 + j < p.topk) p.dw[t * p.topk + j0 + j] = dot[j];
                 }
@@ -471,7 +472,11 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
         const cudaError_t err = f8::launch(count_kernel, (unsigned)g, 512, (size_t)E * 4, st, ids, n, E, chunk, hist);
         if (err != cudaSuccess) return err;
     }
-    return f8::launch(place_kernel, (unsigned)g, NW * 32, smem, st, ids, n, E, align, chunk,
+    // one block's pairs: rows that no pair takes are shared by more blocks (2984 pairs, 256 experts, align 128, 32512 such
+    // rows: 10.0 us by one block, 7.4 by all; 512 rows per block are no faster than 2048)
+    const int64_t free_rows = (int64_t)rows - n;
+    const unsigned blocks = g > 1 ? (unsigned)g : 1u + (unsigned)(free_rows <= 0 ? 0 : free_rows / kRowsPerBlock < 63 ? free_rows / kRowsPerBlock : 63);
+    return f8::launch(place_kernel, blocks, NW * 32, smem, st, ids, n, E, align, chunk,
                       (const int32_t*)(g > 1 ? hist : nullptr), starts, source, rows, slot);
 }
 
