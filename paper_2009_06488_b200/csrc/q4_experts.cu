@@ -231,6 +231,7 @@ place_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t E, int32_t alig
 // ------------------------------------------------------------------------------------- rows
 // A block's 256 threads are TY rows (or tokens) of TX threads, TX a power of two of 8..256.
 using f8::Eight;
+constexpr int kUnaligned = 2;              // rows in flight that need not begin on multiples of 16 bytes
 
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(256)
@@ -247,12 +248,11 @@ gather_kernel(const ExpertRowsParams p, int tx_bits)
     const float w = on && p.w ? p.w[pair] : 1.0f;
     const T* src = static_cast<const T*>(p.X) + (on ? t * p.ldx : 0);
     T* dst = static_cast<T*>(p.out) + (mine ? r * p.ldo : 0);
-    const f8::Span in = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D);
     for (int c0 = 0; c0 < p.D; c0 += TX * 8) {             // whole warps
         const int c = c0 + tx * 8, left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
         f8::Coming<VEC, T> x;
-        x.load(src + c, on ? n : 0, c >= 8 && left >= 16, in);
-        Eight<T> v = x.get(on ? n : 0);
+        x.load(src + c, on ? n : 0, f8::careful_at(t, p.tokens, c, left, p.D));
+        Eight<T> v = x.get(src + c, on ? n : 0);
         if (p.w) {
             float f[8];
 #pragma unroll
@@ -298,11 +298,9 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const int c = (blockIdx.y * TX + tx) * 8, lane = threadIdx.x & 31;
     const bool mine = t < p.tokens;
     const int left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
-    const f8::Span in = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
-    const bool inner = c >= 8 && left >= 16;
     // Rows in flight.  Unaligned ones take two pieces each and code that has to be fetched once per block: two at a time with four
     // blocks per SM 44 us for 4096 x 8 x 2047 (four and three 46, eight and two 56; aligned rows 24).
-    constexpr int J = VEC ? 8 : 2;
+    constexpr int J = VEC ? 8 : kUnaligned;
     float acc[8] = {};
 #pragma unroll 1
     for (int j0 = 0; j0 < p.topk; j0 += J) {
@@ -312,11 +310,12 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
         spread(p, pair_of<J>(p, t, mine, j0, lane), lane, s, w);
 #pragma unroll
         for (int j = 0; j < J; ++j)
-            v[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, in);
+            v[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0,
+                      f8::careful_at(s[j], p.rows, c, left, p.D));
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             if (s[j] < 0) continue;                 // a dropped pair's weight may be anything
-            const Eight<T> y = v[j].get(n);
+            const Eight<T> y = v[j].get(static_cast<const T*>(p.Y) + s[j] * p.ldy + c, n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], y.get(i), acc[i]);
         }
@@ -370,38 +369,40 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
     }
     // Rows in flight.  Unaligned: two with three blocks per SM 121 us for 4096 x 8 x 2047 (four and two 143, one and four 184;
     // aligned rows 59): issue binds, a row's cut and put-together pieces are three times an aligned one's instructions.
-    constexpr int J = VEC ? 8 : 2;
+    constexpr int J = VEC ? 8 : kUnaligned;
     __shared__ float part[8][8];
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
-    // a block walks groups of TY tokens; the next group's pairs are loaded before this one's rows
-    const f8::Span gs = f8::span_of<T>(p.X, p.tokens, p.ldx, p.D), ys = f8::span_of<T>(p.Y, p.rows, p.ldy, p.D);
-    int64_t t = (int64_t)blockIdx.x * TY + ty;
-    const int64_t step = (int64_t)token_blocks * TY;
-    Pair ahead = pair_of<J>(p, t, t < p.tokens, 0, lane);
-    for (int64_t group = (int64_t)blockIdx.x * TY; group < p.tokens; group += step, t += step) {
+    // a block walks groups of TY tokens (unaligned: J pairs of each, other blocks the others); the next group's pairs are
+    // loaded before this one's rows
+    const int parts = VEC ? 1 : (p.topk + J - 1) / J;
+    const int from = VEC ? 0 : (int)blockIdx.x % parts * J, to = VEC ? p.topk : min(p.topk, from + J);
+    int64_t t = (int64_t)(blockIdx.x / (unsigned)parts) * TY + ty;
+    const int64_t step = (int64_t)(token_blocks / parts) * TY;
+    Pair ahead = pair_of<J>(p, t, t < p.tokens, from, lane);
+    for (int64_t group = t - ty; group < p.tokens; group += step, t += step) {
         const bool mine = t < p.tokens;
         const T* g = static_cast<const T*>(p.X) + (mine ? t * p.ldx : 0);
 #pragma unroll 1
-        for (int j0 = 0; j0 < p.topk; j0 += J) {
+        for (int j0 = from; j0 < to; j0 += J) {
             int s[J];
             float w[J], dot[8] = {};
             spread(p, ahead, lane, s, w);
-            ahead = j0 + J < p.topk ? pair_of<J>(p, t, mine, j0 + J, lane) : pair_of<J>(p, t + step, t + step < p.tokens, 0, lane);
+            ahead = j0 + J < to ? pair_of<J>(p, t, mine, j0 + J, lane) : pair_of<J>(p, t + step, t + step < p.tokens, from, lane);
             // (rows of any alignment: whole warps go on together)
             for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
                 const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
-                const bool inner = c >= 8 && left >= 16;
                 f8::Coming<VEC, T> dc;
-                dc.load(g + c, n, inner, gs);
+                dc.load(g + c, n, f8::careful_at(t, p.tokens, c, left, p.D));
                 f8::Coming<VEC, T> yc[J];
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    yc[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0, inner, ys);
-                const Eight<T> d = dc.get(n);
+                    yc[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0,
+                               f8::careful_at(s[j], p.rows, c, left, p.D));
+                const Eight<T> d = dc.get(g + c, n);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
-                    const Eight<T> y = yc[j].get(n);
+                    const Eight<T> y = yc[j].get(static_cast<const T*>(p.Y) + s[j] * p.ldy + c, n);
                     float o[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -498,7 +499,8 @@ cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t s
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const int64_t groups = ((int64_t)p.tokens + ty - 1) / ty;
-    const int tb = (int)(groups < 3 * 148 ? groups : 3 * 148);           // resident at once
+    const int parts = p.vec ? 1 : (p.topk + kUnaligned - 1) / kUnaligned, most = 3 * 148 > parts ? 3 * 148 / parts : 1;
+    const int tb = (int)(groups < most ? groups : most) * parts;         // resident at once
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
     return Q4_ROWS_LAUNCH(combine_grad_kernel, grid, p, b, tb);
 }

@@ -82,36 +82,35 @@ __device__ __forceinline__ uint4 cut16(const uint4& a, const uint4& b, int off)
     return make_uint4(__funnelshift_r(t0, t1, sh), __funnelshift_r(t1, t2, sh), __funnelshift_r(t2, t3, sh), __funnelshift_r(t3, t4, sh));
 }
 
-// Rows that need not begin on multiples of 16 bytes are read in the aligned pieces that hold their values, and
-// cut afterwards.  A piece may hold bytes of a row's neighbours, never bytes outside the matrix's first and last value:
-// such a piece is read value by value.
-struct Span { uintptr_t lo, hi; };
-template <typename T> __device__ __forceinline__ Span span_of(const void* base, int64_t rows, int64_t ld, int cols)
+// Rows that need not begin on multiples of 16 bytes are read in the aligned pieces that hold their values, and cut
+// afterwards.  A piece may hold bytes of a row's neighbours, never bytes before the matrix's first value or behind its
+// last: `careful` values, the first and last eights of those rows, are read one by one.
+__device__ __forceinline__ bool careful_at(int64_t row, int64_t rows, int c, int left, int cols)
 {
-    return {(uintptr_t)base, (uintptr_t)base + (uintptr_t)(rows > 0 ? ((rows - 1) * ld + cols) * (int64_t)sizeof(T) : 0)};
+    return (c == 0 && row == 0) || (left < 16 && row == rows - 1) || cols < 16;
 }
 template <typename T> __device__ __noinline__ uint4 piece_by_values(uintptr_t at, uintptr_t lo, uintptr_t hi)
 {
-    unsigned long long w[2] = {0, 0};
+    constexpr int ES = (int)sizeof(T);
+    uint32_t v[16 / ES], w[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll 1
-        for (int i = 0; i < 8; i += (int)sizeof(T)) {
-            const uintptr_t v = at + 8 * h + i;
-            if (v < lo || v >= hi) continue;
-            if (sizeof(T) == 4) w[h] |= (unsigned long long)*reinterpret_cast<const uint32_t*>(v) << (8 * i);
-            else w[h] |= (unsigned long long)*reinterpret_cast<const uint16_t*>(v) << (8 * i);
-        }
-    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+    for (int i = 0; i < 16 / ES; ++i) {            // all under way before one is used
+        const uintptr_t from = at + ES * i;
+        v[i] = 0;
+        if (from >= lo && from < hi) v[i] = ES == 4 ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = ES == 4 ? v[k] : v[2 * k % (16 / ES)] | v[(2 * k + 1) % (16 / ES)] << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Eight values on their way.  VEC: all eight exist (n = 8, or 0 for none) at an address that is a multiple of 16
+// Eight values on their way.  VEC: all eight exist (n > 0, or none) at an address that is a multiple of 16
 // bytes; else n of them (0..8) anywhere.  What does not exist reads 0.
 template <bool VEC, typename T> struct Coming;
 template <typename T> struct Coming<true, T> {
     Eight<T> e;
     // The data is streamed: read once.
-    __device__ __forceinline__ void load(const T* p, int n, bool, const Span&)
+    __device__ __forceinline__ void load(const T* p, int n, bool)
     {
         e.zero();
         if (n > 0) {
@@ -122,38 +121,34 @@ template <typename T> struct Coming<true, T> {
                              : "l"(reinterpret_cast<const uint4*>(p) + k));
         }
     }
-    __device__ __forceinline__ const Eight<T>& get(int) const { return e; }
+    __device__ __forceinline__ const Eight<T>& get(const T*, int) { return e; }
 };
 template <typename T> struct Coming<false, T> {
     static constexpr int G = Eight<T>::NW / 4 + 1;
     uint4 g[G];
-    int off;
-    // `inner`: the row has eight values more on either side, so that no piece needs a check.
-    __device__ __forceinline__ void load(const T* p, int n, bool inner, const Span& in)
+    int off;                                       // of the values in the first piece; + 16: `careful`, not loaded yet
+    __device__ __forceinline__ void load(const T* p, int n, bool careful)
     {
         off = (int)((uintptr_t)p & 15);
-        const uintptr_t at0 = (uintptr_t)p - off;
-#pragma unroll
-        for (int k = 0; k < G; ++k) g[k] = make_uint4(0, 0, 0, 0);
-        if (inner) {
-#pragma unroll
-            for (int k = 0; k < G; ++k)
-                asm volatile("{\n\t.reg .pred q;\n\tsetp.gt.s32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-                             : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at0 + 16 * k), "r"(n));
-            return;
-        }
+        const uintptr_t at = (uintptr_t)p - off;
+        const int end = n > 0 && !careful ? off + n * (int)sizeof(T) : 0;
 #pragma unroll
         for (int k = 0; k < G; ++k) {
-            const uintptr_t at = at0 + 16 * k;
-            const bool need = n > 0 && 16 * k < off + n * (int)sizeof(T), inside = at >= in.lo && at + 16 <= in.hi;
-            asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-                         : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at), "r"((int)(need && inside)));
-            if (need && !inside) g[k] = piece_by_values<T>(at, in.lo, in.hi);
+            g[k] = make_uint4(0, 0, 0, 0);
+            asm volatile("{\n\t.reg .pred q;\n\tsetp.gt.s32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                         : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at + 16 * k), "r"(end - 16 * k));
         }
+        if (careful) off += 16;
     }
-    __device__ __forceinline__ Eight<T> get(int n) const
+    __device__ __forceinline__ Eight<T> get(const T* p, int n)
     {
         Eight<T> e;
+        if (off > 15) {                            // here, not in load(): a call there would hold up the loads behind it
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+                if (n > 0) g[k] = piece_by_values<T>(((uintptr_t)p & ~(uintptr_t)15) + 16 * k, (uintptr_t)p, (uintptr_t)(p + n));
+            off -= 16;
+        }
 #pragma unroll
         for (int k = 0; k + 1 < G; ++k) {
             const uint4 c = cut16(g[k], g[k + 1], off);

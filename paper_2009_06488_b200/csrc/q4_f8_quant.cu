@@ -94,14 +94,12 @@ quantize_kernel(const QuantizeParams p)
     const bool whole = (int64_t)(rb + 1) * TR <= p.rows && (cb + 1) * BLK <= p.cols;
     Coming<VEC, T> x[RT];
     Eight<T> v[RT];
-    const bool inner = c0 >= 8 && p.cols - c0 >= 16;
-    const Span in = span_of<T>(p.X, p.x_rows, p.ldx, p.cols);
     if (whole && !p.source) {
         const T* src = static_cast<const T*>(p.X) + r0 * p.ldx + c0;
 #pragma unroll
-        for (int i = 0; i < RT; ++i) x[i].load(src + i * p.ldx, 8, inner, in);
+        for (int i = 0; i < RT; ++i) x[i].load(src + i * p.ldx, 8, careful_at(r0 + i, p.x_rows, c0, p.cols - c0, p.cols));
 #pragma unroll
-        for (int i = 0; i < RT; ++i) v[i] = x[i].get(8);
+        for (int i = 0; i < RT; ++i) v[i] = x[i].get(src + i * p.ldx, 8);
     } else {
         int64_t from = -1;
         if (cx < RT && r0 + cx < p.rows) {
@@ -115,10 +113,14 @@ quantize_kernel(const QuantizeParams p)
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int64_t r = __shfl_sync(0xFFFFFFFFu, from, (lane & 16) + i);
-            x[i].load(static_cast<const T*>(p.X) + (r >= 0 ? r * p.ldx + c0 : 0), r >= 0 ? nc : 0, inner, in);
+            x[i].load(static_cast<const T*>(p.X) + (r >= 0 ? r * p.ldx + c0 : 0), r >= 0 ? nc : 0,
+                      careful_at(r, p.x_rows, c0, p.cols - c0, p.cols));
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i) v[i] = x[i].get(nc);
+        for (int i = 0; i < RT; ++i) {
+            const int64_t r = VEC ? 0 : __shfl_sync(0xFFFFFFFFu, from, (lane & 16) + i);
+            v[i] = x[i].get(static_cast<const T*>(p.X) + r * p.ldx + c0, r >= 0 ? nc : 0);
+        }
     }
 
     float binv = 0.0f;
