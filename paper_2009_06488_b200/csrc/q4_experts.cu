@@ -302,12 +302,14 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     // blocks per SM 44 us for 4096 x 8 x 2047 (four and three 46, eight and two 56; aligned rows 24).
     constexpr int J = VEC ? 8 : kUnaligned;
     float acc[8] = {};
+    Pair ahead = pair_of<J>(p, t, mine, 0, lane);
 #pragma unroll 1
     for (int j0 = 0; j0 < p.topk; j0 += J) {
         int s[J];
         float w[J];
         f8::Coming<VEC, T> v[J];
-        spread(p, pair_of<J>(p, t, mine, j0, lane), lane, s, w);
+        spread(p, ahead, lane, s, w);
+        if (j0 + J < p.topk) ahead = pair_of<J>(p, t, mine, j0 + J, lane);
 #pragma unroll
         for (int j = 0; j < J; ++j)
             v[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0,
