@@ -682,35 +682,50 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             // one tile per cluster: CTA `split` of a rank adds its 128 / splits rows of all partial tiles, in order
             Walk<BN> walk(p, lane);
             if (walk.get(cluster_id, t)) {
-                for (int r = split * TMC / splits + warp - 4; r < (split + 1) * TMC / splits; r += 8) {
-                    const int row = t.m0 + (int)rank * TMC + r, col = t.n0 + lane * 4;
-                    if (row >= t.m_end || col >= g.N) continue;
-                    float v[4] = {};
-                    for (int s = 0; s < splits; ++s) {
-                        const uint4 q = lds128_cluster(map_to_cta(sbase + (uint32_t)((r * (BN + 4) + lane * 4) * 4), (uint32_t)s * 2 + rank));
-                        v[0] += __uint_as_float(q.x);
-                        v[1] += __uint_as_float(q.y);
-                        v[2] += __uint_as_float(q.z);
-                        v[3] += __uint_as_float(q.w);
+                // eight rows of a warp at a time (all of them for two pairs or more): their loads are under way together
+                const int col = t.n0 + lane * 4, have = min(4, g.N - col), end = (split + 1) * TMC / splits;
+#pragma unroll 1
+                for (int r0 = split * TMC / splits + warp - 4; r0 < end; r0 += 64) {
+                    float v[8][4] = {};
+#pragma unroll 1
+                    for (int i = 0, s = split; i < splits; ++i, s = s + 1 == splits ? 0 : s + 1) {     // not all from one CTA at a time
+                        const uint32_t part = map_to_cta(sbase, (uint32_t)s * 2 + rank) + (uint32_t)(lane * 16);
+                        uint4 q[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            q[u] = make_uint4(0, 0, 0, 0);
+                            if (r0 + 8 * u < end) q[u] = lds128_cluster(part + (uint32_t)((r0 + 8 * u) * (BN + 4) * 4));
+                        }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            v[u][0] += __uint_as_float(q[u].x);
+                            v[u][1] += __uint_as_float(q[u].y);
+                            v[u][2] += __uint_as_float(q[u].z);
+                            v[u][3] += __uint_as_float(q[u].w);
+                        }
                     }
-                    const int64_t at = (t.crow + (int)rank * TMC + r) * g.ldc + col;
-                    const int have = min(4, g.N - col);
-                    if (g.c_type == Q4_F32) {
-                        float* dst = static_cast<float*>(g.C) + at;
-                        if (p.c_vec && have == 4) *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
-                        else
-    #pragma unroll
-                            for (int j = 0; j < 4; ++j) if (j < have) dst[j] = v[j];
-                    } else {
-                        const bool bf = g.c_type == Q4_BF16;
-                        const uint32_t w0 = bf ? pack2(v[0], v[1], (const __nv_bfloat16*)nullptr) : pack2(v[0], v[1], (const __half*)nullptr);
-                        const uint32_t w1 = bf ? pack2(v[2], v[3], (const __nv_bfloat16*)nullptr) : pack2(v[2], v[3], (const __half*)nullptr);
-                        uint16_t* dst = static_cast<uint16_t*>(g.C) + at;
-                        if (p.c_vec && have == 4) {
-                            *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const int r = r0 + 8 * u, row = (int)rank * TMC + r;
+                        if (r >= end || t.m0 + row >= t.m_end || have <= 0) continue;
+                        const int64_t at = (t.crow + row) * g.ldc + col;
+                        if (g.c_type == Q4_F32) {
+                            float* dst = static_cast<float*>(g.C) + at;
+                            if (p.c_vec && have == 4) *reinterpret_cast<float4*>(dst) = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
+                            else
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) if (j < have) dst[j] = v[u][j];
                         } else {
-    #pragma unroll
-                            for (int j = 0; j < 4; ++j) if (j < have) dst[j] = (uint16_t)((j < 2 ? w0 : w1) >> (16 * (j & 1)));
+                            const bool bf = g.c_type == Q4_BF16;
+                            const uint32_t w0 = bf ? pack2(v[u][0], v[u][1], (const __nv_bfloat16*)nullptr) : pack2(v[u][0], v[u][1], (const __half*)nullptr);
+                            const uint32_t w1 = bf ? pack2(v[u][2], v[u][3], (const __nv_bfloat16*)nullptr) : pack2(v[u][2], v[u][3], (const __half*)nullptr);
+                            uint16_t* dst = static_cast<uint16_t*>(g.C) + at;
+                            if (p.c_vec && have == 4) {
+                                *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) if (j < have) dst[j] = (uint16_t)((j < 2 ? w0 : w1) >> (16 * (j & 1)));
+                            }
                         }
                     }
                 }
@@ -850,15 +865,22 @@ q4_status launch_gemm_f8_pair(const GemmF8Params& g, cudaStream_t st)
     const int64_t t_wide = (tm * n256 + pairs - 1) / pairs * (per * 780 + 2500);
     const int64_t t_narrow = (tm * n128 + pairs - 1) / pairs * (per * 480 + 2500);
     const bool wide = g.N > 128 && t_wide <= t_narrow;
-    // Splitting the depth pays for its exchange (about 3.5 us) from 48 blocks, or 32 of the dearer ones with scales
-    // by row (100 x 4096 x 4096: 12.3 us whole, 13.2 in two parts), and only while all clusters run at once: a
-    // cluster lies within a GPC, so 33 of four CTAs, 22 of six and 15 of eight fit where 74 pairs do (2304 x 256 x
-    // 4097, 18 tiles: 16.9 us whole, 14.8 in two parts, 13.4 in three, 21.2 in four; 512 x 2304 x 2304, 36 tiles:
-    // 9.1 whole, 20.6 in two).
+    // Depth split of narrow tiles, again by measured clocks: 445 per block, 740 with scales by row, 1700 for the exchange and 90
+    // for each pair that takes part in it; only while all clusters run at once (a cluster lies within a GPC, so 33 of four CTAs,
+    // 22 of six and 15 of eight fit where 74 pairs do).  Whole, in two, three and four parts: 200 x 250 x 1024 7.0, 7.2, 6.8, 6.7
+    // us, with scales by row 8.2, 7.7, 7.3, 7.0; 500 x 500 x 2048 7.9, 7.8, 7.5, 7.7; 1000 x 500 x 1024 6.1, 7.2, 8.0, -; 2304 x
+    // 256 x 4097 by row 18.2, 14.0, 12.5, -; 100 x 4096 x 4096 (32 tiles) 11.5, 12.3, -, -.
     int splits = 1;
-    if (!wide && g.mode == kDense && nkb >= (g.b_rows ? 32 : 48))
-        for (int k = 2; k <= 4; ++k)
-            if (tm * n128 <= clusters_of_device(k)) splits = k;
+    if (!wide && g.mode != kExpertRows) {
+        const int64_t block = g.b_rows ? 740 : 445;
+        int64_t best = per * block;
+        for (int k = 2; k <= 4; ++k) {
+            const int64_t clk = (per + k - 1) / k * block + 1700 + 90 * tm * n128 * k;
+            if (clk >= best || tm * n128 > clusters_of_device(k)) continue;
+            best = clk;
+            splits = k;
+        }
+    }
     p.splits = splits;
     p.tiles_n = (int)(wide ? n256 : n128);
     const size_t es = type_size(g.c_type);
