@@ -366,6 +366,9 @@ q4_status q4_dequantize(const int32_t* C, int64_t ldc, int32_t rows, int32_t col
  * allocates nothing and checks its host-side arguments before anything is launched.  Numbers
  * that live on the device (starts, slot, source, expert numbers) are bounds-checked by the
  * kernels: what lies outside its range is treated as absent, nothing outside a buffer is touched.
+ * Rows of float values may begin at any element (multiples of 16 bytes are fastest).  Bytes between a
+ * matrix's rows, where its pitch is larger than its width, may be read and are ignored; they are never
+ * written.
  */
 typedef enum { Q4_F32 = 0, Q4_BF16 = 1, Q4_F16 = 2 } q4_type;
 

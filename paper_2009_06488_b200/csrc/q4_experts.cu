@@ -10,7 +10,8 @@
 // Bound: latency (two short kernels; one for up to kOneBlock pairs).
 //
 // Rows: a row's D values are spread over up to 256 threads, 8 (16 bytes of a 16-bit type) each; a token's
-// topk rows are loaded before they are summed, in order and in binary32.  Bound: HBM.
+// topk rows are loaded before they are summed, in order and in binary32.  Bound: HBM; issue for rows that do not begin on
+// multiples of 16 bytes, which are read and written in aligned pieces (q4_f8.cuh).
 #include "q4_f8.cuh"
 
 namespace q4 {
@@ -299,7 +300,7 @@ combine_kernel(const ExpertRowsParams p, int tx_bits)
     const bool mine = t < p.tokens;
     const int left = mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
     // Rows in flight.  Unaligned ones take two pieces each and code that has to be fetched once per block: two at a time with four
-    // blocks per SM 44 us for 4096 x 8 x 2047 (four and three 46, eight and two 56; aligned rows 24).
+    // blocks per SM 43 us for 4096 x 8 x 2047 (four and three 46, eight and two 56; aligned rows 24).
     constexpr int J = VEC ? 8 : kUnaligned;
     float acc[8] = {};
     Pair ahead = pair_of<J>(p, t, mine, 0, lane);
@@ -370,7 +371,9 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
         return;
     }
     // Rows in flight.  Unaligned: two with three blocks per SM 121 us for 4096 x 8 x 2047 (four and two 143, one and four 184;
-    // aligned rows 59): issue binds, a row's cut and put-together pieces are three times an aligned one's instructions.
+    // aligned rows 59) while one block took all of a token's pairs: issue binds, a row's cut and put-together pieces are
+    // three times an aligned one's instructions.  Its pairs over several blocks 128, but 6 x 8 x 101 3.4 instead of 11.0
+    // and 64 x 8 x 2047 4.7 instead of 8.6.
     constexpr int J = VEC ? 8 : kUnaligned;
     __shared__ float part[8][8];
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;

@@ -12,7 +12,8 @@
 //   warps 1, 2   MMA issuers     (leader CTA) four 32-deep steps per block and 128 columns
 //   warp 3       places          of the tiles, found ahead for the accumulators
 //   warps 4..11  accumulators    each thread one row and BN / 2 columns; then scaled sums out through swizzled
-//                                staging slices and TMA stores (whole 32-row groups) or 16-byte stores (ragged ones)
+//                                staging slices and TMA stores (whole 32-row groups of aligned rows) or aligned 16-byte pieces cut
+//                                from them (ragged groups, rows that begin anywhere)
 //
 // Tensor memory holds four slots of 128 columns.  With HALVES = 2 each column half has two of them and its own
 // four accumulating warps, so a half's drain (and the two hand-offs around it) has three quarters of the
@@ -24,7 +25,7 @@
 // (issue slots bind: 4096^3 72 to 78 us), 32-column loads (they slow the products beside them: 87 us), a second
 // buffer (the loads of one warp do not overlap its arithmetic: no change), waiting for the next block before the
 // last multiply-adds (70 us), a warp that multiplies the scales for all (76 us).  In long runs the power cap binds:
-// 8192^3 448 us = 2.46 PFLOP/s in a short region, 524 us = 2.10 PFLOP/s at about 1.4 GHz in a long one.
+// 8192^3 430 to 460 us = 2.4 to 2.6 PFLOP/s in a short region, 527 us = 2.09 PFLOP/s at about 1.4 GHz in a long one.
 //
 // With SPLIT the cluster is 2 * splits CTAs that share one tile's depth; their partial tiles are added in
 // order through distributed shared memory (problems of few tiles).

@@ -21,7 +21,8 @@
 // rows read back spread over all banks.
 // Bound: HBM (each value is read once, each code written once), with instruction issue close behind (73 % before
 // whole tiles ran without conditions).  8192 x 4096 bf16: one way 17.6 us = 5.8 TB/s, both ways 25.0 us = 5.4
-// TB/s; float32 27.6 and 37.4 us.
+// TB/s; float32 27.6 and 37.4 us.  Rows that do not begin on multiples of 16 bytes (VEC false) are read in aligned pieces
+// and cut: 8192 x 4092 both ways 38.8 us (value by value 47.6), float32 8192 x 4091 52.8.
 #include "q4_f8.cuh"
 
 namespace q4 {
