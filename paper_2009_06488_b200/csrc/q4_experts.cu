@@ -372,7 +372,7 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
     }
     // Rows in flight.  Unaligned: two with three blocks per SM 121 us for 4096 x 8 x 2047 (four and two 143, one and four 184;
     // aligned rows 59) while one block took all of a token's pairs: issue binds, a row's cut and put-together pieces are
-    // three times an aligned one's instructions.  Its pairs over several blocks 128, but 6 x 8 x 101 3.4 instead of 11.0
+    // three times an aligned one's instructions.  Its pairs over several blocks 132, but 6 x 8 x 101 3.4 instead of 11.0
     // and 64 x 8 x 2047 4.7 instead of 8.6.
     constexpr int J = VEC ? 8 : kUnaligned;
     __shared__ float part[8][8];
@@ -407,7 +407,7 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
-                    const Eight<T> y = yc[j].get(static_cast<const T*>(p.Y) + s[j] * p.ldy + c, n);
+                    const Eight<T> y = yc[j].get(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), VEC || s[j] >= 0 ? n : 0);
                     float o[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {

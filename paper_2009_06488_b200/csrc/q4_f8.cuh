@@ -138,7 +138,7 @@ template <typename T> struct Coming<false, T> {
             asm volatile("{\n\t.reg .pred q;\n\tsetp.gt.s32 q, %5, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
                          : "+r"(g[k].x), "+r"(g[k].y), "+r"(g[k].z), "+r"(g[k].w) : "l"(at + 16 * k), "r"(end - 16 * k));
         }
-        if (careful) off += 16;
+        if (careful && n > 0) off += 16;
     }
     __device__ __forceinline__ Eight<T> get(const T* p, int n)
     {
