@@ -206,10 +206,10 @@ struct Walk {
             e = t / per;
             if (e >= g.E) return false;
             local = t - e * per;
-            // block boundaries: starts are rounded down, the depth's own end stays
+            // block boundaries: starts are rounded down, the depth's own end stays (an empty segment there is empty too)
             const int a = clamp_to(g.starts[e], 0, g.K), b = clamp_to(g.starts[e + 1], a, g.K);
             o.k0 = a / ROWB * ROWB;
-            o.nkb = b == g.K ? (b - o.k0 + ROWB - 1) / ROWB : (b / ROWB * ROWB - o.k0) / ROWB;
+            o.nkb = a == b ? 0 : b == g.K ? (b - o.k0 + ROWB - 1) / ROWB : (b / ROWB * ROWB - o.k0) / ROWB;
         } else if (t >= per) {
             return false;
         }

@@ -43,8 +43,10 @@ gemm_f8_simt_kernel(const GemmF8Params p)
     } else if (p.mode == kExpertDepth) {
         k_lo = min(max(p.starts[e], 0), p.K);
         k_hi = min(max(p.starts[e + 1], k_lo), p.K);
-        k_lo = k_lo / BLK * BLK;
-        if (k_hi != p.K) k_hi = k_hi / BLK * BLK;
+        if (k_lo < k_hi) {                     // an empty segment stays empty where the depth ends inside a block
+            k_lo = k_lo / BLK * BLK;
+            if (k_hi != p.K) k_hi = k_hi / BLK * BLK;
+        }
         crow0 = (int64_t)e * p.M;
     }
     const int n0 = blockIdx.x * TILE;
