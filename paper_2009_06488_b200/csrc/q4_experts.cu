@@ -361,7 +361,8 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
         constexpr int PV = 16 / (int)sizeof(T);
         const int64_t r0 = ((int64_t)blockIdx.x - token_blocks) * 256 + warp * 32;
         const int pair = r0 + lane < p.rows ? p.source[r0 + lane] : 0;
-        for (unsigned none = __ballot_sync(0xFFFFFFFFu, pair < 0); none; none &= none - 1) {
+        const bool absent = r0 + lane < p.rows && (pair < 0 || pair / p.topk >= p.tokens);
+        for (unsigned none = __ballot_sync(0xFFFFFFFFu, absent); none; none &= none - 1) {
             T* const dst = static_cast<T*>(p.out) + (r0 + __ffs(none) - 1) * p.ldo;
             const int head = min((int)(-(uintptr_t)dst & 15) / (int)sizeof(T), p.D), body = (p.D - head) / PV;
             for (int k = lane; k < body; k += 32) __stcs(reinterpret_cast<uint4*>(dst + head) + k, make_uint4(0, 0, 0, 0));

@@ -1,0 +1,57 @@
+"""Pairs and rows that are absent, in the expert layer's gradient.
+
+dw of an absent pair is 0 and a row of no pair gets zeros, whatever the other operands hold.  A product of two
+binary32 values is off by 2^-24 of itself, a sum of D of them by (D + 1) * 2^-24 of their magnitudes; the output's
+type adds half of its last place.
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HALF_ULP = {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def q4():
+    from paper_2009_06488_b200 import binding
+    return binding
+
+
+def types():
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [8, 40, 41, 100, 129, 264, 2048, 2051])
+def test_rows_whose_pair_lies_past_the_end_get_zeros(q4, t, D):
+    import torch
+    tokens, topk = 4, 3
+    pairs = tokens * topk
+    # rows 0, 4 and 5 hold pairs; all others are absent, in one way or another
+    source = np.array([3, pairs, -1, 2 ** 31 - 1, 11, 0, pairs + 1, -2 ** 31] + [pairs] * 40 + [-1], dtype=np.int32)
+    slot = np.full((tokens, topk), -1, dtype=np.int32)
+    slot[1, 0], slot[3, 2], slot[0, 0] = 0, 4, 5
+    slot[2, 1], slot[0, 2] = source.size, 2 ** 31 - 1
+    r = np.random.default_rng(D)
+    w = r.standard_normal((tokens, topk)).astype(np.float32)
+    G, Y = (dev(r.standard_normal((n, D)).astype(np.float32)).to(types()[t]) for n in (tokens, source.size))
+    for weights in (w, None):
+        dY = torch.full((source.size, D), float("nan"), dtype=types()[t], device="cuda")
+        dw = torch.full((tokens, topk), float("nan"), device="cuda")
+        q4.q4_expert_combine_grad(G, Y, dev(slot), None if weights is None else dev(weights), dev(source), dY, dw)
+        want, ww = np.zeros((source.size, D)), np.zeros((tokens, topk))
+        mag = np.zeros((tokens, topk))
+        g, y = G.double().cpu().numpy(), Y.double().cpu().numpy()
+        for row, tok, j in ((0, 1, 0), (4, 3, 2), (5, 0, 0)):
+            want[row] = g[tok] * (1.0 if weights is None else float(weights[tok, j]))
+            ww[tok, j], mag[tok, j] = (g[tok] * y[row]).sum(), np.abs(g[tok] * y[row]).sum()
+        off = np.abs(dY.double().cpu().numpy() - want)
+        assert (off <= np.abs(want) * (2.0 ** -24 + HALF_ULP[t] * (1 + 2.0 ** -24)) + 2.0 ** -25 * (t == "f16")).all()
+        assert (np.abs(dw.double().cpu().numpy() - ww) <= (D + 1) * 2.0 ** -24 * mag).all()
