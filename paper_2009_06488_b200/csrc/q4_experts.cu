@@ -420,6 +420,11 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
                     f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e, tx, TX);
                 }
             }
+            // an absent pair beside a present one of the warp's other tokens: what its dOut times nothing came to
+            // (NaN, if dOut is not finite) does not count
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (!VEC && s[j] < 0) dot[j] = 0.0f;
             if (TX >= 32) {
                 const float sum = reduce8(dot, lane);
                 if (lane < 8) part[warp][lane] = sum;

@@ -55,3 +55,35 @@ def test_rows_whose_pair_lies_past_the_end_get_zeros(q4, t, D):
         off = np.abs(dY.double().cpu().numpy() - want)
         assert (off <= np.abs(want) * (2.0 ** -24 + HALF_ULP[t] * (1 + 2.0 ** -24)) + 2.0 ** -25 * (t == "f16")).all()
         assert (np.abs(dw.double().cpu().numpy() - ww) <= (D + 1) * 2.0 ** -24 * mag).all()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [1, 8, 13, 64, 65, 100, 121, 128, 200, 2048, 2051])
+def test_weight_gradient_of_an_absent_pair_is_zero_beside_infinities(q4, t, D):
+    import torch
+    tokens, topk, rows = 9, 3, 20
+    r = np.random.default_rng(D)
+    # tokens in turn: all pairs absent, none, the first only present, the last only
+    slot = np.full((tokens, topk), -1, dtype=np.int32)
+    at = 0
+    for i in range(tokens):
+        for j in range(topk):
+            if i % 4 == 1 or (i % 4 == 2 and j == 0) or (i % 4 == 3 and j == topk - 1):
+                slot[i, j], at = at, at + 1
+    assert at <= rows
+    source = np.full(rows, -1, dtype=np.int32)
+    source[slot[slot >= 0]] = np.flatnonzero(slot.reshape(-1) >= 0)
+    G = dev(r.standard_normal((tokens, D)).astype(np.float32)).to(types()[t])
+    G[0::4, 0], G[2::4, D - 1], G[3::4, D // 2] = float("inf"), float("nan"), float("-inf")
+    Y = dev(r.standard_normal((rows, D)).astype(np.float32)).to(types()[t])
+    w = dev(np.full((tokens, topk), np.nan, dtype=np.float32))
+    w[dev(slot) >= 0] = 1.0
+    dY, dw = torch.full_like(Y, 7.0), torch.full((tokens, topk), 7.0, device="cuda")
+    q4.q4_expert_combine_grad(G, Y, dev(slot), w, dev(source), dY, dw)
+    dw, dY = dw.cpu().numpy(), dY.cpu()
+    assert (dw[slot < 0] == 0).all()
+    assert np.isfinite(dw[1::4]).all() and not np.isfinite(dw[2::4, 0]).any() and not np.isfinite(dw[3::4, -1]).any()
+    assert (dY[torch.from_numpy(source < 0)] == 0).all()
+    rows_of = slot[slot >= 0]
+    assert torch.equal(dY[torch.from_numpy(rows_of)].nan_to_num(5.0),
+                       G.cpu()[torch.from_numpy(np.flatnonzero(slot.reshape(-1) >= 0) // topk)].nan_to_num(5.0))
