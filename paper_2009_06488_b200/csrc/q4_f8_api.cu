@@ -68,7 +68,7 @@ q4_status q4_f8_quantize(const void* X, int32_t x_type, int64_t ldx, int32_t row
     if (Q && (ldq < cols || lds < (blocks ? f8::blocks_of(cols) : rows))) return Q4_ERR_INVALID_ARG;
     if (Qt && (ldqt < rows || ldst < (blocks ? f8::blocks_of(rows) : cols))) return Q4_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return Q4_OK;
-    if (!X) return Q4_ERR_INVALID_ARG;
+    if (!X && !(source && x_rows == 0)) return Q4_ERR_INVALID_ARG;         // an empty matrix to pick from: every row is absent
     if (!aligned(X, f8::type_size(x_type)) || !aligned(S, 4) || !aligned(St, 4) || !aligned(source, 4))
         return Q4_ERR_ALIGNMENT;
     if (f8::blocks_of(cols) * (((int64_t)rows + 31) / 32) > INT32_MAX) return Q4_ERR_RANGE;

@@ -1,4 +1,4 @@
-"""Pairs and rows that are absent, in the expert layer's gradient.
+"""Pairs and rows that are absent, in the expert layer's gradient and in gathers from no tokens at all.
 
 dw of an absent pair is 0 and a row of no pair gets zeros, whatever the other operands hold.  A product of two
 binary32 values is off by 2^-24 of itself, a sum of D of them by (D + 1) * 2^-24 of their magnitudes; the output's
@@ -87,3 +87,24 @@ def test_weight_gradient_of_an_absent_pair_is_zero_beside_infinities(q4, t, D):
     rows_of = slot[slot >= 0]
     assert torch.equal(dY[torch.from_numpy(rows_of)].nan_to_num(5.0),
                        G.cpu()[torch.from_numpy(np.flatnonzero(slot.reshape(-1) >= 0) // topk)].nan_to_num(5.0))
+
+
+@pytest.mark.parametrize("blocks", [False, True])
+def test_rows_picked_from_no_tokens_are_zeros(q4, blocks):
+    """Every entry of source is past the end of an empty matrix: absent, as with any other."""
+    import torch
+    X = torch.empty(0, 200, dtype=torch.bfloat16, device="cuda")
+    source = torch.tensor([-1, 0, 5], dtype=torch.int32, device="cuda")
+    Q, Qt = torch.full((3, 200), 9, dtype=torch.uint8, device="cuda"), torch.full((200, 3), 9, dtype=torch.uint8, device="cuda")
+    S = torch.full((1, 2) if blocks else (2, 3), -1.0, device="cuda")
+    St = torch.full((2, 1) if blocks else (1, 200), -1.0, device="cuda")
+    q4.q4_f8_quantize(X, Q, S, Qt, St, blocks=blocks, source=source)
+    least = np.float32(2.0 ** -60) / np.float32(448)
+    assert (Q == 0).all() and (Qt == 0).all()
+    assert (S.cpu().numpy() == least).all() and (St.cpu().numpy() == least).all()
+    Xs = torch.full((3, 200), 7.0, dtype=torch.bfloat16, device="cuda")
+    q4.q4_expert_gather(X, source, 1, Xs)
+    assert (Xs == 0).all()
+    # a matrix that has rows has to be given
+    assert q4._lib.q4_f8_quantize(None, q4.Q4_BF16, 200, 3, 200, source.data_ptr(), 1, 1, int(blocks), Q.data_ptr(), 200,
+                                  S.data_ptr(), S.shape[1], None, 0, None, 0, None) == q4.Q4_ERR_INVALID_ARG
