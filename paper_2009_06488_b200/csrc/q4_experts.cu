@@ -476,8 +476,18 @@ cudaError_t launch_expert_sort(const int32_t* ids, int32_t n, int32_t E, int32_t
     const int64_t chunk = ((int64_t)n + g - 1) / g;
     const size_t smem = (size_t)PlaceLayout(E).all * 4;
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
+        // the limit belongs to the device, not to the call: set once, to the most experts' size, so that a call of fewer
+        // on another host thread does not lower it between this one's setting and its launch
+        static bool ready[64] = {};
+        int dev = 0;
+        const cudaError_t at = cudaGetDevice(&dev);
+        if (at != cudaSuccess) return at;
+        if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+        if (!ready[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PlaceLayout(Q4_MAX_EXPERTS).all * 4);
+            if (e != cudaSuccess) return e;
+            ready[dev] = true;
+        }
     }
     int32_t* hist = static_cast<int32_t*>(ws);
     if (g > 1) {
