@@ -290,8 +290,9 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     cluster_sync_all();              // barriers of all CTAs are initialised past this point
     tc_fence_after();
     const uint32_t tmem_base = (uint32_t)lds32(tmem_slot);
-    // Before a warp's first access to global memory.  What does not need any comes before it: it overlaps the end of the
-    // kernel before, the places of a dense product's first tile with it.
+    // Every warp of the roles below waits for the kernel before ahead of its first access to global memory and of its first
+    // bounded wait: what another warp does only behind it may take as long as that kernel runs.  What needs neither comes
+    // first and overlaps its end, the places of a dense product's first tile with it.
     const bool dense = g.mode == kDense;
 
     // the share of a tile's depth blocks that this pair sums
@@ -360,6 +361,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             uint32_t st = 0, ph = 0, u = 0;
             Tile next;
             bool more = walk.get(cluster_id, next);
+            if (dense) wait_for_predecessor();
             for (int tile = cluster_id; more;) {
                 t = next;
                 share(t);
@@ -420,6 +422,7 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             }
             __syncwarp();
             if (last) break;
+            if (dense && tile == cluster_id) wait_for_predecessor();
             if (++ti == TI_RING) { ti = 0; ph ^= 1u; }
         }
         __syncwarp();
