@@ -279,7 +279,10 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 r[4 * qd + 3] += rowterm + ct.w;
             }
         }
-        if (!REQUANT && p.c_tma) {
+        // A TMA store clips rows exactly and columns in pieces of 16 bytes: the last chunk of a
+        // ragged width would write up to three values behind N, inside the pitch or past the end
+        const bool by_tma = !REQUANT && p.c_tma && (nc + 32 <= g.N || g.N % 4 == 0);
+        if (by_tma) {
             // int32 tile out through shared memory and one TMA store per warp: my
             // row's 128 bytes go to the swizzled staging slice of my warp; rows and
             // columns past M / N are clipped by the tensor map
@@ -297,7 +300,11 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 tma_store_2d(&tmC, slice, nc, tm * 256 + (int)rank * TMC + lg * 32);
                 bulk_commit();
             }
-        } else if (m < g.M) {
+            return;
+        }
+        // (an empty group in the place of the chunk's store: the slices' waits count groups)
+        if (!REQUANT && p.c_tma && lane == 0) bulk_commit();
+        if (m < g.M) {
             const bool full = (nc + 32 <= g.N);
             if (!REQUANT) {
                 int32_t* dst = g.C + (int64_t)m * g.ldc + nc;

@@ -435,9 +435,10 @@ gemm_u8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     r[4 * qd + 2] += rowterm + ct.z;
                     r[4 * qd + 3] += rowterm + ct.w;
                 }
-                if (p.c_tma) {
+                if (p.c_tma && (nc + 32 <= g.N || g.N % 4 == 0)) {
                     // my row's 128 bytes go to the swizzled staging slice of my warp; rows and
-                    // columns past M / N are clipped by the tensor map
+                    // columns past M / N are clipped by the tensor map (columns in pieces of 16
+                    // bytes: the last chunk of a ragged width goes out by values)
                     const uint32_t slice = sbase + OFF_STG + (uint32_t)(lg * 4096);
                     if (lane == 0) bulk_wait_read();       // the previous store has read the slice
                     __syncwarp();
