@@ -25,7 +25,31 @@ if not os.path.exists(LIB_PATH):
         "(python -m paper_2009_06488_b200.build); there is no CPU fallback")
 
 _lib = ctypes.CDLL(LIB_PATH)
-from . import _q4_torch as _t  # noqa: E402  (links to the library just loaded)
+
+
+def _marshalling():
+    """The C++ module that hands torch tensors to the e4m3 and expert-layer calls."""
+    try:
+        from . import _q4_torch as m          # links to the library just loaded
+    except ImportError as e:
+        raise ImportError("_q4_torch, which the e4m3 and expert-layer calls go through, cannot be loaded "
+                          f"({e}): build it with python -m paper_2009_06488_b200.build") from e
+    if m.built_for != torch.__version__:
+        raise ImportError(f"_q4_torch was built for torch {m.built_for}, this is {torch.__version__}: "
+                          "build it again with python -m paper_2009_06488_b200.build")
+    return m
+
+
+class _Late:
+    """Stands for the module until the first of its calls is made: the other calls need nothing of it."""
+
+    def __getattr__(self, name):
+        global _t
+        _t = _marshalling()
+        return getattr(_t, name)
+
+
+_t = _Late()
 
 (Q4_OK, Q4_ERR_INVALID_ARG, Q4_ERR_ALIGNMENT, Q4_ERR_RANGE, Q4_ERR_WORKSPACE,
  Q4_ERR_UNSUPPORTED, Q4_ERR_CUDA, Q4_ERR_DEVICE_TIMEOUT, Q4_ERR_STATIC_SCRATCH, Q4_ERR_WEIGHT_IMAGE) = range(10)

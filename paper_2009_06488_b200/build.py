@@ -21,6 +21,7 @@ TORCH_LIB = os.path.join(HERE, "_q4_torch.so")      # tensors to the C ABI; link
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-cudart", "static"]
 OBJ_DIR = os.path.join(HERE, "_build")
+TORCH_STAMP = os.path.join(OBJ_DIR, "q4_torch.built_for")      # torch and Python that the module was built for
 
 
 def sources() -> list[str]:
@@ -62,10 +63,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *objs])
         os.replace(tmp, LIB)
-    if force or not os.path.exists(TORCH_LIB) or \
+    if force or not os.path.exists(TORCH_LIB) or _stamp() != _torch_and_python() or \
             os.path.getmtime(TORCH_LIB) < max(os.path.getmtime(TORCH_SRC), os.path.getmtime(os.path.join(INCLUDE, "q4.h"))):
         build_torch()
     return LIB
+
+
+def _torch_and_python() -> str:
+    import torch
+    return f"{torch.__version__} {sys.implementation.cache_tag}"
+
+
+def _stamp() -> str:
+    try:
+        with open(TORCH_STAMP) as f:
+            return f.read()
+    except OSError:
+        return ""
 
 
 def build_torch() -> None:
@@ -77,12 +91,16 @@ def build_torch() -> None:
     tmp = TORCH_LIB + f".tmp{os.getpid()}"
     subprocess.check_call(
         ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         f'-DQ4_TORCH_VERSION="{torch.__version__}"',
          "-I", INCLUDE, "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
          "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
          "-isystem", os.environ.get("CUDA_HOME", "/usr/local/cuda") + "/include", "-o", tmp, TORCH_SRC,
          "-L", HERE, "-l:libq4.so", "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
          "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, TORCH_LIB)
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    with open(TORCH_STAMP, "w") as f:
+        f.write(_torch_and_python())
 
 
 if __name__ == "__main__":

@@ -286,4 +286,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q4_torch", nullptr, -1, methods, 
 
 }  // namespace
 
-extern "C" PyObject* PyInit__q4_torch(void) { return PyModule_Create(&module); }
+extern "C" PyObject* PyInit__q4_torch(void)
+{
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", Q4_TORCH_VERSION) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
