@@ -12,6 +12,8 @@
 // Rows: a row's D values are spread over up to 256 threads, 8 (16 bytes of a 16-bit type) each; a token's
 // topk rows are loaded before they are summed, in order and in binary32.  Bound: HBM; issue for rows that do not begin on
 // multiples of 16 bytes, which are read and written in aligned pieces (q4_f8.cuh).
+#include <type_traits>
+
 #include "q4_f8.cuh"
 
 namespace q4 {
@@ -349,7 +351,8 @@ __device__ __forceinline__ float reduce8(float (&d)[8], int lane)
 // By tokens: a token's gradient is read once, its rows wherever they lie.  (By rows of the experts' side, read and
 // written front to back with the gradients from L2, 4096 x 8 x 2048 takes 68 us instead of 60: the streams push the
 // gradients out of L2.  Rows that happen to lie in token order take 48: the rest is the scattered writes.)
-template <int TYPE, bool VEC>
+// SPREAD (unaligned rows): a token's pairs are shared by as many blocks as have two of them each.
+template <int TYPE, bool VEC, bool SPREAD>
 __global__ void __launch_bounds__(256, VEC && TYPE == Q4_F32 ? 2 : 3)
 combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
 {
@@ -372,16 +375,14 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
         return;
     }
     // Rows in flight.  Unaligned: two with three blocks per SM 121 us for 4096 x 8 x 2047 (four and two 143, one and four 184;
-    // aligned rows 59) while one block took all of a token's pairs: issue binds, a row's cut and put-together pieces are
-    // three times an aligned one's instructions.  Its pairs over several blocks 132, but 6 x 8 x 101 3.4 instead of 11.0
-    // and 64 x 8 x 2047 4.7 instead of 8.6.
+    // aligned rows 59): issue binds, a row's cut and put-together pieces are three times an aligned one's instructions.
     constexpr int J = VEC ? 8 : kUnaligned;
     __shared__ float part[8][8];
     const int TX = 1 << tx_bits, tx = threadIdx.x & (TX - 1), TY = 256 >> tx_bits, ty = threadIdx.x >> tx_bits;
-    // a block walks groups of TY tokens (unaligned: J pairs of each, other blocks the others); the next group's pairs are
+    // a block walks groups of TY tokens (SPREAD: J pairs of each, other blocks the others); the next group's pairs are
     // loaded before this one's rows
-    const int parts = VEC ? 1 : (p.topk + J - 1) / J;
-    const int from = VEC ? 0 : (int)blockIdx.x % parts * J, to = VEC ? p.topk : min(p.topk, from + J);
+    const int parts = SPREAD ? (p.topk + J - 1) / J : 1;
+    const int from = SPREAD ? (int)blockIdx.x % parts * J : 0, to = SPREAD ? min(p.topk, from + J) : p.topk;
     int64_t t = (int64_t)(blockIdx.x / (unsigned)parts) * TY + ty;
     const int64_t step = (int64_t)(token_blocks / parts) * TY;
     Pair ahead = pair_of<J>(p, t, t < p.tokens, from, lane);
@@ -393,33 +394,45 @@ combine_grad_kernel(const ExpertRowsParams p, int tx_bits, int token_blocks)
             int s[J];
             float w[J], dot[8] = {};
             spread(p, ahead, lane, s, w);
-            ahead = j0 + J < to ? pair_of<J>(p, t, mine, j0 + J, lane) : pair_of<J>(p, t + step, t + step < p.tokens, from, lane);
-            // (rows of any alignment: whole warps go on together)
-            for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
-                const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
-                f8::Coming<VEC, T> dc;
-                dc.load(g + c, n, f8::careful_at(t, p.tokens, c, left, p.D));
-                f8::Coming<VEC, T> yc[J];
+            const bool more = !SPREAD && j0 + J < to;
+            const int64_t t_next = more ? t : t + step;
+            ahead = pair_of<J>(p, t_next, t_next < p.tokens, more ? j0 + J : from, lane);
+            auto columns = [&](auto careful) {
+                constexpr bool CAREFUL = decltype(careful)::value;
+                // (rows of any alignment: whole warps go on together)
+                for (int c = tx * 8; VEC ? mine && c < p.D : c - tx * 8 < p.D; c += TX * 8) {
+                    const int left = VEC || mine ? p.D - c : 0, n = VEC ? left : max(0, min(8, left));
+                    f8::Coming<VEC, T> dc;
+                    dc.load(g + c, n, CAREFUL && f8::careful_at(t, p.tokens, c, left, p.D));
+                    f8::Coming<VEC, T> yc[J];
 #pragma unroll
-                for (int j = 0; j < J; ++j)
-                    yc[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0,
-                               f8::careful_at(s[j], p.rows, c, left, p.D));
-                const Eight<T> d = dc.get(g + c, n);
+                    for (int j = 0; j < J; ++j)
+                        yc[j].load(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), s[j] >= 0 ? n : 0,
+                                   CAREFUL && f8::careful_at(s[j], p.rows, c, left, p.D));
+                    const Eight<T> d = dc.template get<CAREFUL>(g + c, n);
 #pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
-                    const Eight<T> y = yc[j].get(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), VEC || s[j] >= 0 ? n : 0);
-                    float o[8];
+                    for (int j = 0; j < J; ++j) {
+                        if (VEC ? s[j] < 0 : __all_sync(0xFFFFFFFFu, s[j] < 0)) continue;
+                        const Eight<T> y = yc[j].template get<CAREFUL>(static_cast<const T*>(p.Y) + (s[j] >= 0 ? s[j] * p.ldy + c : 0), VEC || s[j] >= 0 ? n : 0);
+                        float o[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dot[j] = fmaf(d.get(i), y.get(i), dot[j]);
-                        o[i] = w[j] * d.get(i);
+                        for (int i = 0; i < 8; ++i) {
+                            dot[j] = fmaf(d.get(i), y.get(i), dot[j]);
+                            o[i] = w[j] * d.get(i);
+                        }
+                        Eight<T> e;
+                        f8::pack8(e, o);
+                        f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e, tx, TX);
                     }
-                    Eight<T> e;
-                    f8::pack8(e, o);
-                    f8::store8<VEC>(static_cast<T*>(p.out) + (VEC || s[j] >= 0 ? s[j] * p.ldo + c : 0), VEC || s[j] >= 0 ? left : 0, e, tx, TX);
                 }
-            }
+            };
+            // Many unaligned tokens: rows without careful values go through code without the call that reads them, whose
+            // place among the rows in flight costs registers (132 us with it, 121 without)
+            bool edge = VEC || SPREAD || t == 0 || t == p.tokens - 1 || p.D < 16;
+#pragma unroll
+            for (int j = 0; j < J; ++j) edge = edge || s[j] == 0 || s[j] == p.rows - 1;
+            if (VEC || SPREAD || __any_sync(0xFFFFFFFFu, edge)) columns(std::true_type{});
+            else columns(std::false_type{});
             // an absent pair beside a present one of the warp's other tokens: what its dOut times nothing came to
             // (NaN, if dOut is not finite) does not count
 #pragma unroll
@@ -520,10 +533,19 @@ cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t s
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const int64_t groups = ((int64_t)p.tokens + ty - 1) / ty;
-    const int parts = p.vec ? 1 : (p.topk + kUnaligned - 1) / kUnaligned, most = 3 * 148 > parts ? 3 * 148 / parts : 1;
-    const int tb = (int)(groups < most ? groups : most) * parts;         // resident at once
+    const int resident = 3 * 148;
+    // Unaligned rows: a token's pairs over several blocks while the tokens alone do not keep the blocks evenly busy.  From five
+    // rounds on the gradients that such blocks read again, and the calls for their edges, cost more: with and without,
+    // 6 x 8 x 101 3.4 and 9.5 us, 600 x 8 x 2047 21.6 and 27.7, 2048 x 8 x 2047 64 and 67, 2220 x 8 x 2047 70 and 68, 4096 x 8 x 2047
+    // 127 and 121, 8192 x 8 x 2047 251 and 238; float32 4096 x 8 x 2047 155 and 145.
+    const bool spread = !p.vec && groups < 5 * resident;
+    const int parts = spread ? (p.topk + kUnaligned - 1) / kUnaligned : 1, most = resident > parts ? resident / parts : 1;
+    const int tb = (int)(groups < most ? groups : most) * parts;
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
-    return Q4_ROWS_LAUNCH(combine_grad_kernel, grid, p, b, tb);
+    const auto run = [&](auto aligned, auto shared, auto whole) { return f8::launch(p.vec ? aligned : spread ? shared : whole, grid, 256, 0, st, p, b, tb); };
+    if (p.type == Q4_F32) return run(combine_grad_kernel<Q4_F32, true, false>, combine_grad_kernel<Q4_F32, false, true>, combine_grad_kernel<Q4_F32, false, false>);
+    if (p.type == Q4_BF16) return run(combine_grad_kernel<Q4_BF16, true, false>, combine_grad_kernel<Q4_BF16, false, true>, combine_grad_kernel<Q4_BF16, false, false>);
+    return run(combine_grad_kernel<Q4_F16, true, false>, combine_grad_kernel<Q4_F16, false, true>, combine_grad_kernel<Q4_F16, false, false>);
 }
 
 }  // namespace q4

@@ -121,7 +121,7 @@ template <typename T> struct Coming<true, T> {
                              : "l"(reinterpret_cast<const uint4*>(p) + k));
         }
     }
-    __device__ __forceinline__ const Eight<T>& get(const T*, int) { return e; }
+    template <bool CAREFUL = true> __device__ __forceinline__ const Eight<T>& get(const T*, int) { return e; }
 };
 template <typename T> struct Coming<false, T> {
     static constexpr int G = Eight<T>::NW / 4 + 1;
@@ -140,10 +140,11 @@ template <typename T> struct Coming<false, T> {
         }
         if (careful && n > 0) off += 16;
     }
-    __device__ __forceinline__ Eight<T> get(const T* p, int n)
+    // CAREFUL = false: load() was given no `careful` values.
+    template <bool CAREFUL = true> __device__ __forceinline__ Eight<T> get(const T* p, int n)
     {
         Eight<T> e;
-        if (off > 15) {                            // here, not in load(): a call there would hold up the loads behind it
+        if (CAREFUL && off > 15) {                 // here, not in load(): a call there would hold up the loads behind it
 #pragma unroll
             for (int k = 0; k < G; ++k)
                 if (n > 0) g[k] = piece_by_values<T>(((uintptr_t)p & ~(uintptr_t)15) + 16 * k, (uintptr_t)p, (uintptr_t)(p + n));
