@@ -533,13 +533,16 @@ cudaError_t launch_expert_combine_grad(const ExpertRowsParams& p, cudaStream_t s
 {
     const int b = tx_bits_of(p.D), ty = 256 >> b;
     const int64_t groups = ((int64_t)p.tokens + ty - 1) / ty;
-    const int resident = 3 * 148;
+    // Blocks that walk the tokens: three per SM, as many as are resident; of aligned float32 rows (128 registers) two are, and
+    // four take two rounds whose second evens out the first's ends (two, three and four: 4096 x 8 x 2048 94, 111 and 94 us,
+    // 1000 x 8 x 2048 28.4, 29.2 and 27.7; bfloat16 4096 x 8 x 2048 56, 48 and 56).
+    const int blocks = 2 * f8_pairs_of_device() * (p.vec && p.type == Q4_F32 ? 4 : 3);
     // Unaligned rows: a token's pairs over several blocks while the tokens alone do not keep the blocks evenly busy.  From five
     // rounds on the gradients that such blocks read again, and the calls for their edges, cost more: with and without,
     // 6 x 8 x 101 3.4 and 9.5 us, 600 x 8 x 2047 21.6 and 27.7, 2048 x 8 x 2047 64 and 67, 2220 x 8 x 2047 70 and 68, 4096 x 8 x 2047
     // 127 and 121, 8192 x 8 x 2047 251 and 238; float32 4096 x 8 x 2047 155 and 145.
-    const bool spread = !p.vec && groups < 5 * resident;
-    const int parts = spread ? (p.topk + kUnaligned - 1) / kUnaligned : 1, most = resident > parts ? resident / parts : 1;
+    const bool spread = !p.vec && groups < 5 * blocks;
+    const int parts = spread ? (p.topk + kUnaligned - 1) / kUnaligned : 1, most = blocks > parts ? blocks / parts : 1;
     const int tb = (int)(groups < most ? groups : most) * parts;
     const unsigned grid = (unsigned)(tb + ((int64_t)p.rows + 255) / 256);
     const auto run = [&](auto aligned, auto shared, auto whole) { return f8::launch(p.vec ? aligned : spread ? shared : whole, grid, 256, 0, st, p, b, tb); };
