@@ -282,6 +282,9 @@ using namespace f8;
 // rows 34 against 43 us on the pair kernel, 1024 rows 55 against 43); one product up to 16 rows (4096 x 4096: 6.6
 // against 10.7 us), and up to 32 while its tiles go round the SMs twice at most (4096 x 4096 8.2 against 11.6 us,
 // 16384 x 4096 26 against 22 us): beyond, the warp-level matrix instructions bind.
+// By experts the rule knows the rows of A's buffer, not the segments, which are on the device.  Where they are not alike, it
+// can choose the slower kernel: 512 rows all at one of 64 experts take 19 us here, 8 on the pair kernel (64 rows 4.8 and
+// 7.3); a buffer of more rows than its segments hold goes to the pair kernel (a serving sort leaves none: align = 1).
 bool gemm_f8_few_supported(const GemmF8Params& g)
 {
     if ((uintptr_t)g.A % 16 || (uintptr_t)g.Bt % 16 || g.lda % 16 || g.ldb % 16) return false;
