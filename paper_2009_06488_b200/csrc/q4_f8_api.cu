@@ -192,7 +192,8 @@ q4_status q4_expert_combine_grad(const void* dOut, int64_t ldd, const void* Y, i
     if (s != Q4_OK) return s;
     if (ldd < D || ldy < D || lddy < D) return Q4_ERR_INVALID_ARG;
     if (tokens == 0 && (rows == 0 || D == 0)) return Q4_OK;
-    if ((rows > 0 && (!Y || !dY || !source)) || (tokens > 0 && (!dOut || !slot || !dw))) return Q4_ERR_INVALID_ARG;
+    // (rows of no values have no address; dw is 0 for every pair then)
+    if ((rows > 0 && ((D > 0 && (!Y || !dY)) || !source)) || (tokens > 0 && ((D > 0 && !dOut) || !slot || !dw))) return Q4_ERR_INVALID_ARG;
     const size_t z = f8::type_size(type);
     if (!aligned(dOut, z) || !aligned(Y, z) || !aligned(dY, z) || !aligned(slot, 4) || !aligned(source, 4) ||
         !aligned(w, 4) || !aligned(dw, 4)) return Q4_ERR_ALIGNMENT;

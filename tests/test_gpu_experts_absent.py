@@ -108,3 +108,24 @@ def test_rows_picked_from_no_tokens_are_zeros(q4, blocks):
     # a matrix that has rows has to be given
     assert q4._lib.q4_f8_quantize(None, q4.Q4_BF16, 200, 3, 200, source.data_ptr(), 1, 1, int(blocks), Q.data_ptr(), 200,
                                   S.data_ptr(), S.shape[1], None, 0, None, 0, None) == q4.Q4_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [0, 40, 41])
+def test_gradient_without_tokens_rows_or_values(q4, t, D):
+    import torch
+    new = lambda n: torch.full((n, D), 7.0, dtype=types()[t], device="cuda")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    dY, none = new(5), torch.empty(0, 2, device="cuda")
+    q4.q4_expert_combine_grad(new(0), new(5), none.int(), None, i32([-1, 0, 3, 9, -5]), dY, none)
+    assert (dY == 0).all()
+    dw = torch.full((3, 2), 7.0, device="cuda")
+    q4.q4_expert_combine_grad(new(3), new(0), i32([[0, -1], [3, 4], [-1, 7]]), None, i32([]), new(0), dw)
+    assert (dw == 0).all()
+    dw.fill_(7.0)
+    dY = new(2)
+    q4.q4_expert_combine_grad(new(3), new(2), i32([[0, -1], [-1, 1], [-1, -1]]), None, i32([0, 3]), dY, dw)
+    assert (dY == 7).all()
+    want = torch.zeros(3, 2)
+    want[0, 0] = want[1, 1] = 49.0 * D
+    assert torch.equal(dw.cpu(), want)
