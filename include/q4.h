@@ -98,7 +98,8 @@ typedef struct {
  *   C[m][n] = sum_k (a(m,k) - za) * (b(k,n) - zb)
  *           = sum_k a b  -  zb * rowsum_a[m]  -  za * colsum_b[n]  +  K * za * zb.
  * A [M x K] pitch lda bytes; Bt [N x K] pitch ldb bytes; C [M x N] int32, pitch ldc
- * elements (>= N).  za, zb in 0..15.  1 <= K <= Q4_MAX_K.  M or N = 0 is a no-op.
+ * elements (>= N; what lies between N and ldc is not written).  za, zb in 0..15.
+ * 1 <= K <= Q4_MAX_K.  M or N = 0 is a no-op.
  * rowsum_a [M] / colsum_b [N]: optional precomputed sums (e.g. from q4_im2col, or
  * computed once for the weights); NULL = computed inside the kernel.
  * ws / ws_bytes: optional workspace of at least q4_gemm_workspace_bytes(M, N, K) bytes,
