@@ -209,7 +209,7 @@ def _codes(x, by16, factor):
     a = v.abs().amax(2)
     if by16:
         r = torch.ones_like(factor) / factor
-        s = ((a / torch.full_like(a, 6.0)) * r).clamp(max=448).to(torch.float8_e4m3fn).float().clamp(min=2.0 ** -9)
+        s = (a * (r / torch.full_like(r, 6.0))).clamp(max=448).to(torch.float8_e4m3fn).float().clamp(min=2.0 ** -9)
         inv, byte = r / s, s.to(torch.float8_e4m3fn).view(torch.uint8)
     else:
         s = a.clamp(min=FLOOR) / torch.full_like(a, 6.0)
@@ -328,7 +328,7 @@ def _round_trip_64(x, by16, factor):
         a = part.abs().amax(1, keepdim=True)
         if by16:
             r = _f32(1 / factor.double())
-            s = _e4m3_64(_f32(_f32(a / 6) * r))
+            s = _e4m3_64(_f32(a * _f32(r / 6)))
             y[:, c:c + grp] = _e2m1_64(_f32(part * _f32(r / s))) * s * factor.double()
         else:
             m, e = torch.frexp(_f32(a.clamp(min=FLOOR) / 6))
