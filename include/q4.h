@@ -475,6 +475,89 @@ q4_status q4_expert_combine_grad(const void* dOut, int64_t ldd, const void* Y, i
                                  int32_t tokens, int32_t topk, void* dY, int64_t lddy, float* dw, void* stream);
 
 /*
+ * 4-bit floating point with microscales.  Extension of the paper's 4-bit values (Section II-A: one scale per
+ * matrix) to the operands that language models are served with on this hardware.
+ *
+ * Codes are e2m1 (sign, 2 exponent bits with bias 1, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two per byte,
+ * low half = even column, an odd row's last high half 0.  x ~= factor * scale * code:
+ *   by default    a scale per 32 columns of a row, a power of two: one byte b, 2^(b - 127), 255 = NaN;
+ *   Q4_F4_BY16    a scale per 16 columns, e4m3 (one byte, bit 7 ignored, 0x7F = NaN).
+ * The scales of four neighbouring groups make a 32-bit word, the first in its low byte; words are stored
+ * S[word][row], word = column / 128 (Q4_F4_BY16: column / 64), pitch in words >= rows.  Bytes of groups
+ * behind the last column are written as 0 and ignored when read.  factor: one float32 on the device per matrix (by experts:
+ * per expert), NULL = 1.
+ * Sums are float32.  Everything below is asynchronous on `stream`, allocates nothing and checks its host-side arguments
+ * before anything is launched; numbers that live on the device (starts, source, ids) are bounds-checked by the kernels,
+ * what lies outside its range is treated as absent.  Rows of float values may begin at any element (multiples of
+ * 16 bytes are fastest).  Bytes between a matrix's rows may be read and are ignored; they are never written.
+ */
+#define Q4_F4_BY16  1    /* a scale per 16 columns (e4m3) instead of one per 32 (power of two)                 */
+#define Q4_F4_GATED 2    /* q4_expert_layer_f4: W1 holds H gate rows and then H rows that they are multiplied with */
+
+/*
+ * Codes and scales of a matrix X [rows x cols] (x_type a q4_type, pitch ldx elements), a = max |x| over a group:
+ *   by default    s = the smallest power of two that is not below max(a, 2^-60) / 6,  code = e2m1(x / s);
+ *   Q4_F4_BY16    r = 1 / factor, s = max(e4m3(a * (r / 6)), 2^-9),  code = e2m1(x * (r / s)).
+ * All steps are float32; e2m1() and e4m3() round to nearest even and saturate.  factor (Q4_F4_BY16 only, else NULL) is
+ * positive; max |X| / 2688 puts the largest scale at e4m3's largest value.
+ * Q [rows][ldq bytes], S: the codes and their scales.  Qt [cols][ldqt bytes], St: the same of X transposed (its groups
+ * run along the rows of X), taken from the same read.  Either pair may be NULL, not both.
+ * source, topk, x_rows: as in q4_f8_quantize.  A group that holds a NaN or an infinity gets the scale NaN and
+ * unspecified codes.
+ */
+q4_status q4_f4_quantize(const void* X, int32_t x_type, int64_t ldx, int32_t rows, int32_t cols,
+                         const int32_t* source, int32_t topk, int32_t x_rows, int32_t flags, const float* factor,
+                         uint8_t* Q, int64_t ldq, uint32_t* S, int64_t lds,
+                         uint8_t* Qt, int64_t ldqt, uint32_t* St, int64_t ldst, void* stream);
+
+/* Y[r][c] = factor * (scale * code): read-back into y_type, pitch ldy elements, rounded once. */
+q4_status q4_f4_dequantize(const uint8_t* Q, int64_t ldq, const uint32_t* S, int64_t lds, int32_t rows, int32_t cols,
+                           int32_t flags, const float* factor, void* Y, int32_t y_type, int64_t ldy, void* stream);
+
+/*
+ * Product of such operands, both scaled along the depth:
+ *   C[m][n] = FA * FB * sum_g SA[m][g] * SB[n][g] * sum_{k in group g} A[m][k] * Bt[n][k]
+ * A [M][lda bytes], Bt [N][ldb bytes], C [M x N] of c_type (a q4_type), pitch ldc elements, rounded once.
+ * Forward: A = input, Bt = weights [out][in].  Gradient of the input: A = the output's gradient, Bt = the transposed
+ * weights (Qt, St of q4_f4_quantize).  Gradient of the weights: both operands transposed, depth = tokens.
+ * Fast path: A, Bt 16-byte aligned and lda, ldb multiples of 16; anything else runs a slower general kernel.
+ */
+q4_status q4_gemm_f4(const uint8_t* A, int64_t lda, const uint32_t* SA, int64_t ldsa,
+                     const uint8_t* Bt, int64_t ldb, const uint32_t* SB, int64_t ldsb, int32_t flags,
+                     const float* FA, const float* FB,
+                     void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K, void* stream);
+
+/*
+ * The product by experts: rows starts[e] .. starts[e + 1] of A and C (starts: device, E + 1 non-decreasing values of
+ * 0 .. M) are multiplied with expert e's weights, rows e * N .. of Bt [E * N][ldb], whose words of scales are at the same
+ * rows of SB, its factor FB[e].  Rows of C outside every segment are left untouched; experts without rows cost nothing.
+ * E <= Q4_MAX_EXPERTS.
+ */
+q4_status q4_gemm_f4_experts(const uint8_t* A, int64_t lda, const uint32_t* SA, int64_t ldsa,
+                             const uint8_t* Bt, int64_t ldb, const uint32_t* SB, int64_t ldsb, int32_t flags,
+                             const float* FA, const float* FB, const int32_t* starts, int32_t E,
+                             void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K, void* stream);
+
+/*
+ * The whole expert layer for a few tokens, in two kernels and without quantizing the activations:
+ *   Out[t] = sum_j w[t][j] * W2_e h,   h = silu(G_e X[t])              or, with Q4_F4_GATED,
+ *                                      h = silu(G_e X[t]) * (U_e X[t]),   e = ids[t][j]
+ * X, Out [tokens x D] of type (a q4_type); ids [tokens][topk]: a number outside 0 .. E - 1 leaves the pair out; w
+ * [tokens][topk] float32 or NULL (= 1).  W1 [E * H][ldw1] codes of G (gated: [E * 2 H], an expert's H rows of G, then its
+ * H rows of U), W2 [E * D][ldw2]; scales at the same rows of S1, S2; F1, F2: a factor per expert or NULL.
+ * Only the weights of experts that ids names are read.
+ * ws: q4_expert_layer_f4_workspace_bytes(tokens, topk, D, H) bytes, 256-byte aligned, not shared by calls that may run
+ * at the same time (captured graphs among them).  The same inputs give the same bits.  Meant for up to a few dozen
+ * tokens: many are served by q4_expert_sort and the products by experts.
+ */
+q4_status q4_expert_layer_f4(const void* X, int64_t ldx, int32_t type, int32_t tokens, int32_t D, int32_t H,
+                             const int32_t* ids, const float* w, int32_t topk, int32_t E, int32_t flags,
+                             const uint8_t* W1, int64_t ldw1, const uint32_t* S1, int64_t lds1, const float* F1,
+                             const uint8_t* W2, int64_t ldw2, const uint32_t* S2, int64_t lds2, const float* F2,
+                             void* Out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+size_t    q4_expert_layer_f4_workspace_bytes(int32_t tokens, int32_t topk, int32_t D, int32_t H);
+
+/*
  * q4_gemm with HOST operands: copies A and Bt to the device, runs q4_gemm and
  * copies C back, then synchronizes `stream`.  The work is ordered behind `stream`
  * and goes in row slices over `stream` and one stream of the library's own (created

@@ -66,10 +66,13 @@ EXPORTS = ["q4_gemm", "q4_gemm_requant", "q4_im2col", "q4_conv2d", "q4_conv2d_st
            "q4_conv2d_prepared",
            "q4_f8_quantize", "q4_gemm_f8", "q4_gemm_f8_experts", "q4_gemm_f8_experts_wgrad", "q4_expert_sort",
            "q4_expert_sort_workspace_bytes", "q4_expert_sort_rows", "q4_expert_gather", "q4_expert_combine",
-           "q4_expert_combine_grad"]
+           "q4_expert_combine_grad",
+           "q4_f4_quantize", "q4_f4_dequantize", "q4_gemm_f4", "q4_gemm_f4_experts", "q4_expert_layer_f4",
+           "q4_expert_layer_f4_workspace_bytes"]
 
 Q4_F32, Q4_BF16, Q4_F16 = range(3)
 Q4_F8_BLOCKS, Q4_F8_POW2, Q4_F8_B_ROWS = 1, 2, 4
+Q4_F4_BY16, Q4_F4_GATED = 1, 2
 Q4_MAX_EXPERTS = 1024
 
 
@@ -189,6 +192,16 @@ _lib.q4_expert_gather.argtypes = [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _i32, 
 _lib.q4_expert_combine.argtypes = [_vp, _i64, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _i64, _vp]
 _lib.q4_expert_combine_grad.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _i64,
                                         _vp, _vp]
+_lib.q4_f4_quantize.argtypes = [_vp, _i32, _i64, _i32, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _i64,
+                                _vp, _i64, _vp, _i64, _vp]
+_lib.q4_f4_dequantize.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _i32, _i64, _vp]
+_lib.q4_gemm_f4.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp]
+_lib.q4_gemm_f4_experts.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i64,
+                                    _i32, _i32, _i32, _vp]
+_lib.q4_expert_layer_f4.argtypes = [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp,
+                                    _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _sz, _vp]
+_lib.q4_expert_layer_f4_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32]
+_lib.q4_expert_layer_f4_workspace_bytes.restype = _sz
 _lib.q4_last_device_status.argtypes = [_vp]
 _lib.q4_set_variant.argtypes = [ctypes.c_int]
 _lib.q4_launch_count.restype = ctypes.c_uint64
@@ -527,6 +540,47 @@ def q4_expert_combine_grad(dOut, Y, slot, w, source, dY, dw):
     """Gradient of q4_expert_combine: dY[slot[t, j]] = w[t, j] * dOut[t] (zeros in rows of no pair) and
     dw[t, j] = <dOut[t], Y[slot[t, j]]>; see include/q4.h."""
     _check(_t.expert_combine_grad(dOut, Y, slot, w, source, dY, dw), "q4_expert_combine_grad")
+
+
+def q4_f4_quantize(X, Q=None, S=None, Qt=None, St=None, by16: bool = False, factor=None, source=None, topk: int = 1):
+    """e2m1 codes (uint8, two per byte) and words of scales (int32 [ceil(cols/128), rows], by16: [ceil(cols/64), rows])
+    of X, straight (Q, S) and/or transposed (Qt, St).  by16: scales per 16 columns in e4m3 times ``factor`` (float32
+    tensor of one element), else per 32 as powers of two.  ``source``, ``topk`` as in q4_f8_quantize; see include/q4.h."""
+    _check(_t.f4_quantize(X, Q, S, Qt, St, source, topk, Q4_F4_BY16 if by16 else 0, factor), "q4_f4_quantize")
+
+
+def q4_f4_dequantize(Q, S, Y, by16: bool = False, factor=None):
+    """Y = factor * scale * code; Y's shape and type (float32, bfloat16, float16) say what is read.  See include/q4.h."""
+    _check(_t.f4_dequantize(Q, S, Y, Q4_F4_BY16 if by16 else 0, factor), "q4_f4_dequantize")
+    return Y
+
+
+def q4_gemm_f4(A, SA, Bt, SB, C, M: int, N: int, K: int, by16: bool = False, FA=None, FB=None):
+    """C = FA FB A Bt^T of e2m1 codes with their scales along the depth; C float32, bfloat16 or float16; FA, FB float32
+    tensors of one element or None.  See include/q4.h."""
+    _check(_t.gemm_f4(A, SA, Bt, SB, C, M, N, K, Q4_F4_BY16 if by16 else 0, FA, FB, None), "q4_gemm_f4")
+    return C
+
+
+def q4_gemm_f4_experts(A, SA, Bt, SB, starts, C, M: int, N: int, K: int, by16: bool = False, FA=None, FB=None):
+    """Rows starts[e] .. starts[e + 1] of A times expert e's weights (rows e * N .. of Bt, words of scales at the same
+    rows of SB, factor FB[e]); rows of C outside every segment stay untouched.  See include/q4.h."""
+    _check(_t.gemm_f4(A, SA, Bt, SB, C, M, N, K, Q4_F4_BY16 if by16 else 0, FA, FB, starts), "q4_gemm_f4_experts")
+    return C
+
+
+def q4_expert_layer_f4_workspace_bytes(tokens: int, topk: int, D: int, H: int) -> int:
+    return int(_lib.q4_expert_layer_f4_workspace_bytes(tokens, topk, D, H))
+
+
+def q4_expert_layer_f4(X, ids, w, W1, S1, W2, S2, Out, E: int, H: int, ws, gated: bool = True, by16: bool = False,
+                       F1=None, F2=None):
+    """Out[t] = sum_j w[t, j] * W2_e h, h = silu(G_e X[t]) * (U_e X[t]) (not gated: silu(G_e X[t])), e = ids[t, j]: the
+    expert layer for a few tokens on 4-bit weights, in two kernels.  W1 [E * 2 H (not gated: E * H), D], W2 [E * D, H]
+    as codes, their scales at the same rows; F1, F2 float32 [E] or None; ws uint8.  See include/q4.h."""
+    _check(_t.expert_layer_f4(X, ids, w, W1, S1, W2, S2, Out, E, H, ws,
+                              (Q4_F4_GATED if gated else 0) | (Q4_F4_BY16 if by16 else 0), F1, F2), "q4_expert_layer_f4")
+    return Out
 
 
 def q4_row_sums(P, rows: int, K: int, sums):

@@ -1,4 +1,4 @@
-// Argument marshalling of the e4m3 and expert-layer calls for torch tensors: checks types, shapes, strides and
+// Argument marshalling of the e4m3, 4-bit float and expert-layer calls for torch tensors: checks types, shapes, strides and
 // devices, takes pointers and pitches, and calls the C ABI on the tensors' device and its current stream.
 // The same in Python took 3 to 4 us of a call whose kernel may take two; this takes about half of one.
 #include <Python.h>
@@ -279,9 +279,133 @@ PyObject* expert_combine_grad(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- 4-bit floats: codes uint8 (two per byte), words of scales int32 [word of columns][row]
+
+int64_t words(int64_t cols, int32_t flags) { return flags & Q4_F4_BY16 ? (cols + 63) / 64 : blocks(cols); }
+
+// Row pitch of codes of rows x cols values, in bytes.
+int64_t code_pitch(const at::Tensor& t, const char* name, int64_t rows, int64_t cols)
+{
+    if (t.scalar_type() != at::kByte) fail(PyExc_TypeError, name, " must be uint8");
+    return pitch(t, name, kCode, rows, (cols + 1) / 2);
+}
+// Pitch of their words of scales.
+int64_t word_pitch(const at::Tensor& t, const char* name, int64_t rows, int64_t cols, int32_t flags)
+{
+    if (t.scalar_type() != at::kInt) fail(PyExc_TypeError, name, " must be int32");
+    const int64_t n = words(cols, flags);
+    if (t.dim() != 2 || t.size(0) < n || t.size(1) < rows) fail(PyExc_ValueError, name, " must be 2-D and at least ", n, " x ", rows);
+    if (t.stride(1) != 1 && t.size(1) > 1) fail(PyExc_ValueError, name, " must have contiguous rows");
+    return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
+}
+uint32_t* word_data(const at::Tensor* t) { return t ? static_cast<uint32_t*>(t->data_ptr()) : nullptr; }
+
+// X, Q, S, Qt, St, source, topk, flags, factor
+PyObject* f4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return entry<9>(a, n, [](PyObject* const* a) {
+        const at::Tensor& X = tensor(a[0], "X");
+        const at::Tensor *Q = optional(a[1], "Q"), *S = optional(a[2], "S"), *Qt = optional(a[3], "Qt"), *St = optional(a[4], "St");
+        const at::Tensor *source = optional(a[5], "source"), *factor = optional(a[8], "factor");
+        const int32_t topk = int32(a[6], "topk"), flags = int32(a[7], "flags");
+        const c10::Device d = device_of(X, Q, S, Qt, St, source, factor);
+        if (!Q != !S || !Qt != !St || (!Q && !Qt))
+            fail(PyExc_ValueError, "codes come with their scales: give Q and S, Qt and St, or both pairs");
+        const int64_t ldx = pitch(X, "X", kReal, 0, 0), x_rows = X.size(0), cols = X.size(1);
+        const int64_t rows = source ? source->numel() : x_rows;
+        int64_t ldq = 0, lds = 0, ldqt = 0, ldst = 0;
+        if (Q) {
+            ldq = code_pitch(*Q, "Q", rows, cols);
+            lds = word_pitch(*S, "S", rows, cols, flags);
+        }
+        if (Qt) {
+            ldqt = code_pitch(*Qt, "Qt", cols, rows);
+            ldst = word_pitch(*St, "St", cols, rows, flags);
+        }
+        const int32_t* src = flat(source, "source", at::kInt, rows);
+        const float* f = flat<float>(factor, "factor", at::kFloat, 1);
+        return on(d, [&](void* st) {
+            return q4_f4_quantize(X.data_ptr(), type_of(X), ldx, int32(rows, "rows"), int32(cols, "cols"), src, topk,
+                                  int32(x_rows, "rows of X"), flags, f, bytes(Q), ldq, word_data(S), lds, bytes(Qt), ldqt, word_data(St),
+                                  ldst, st);
+        });
+    });
+}
+
+// Q, S, Y, flags, factor
+PyObject* f4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return entry<5>(a, n, [](PyObject* const* a) {
+        const at::Tensor &Q = tensor(a[0], "Q"), &S = tensor(a[1], "S"), &Y = tensor(a[2], "Y");
+        const int32_t flags = int32(a[3], "flags");
+        const at::Tensor* factor = optional(a[4], "factor");
+        const c10::Device d = device_of(Y, &Q, &S, factor);
+        const int64_t ldy = pitch(Y, "Y", kReal, 0, 0), rows = Y.size(0), cols = Y.size(1);
+        const int64_t ldq = code_pitch(Q, "Q", rows, cols), lds = word_pitch(S, "S", rows, cols, flags);
+        const float* f = flat<float>(factor, "factor", at::kFloat, 1);
+        return on(d, [&](void* st) {
+            return q4_f4_dequantize(bytes(&Q), ldq, word_data(&S), lds, int32(rows, "rows"), int32(cols, "cols"), flags, f, Y.data_ptr(),
+                                    type_of(Y), ldy, st);
+        });
+    });
+}
+
+// A, SA, Bt, SB, C, M, N, K, flags, FA, FB, starts (None: dense)
+PyObject* gemm_f4(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return entry<12>(a, n, [](PyObject* const* a) {
+        const at::Tensor &A = tensor(a[0], "A"), &SA = tensor(a[1], "SA"), &B = tensor(a[2], "Bt"), &SB = tensor(a[3], "SB"), &C = tensor(a[4], "C");
+        const int32_t M = int32(a[5], "M"), N = int32(a[6], "N"), K = int32(a[7], "K"), flags = int32(a[8], "flags");
+        const at::Tensor *FA = optional(a[9], "FA"), *FB = optional(a[10], "FB"), *starts = optional(a[11], "starts");
+        const c10::Device d = device_of(A, &SA, &B, &SB, &C, FA, FB, starts);
+        const int32_t* at = flat(starts, "starts", at::kInt, 1);
+        const int64_t E = starts ? starts->numel() - 1 : 1;
+        const int64_t lda = code_pitch(A, "A", M, K), ldb = code_pitch(B, "Bt", E * N, K), ldc = pitch(C, "C", kReal, M, N);
+        const int64_t ldsa = word_pitch(SA, "SA", M, K, flags), ldsb = word_pitch(SB, "SB", E * N, K, flags);
+        const float *fa = flat<float>(FA, "FA", at::kFloat, 1), *fb = flat<float>(FB, "FB", at::kFloat, E);
+        return on(d, [&](void* st) {
+            if (starts)
+                return q4_gemm_f4_experts(bytes(&A), lda, word_data(&SA), ldsa, bytes(&B), ldb, word_data(&SB), ldsb, flags, fa, fb, at,
+                                          int32(E, "experts"), C.data_ptr(), type_of(C), ldc, M, N, K, st);
+            return q4_gemm_f4(bytes(&A), lda, word_data(&SA), ldsa, bytes(&B), ldb, word_data(&SB), ldsb, flags, fa, fb, C.data_ptr(),
+                              type_of(C), ldc, M, N, K, st);
+        });
+    });
+}
+
+// X, ids, w, W1, S1, W2, S2, Out, E, H, ws, flags, F1, F2
+PyObject* expert_layer_f4(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return entry<14>(a, n, [](PyObject* const* a) {
+        const at::Tensor &X = tensor(a[0], "X"), &ids = tensor(a[1], "ids"), &W1 = tensor(a[3], "W1"), &S1 = tensor(a[4], "S1"),
+                         &W2 = tensor(a[5], "W2"), &S2 = tensor(a[6], "S2"), &Out = tensor(a[7], "Out"), &ws = tensor(a[10], "ws");
+        const at::Tensor *w = optional(a[2], "w"), *F1 = optional(a[12], "F1"), *F2 = optional(a[13], "F2");
+        const int32_t E = int32(a[8], "E"), H = int32(a[9], "H"), flags = int32(a[11], "flags");
+        const c10::Device d = device_of(X, &ids, w, &W1, &S1, &W2, &S2, &Out, &ws, F1, F2);
+        if (ids.dim() != 2) fail(PyExc_ValueError, "ids must be [tokens, topk]");
+        if (!ws.is_contiguous()) fail(PyExc_ValueError, "ws must be contiguous");
+        const int64_t ldx = pitch(X, "X", kReal, 0, 0), tokens = X.size(0), D = X.size(1), topk = ids.size(1);
+        if (ids.size(0) != tokens) fail(PyExc_ValueError, "ids must have a row per token");
+        const int64_t ldo = pitch(Out, "Out", kReal, tokens, D), rows1 = (int64_t)E * (flags & Q4_F4_GATED ? 2 : 1) * H, rows2 = (int64_t)E * D;
+        same_rows(X, Out);
+        const int64_t ldw1 = code_pitch(W1, "W1", rows1, D), lds1 = word_pitch(S1, "S1", rows1, D, flags);
+        const int64_t ldw2 = code_pitch(W2, "W2", rows2, H), lds2 = word_pitch(S2, "S2", rows2, H, flags);
+        const int32_t* i = flat(&ids, "ids", at::kInt, 0);
+        const float *pw = flat<float>(w, "w", at::kFloat, tokens * topk), *f1 = flat<float>(F1, "F1", at::kFloat, E),
+                    *f2 = flat<float>(F2, "F2", at::kFloat, E);
+        return on(d, [&](void* st) {
+            return q4_expert_layer_f4(X.data_ptr(), ldx, type_of(X), int32(tokens, "tokens"), int32(D, "width"), H, i, pw,
+                                      int32(topk, "topk"), E, flags, bytes(&W1), ldw1, word_data(&S1), lds1, f1, bytes(&W2), ldw2,
+                                      word_data(&S2), lds2, f2, Out.data_ptr(), ldo, ws.data_ptr(),
+                                      (size_t)ws.numel() * ws.element_size(), st);
+        });
+    });
+}
+
 #define Q4_ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {Q4_ENTRY(f8_quantize), Q4_ENTRY(gemm_f8), Q4_ENTRY(gemm_f8_experts), Q4_ENTRY(expert_sort),
-                         Q4_ENTRY(expert_gather), Q4_ENTRY(expert_combine), Q4_ENTRY(expert_combine_grad), {nullptr, nullptr, 0, nullptr}};
+                         Q4_ENTRY(expert_gather), Q4_ENTRY(expert_combine), Q4_ENTRY(expert_combine_grad),
+                         Q4_ENTRY(f4_quantize), Q4_ENTRY(f4_dequantize), Q4_ENTRY(gemm_f4), Q4_ENTRY(expert_layer_f4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q4_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
