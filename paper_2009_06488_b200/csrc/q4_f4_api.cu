@@ -29,6 +29,10 @@ q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* 
         !aligned(p.C, f8::type_size(p.c_type))) return Q4_ERR_ALIGNMENT;
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
+    if (kernel_variant() != 1 && gemm_f4_pair_supported(p)) {
+        log_choice(call, "CTA-pair tcgen05 kernel");
+        return launch_gemm_f4_pair(p, by16, stream_of(stream));
+    }
     log_choice(call, "general kernel");
     return done(launch_gemm_f4_simt(p, by16, stream_of(stream)));
 }
