@@ -9,8 +9,8 @@
 //   warp 0       TMA producer   per stage (256 depth values): the CTA's 128 rows of A and its half of the tile's rows of
 //                               Bt, 128 bytes each, 128-byte swizzle; rows past the end of the segment are not loaded
 //   warp 1       MMA issuer     (leader CTA) a stage's scales to tensor memory (two buffers), then four products
-//   warps 2, 3   scales         in turn: words of the CTA's 128 rows of A and of all the tile's rows of Bt, put in atoms
-//   warps 4..11  epilogue       each thread one row and BN / 2 columns: times f, rounded, out through swizzled staging slices
+//   warps 2..7   scales         words of the CTA's 128 rows of A and of all the tile's rows of Bt, put in atoms
+//   warps 8..15  epilogue       each thread one row and BN / 2 columns: times f, rounded, out through swizzled staging slices
 //                               and TMA stores (whole 32-row groups of aligned rows) or by pieces
 #include <cuda.h>
 
@@ -21,7 +21,7 @@ namespace f4 {
 
 constexpr int TMC = 128;                 // rows of A per CTA
 constexpr int FEW = 32;                  // rows of the smaller box of A
-constexpr int NTHREADS = 12 * 32;
+constexpr int NTHREADS = 16 * 32;
 constexpr int SLICE = 4096;              // staging slice of an epilogue warp: 32 rows x 128 bytes
 
 template <int BN, bool BY16> struct Cfg {
@@ -32,6 +32,7 @@ template <int BN, bool BY16> struct Cfg {
     static constexpr int SCALES = WORDS * (1 + BATOMS) * ATOM;
     static constexpr int STAGE = (TMC + BSH) * ROWB + SCALES;
     static constexpr int STAGES = BN == 256 ? 5 : 6;
+    static constexpr int PARTS = 1 + BATOMS, TEAMS = 6 / PARTS;      // warps that bring a stage's scales, and how many of these
     static constexpr int ACCS = BN == 256 ? 1 : 2;
     static constexpr int COL_SCALE = ACCS * BN;                // tensor memory: accumulators, then two buffers of scales
     static constexpr int SCALE_COLS = WORDS * (1 + BATOMS) * 4;
@@ -40,7 +41,7 @@ template <int BN, bool BY16> struct Cfg {
     static constexpr int NBAR = 2 * STAGES + 2 * ACCS;
     static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
     static constexpr int SMEM = OFF_MISC + 16 + 1024;          // + slack to align the base
-    static_assert(STAGE % 1024 == 0 && SMEM <= 232448 && COL_SCALE + 2 * SCALE_COLS <= 512, "shared or tensor memory");
+    static_assert(STAGES >= TEAMS && STAGE % 1024 == 0 && SMEM <= 232448 && COL_SCALE + 2 * SCALE_COLS <= 512, "shared or tensor memory");
 };
 
 struct PairParams {
@@ -180,7 +181,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
-            mbar_init(bar_full(s), 4);       // an announcement of copies and an arrival of scales per CTA
+            mbar_init(bar_full(s), 2 + 2 * C::PARTS);        // an announcement of copies and the scales' warps per CTA
             mbar_init(bar_empty(s), 1);      // the leader's commit
         }
         for (int a = 0; a < C::ACCS; ++a) {
@@ -264,44 +265,87 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 if (++acc == C::ACCS) { acc = 0; aph ^= 1u; }
             }
         }
-    } else if (warp < 4) {
+    } else if (warp < 8) {
         // ------------------------------------------------------------ scales
+        // A team of warps takes a stage, teams in turn: one warp the words of A, one for each 128 rows of Bt.  The words of
+        // a team's next three stages are under way.  The wait for a team's stage before told that the stages up to
+        // STAGES + TEAMS back are consumed, so the parity waited for cannot be that of an older round.
+        const int part = (warp - 2) % C::PARTS, team = (warp - 2) / C::PARTS;
         const uint32_t full_leader = map_to_cta(bar_full(0), 0);
-        const int64_t brows = (int64_t)g.N * (g.E ? g.E : 1);
+        const int64_t ld = part ? g.ldsb : g.ldsa;
         const int nw = (int)words_of(g.K, BY16);
-        uint32_t st = 0, ph = 0, it = 0;
-        for (int tile = cluster_id; walk.get(tile, t) && !lds32(abort_flag); tile += nclusters) {
-            const int arow = t.m0 + (int)rank * TMC;
-            const int arows = clamp_to(t.m_end - arow, 0, TMC);
-            const int bcols = (int)min(brows - t.brow, (int64_t)min(g.N - t.n0, BN));
-            for (int b = 0; b < nkb; ++b, ++it) {
-                if ((it & 1u) == (uint32_t)(warp - 2)) {
-                    uint4 v[C::WORDS * (1 + C::BATOMS)];
+        const uint32_t last_mask = valid_bytes(g.K - (nw - 1) * word_cols(BY16), group_of(BY16));
+        int tile = cluster_id, b = team;                       // what is loaded next: block b of the tile
+        const uint32_t* src = nullptr;
+        bool in[4];
+        bool more = walk.get(tile, t);
+        auto place = [&]() {
+            const int row0 = t.m0 + (int)rank * TMC, rows = part ? g.N - t.n0 - 128 * (part - 1) : t.m_end - row0;
+            src = (part ? g.SB + t.brow + 128 * (part - 1) : g.SA + row0) + lane;
 #pragma unroll
-                    for (int w = 0; w < C::WORDS; ++w) {
-                        const int word = b * C::WORDS + w;
-                        const uint32_t mask = word < nw ? valid_bytes(g.K - word * word_cols(BY16), group_of(BY16)) : 0u;
-                        v[w] = load_atom(g.SA + word * g.ldsa + arow, arows, mask, lane);
-#pragma unroll
-                        for (int j = 0; j < C::BATOMS; ++j)
-                            v[C::WORDS + w * C::BATOMS + j] = load_atom(g.SB + word * g.ldsb + t.brow + 128 * j, bcols - 128 * j, mask, lane);
-                    }
-                    mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
-                    const uint32_t dst = sbase + st * C::STAGE + (TMC + C::BSH) * ROWB + (uint32_t)lane * 16u;
-#pragma unroll
-                    for (int i = 0; i < C::WORDS * (1 + C::BATOMS); ++i) sts128(dst + (uint32_t)(i * ATOM), v[i]);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster_relaxed(full_leader + 8u * st);
-                }
-                if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+            for (int c = 0; c < 4; ++c) in[c] = lane + 32 * c < rows;
+        };
+        auto settle = [&]() {                                  // b may lie past the tile's end
+            if (more && b >= nkb) {
+                do {
+                    b -= nkb;
+                    more = walk.get(tile += nclusters, t);
+                } while (more && b >= nkb);
+                if (more) place();
             }
+        };
+        auto load = [&](uint4 (&v)[C::WORDS]) {                // the next stage's; false: there is none
+            if (!more) return false;
+#pragma unroll
+            for (int w = 0; w < C::WORDS; ++w) {
+                const int word = b * C::WORDS + w;
+                const uint32_t* at = src + word * ld;
+                v[w] = make_uint4(load_word(at, in[0] && word < nw), load_word(at + 32, in[1] && word < nw),
+                                  load_word(at + 64, in[2] && word < nw), load_word(at + 96, in[3] && word < nw));
+            }
+            b += C::TEAMS;
+            settle();
+            return true;
+        };
+        uint32_t it = (uint32_t)team, kb = (uint32_t)team;     // the stage that is written next, its block in its tile
+        auto put = [&](uint4 (&v)[C::WORDS]) {
+            while (kb >= (uint32_t)nkb) kb -= (uint32_t)nkb;
+            if ((int)(kb + 1) * C::WORDS >= nw) {
+#pragma unroll
+                for (int w = 0; w < C::WORDS; ++w)
+                    if ((int)kb * C::WORDS + w == nw - 1) v[w] = make_uint4(v[w].x & last_mask, v[w].y & last_mask, v[w].z & last_mask, v[w].w & last_mask);
+            }
+            const uint32_t st = it % C::STAGES, ph = it / C::STAGES & 1u;
+            mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
+            const uint32_t dst = sbase + st * C::STAGE + (TMC + C::BSH) * ROWB + (uint32_t)lane * 16u;
+#pragma unroll
+            for (int w = 0; w < C::WORDS; ++w)
+                sts128(dst + (uint32_t)((part ? C::WORDS + w * C::BATOMS + part - 1 : w) * ATOM), v[w]);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(full_leader + 8u * st);
+            it += C::TEAMS;
+            kb += C::TEAMS;
+        };
+        if (more) place();
+        settle();
+        uint4 v0[C::WORDS], v1[C::WORDS], v2[C::WORDS];
+        bool h0 = load(v0), h1 = load(v1), h2 = load(v2);
+        while (h0 && !lds32(abort_flag)) {
+            put(v0);
+            h0 = load(v0);
+            if (!h1) break;
+            put(v1);
+            h1 = load(v1);
+            if (!h2) break;
+            put(v2);
+            h2 = load(v2);
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        const int lg = warp & 3, set = warp >= 8 ? 1 : 0;
+        const int lg = warp & 3, set = warp >= 12 ? 1 : 0;
         const uint32_t tempty_leader = map_to_cta(bar_tempty(0), 0);
-        const uint32_t slice = sbase + C::OFF_SLICE + (uint32_t)((warp - 4) * SLICE);
+        const uint32_t slice = sbase + C::OFF_SLICE + (uint32_t)((warp - 8) * SLICE);
         const uint32_t mine = slice + (uint32_t)(lane * 128), sw = (uint32_t)(lane & 7);
         const float fa = g.FA ? __ldg(g.FA) : 1.0f;
         uint32_t acc = 0, aph = 0;

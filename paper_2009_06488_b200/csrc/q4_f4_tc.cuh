@@ -66,16 +66,13 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t saddr)
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
 }
 
-// The words of scales of up to 128 rows as a lane's part of an atom: rows lane, lane + 32, ...
-// `base`: the first row's word; rows from `rows` on and bytes outside `mask` read 0.
-__device__ __forceinline__ uint4 load_atom(const uint32_t* base, int rows, uint32_t mask, int lane)
+// A load that stays where it is written, ahead of its use; 0 where `in` is false.
+__device__ __forceinline__ uint32_t load_word(const uint32_t* at, bool in)
 {
-    uint32_t w[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b32 %0, 0;\n\t@p ld.global.nc.b32 %0, [%1];\n\t}"
-                     : "=r"(w[c]) : "l"(base + lane + 32 * c), "r"((int)(lane + 32 * c < rows && mask)));
-    return make_uint4(w[0] & mask, w[1] & mask, w[2] & mask, w[3] & mask);
+    uint32_t w;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b32 %0, 0;\n\t@p ld.global.nc.b32 %0, [%1];\n\t}"
+                 : "=r"(w) : "l"(at), "r"((int)in));
+    return w;
 }
 
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
