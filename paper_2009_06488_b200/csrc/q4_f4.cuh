@@ -128,6 +128,8 @@ cudaError_t launch_f4_dequantize(const f4::DequantizeParams& p, int y_type, bool
 cudaError_t launch_gemm_f4_simt(const f4::GemmParams& p, bool by16, cudaStream_t st);
 bool        gemm_f4_pair_supported(const f4::GemmParams& p);
 q4_status   launch_gemm_f4_pair(const f4::GemmParams& p, bool by16, cudaStream_t st);
+bool        expert_layer_f4_stream_supported(const f4::LayerParams& p, bool by16);
+q4_status   launch_expert_layer_f4_stream(const f4::LayerParams& p, bool by16, cudaStream_t st);
 cudaError_t launch_expert_layer_f4_simt(const f4::LayerParams& p, bool by16, cudaStream_t st);
 int64_t     expert_layer_f4_ws_bytes(int64_t pairs, int32_t D, int32_t H);
 

@@ -135,6 +135,10 @@ q4_status q4_expert_layer_f4(const void* X, int64_t ldx, int32_t type, int32_t t
     f4::LayerParams p{X, ldx, type, tokens, topk, D, H, E, up == 2, ids, w, W1, ldw1, S1, lds1, F1, W2, ldw2, S2, lds2, F2,
                       Out, ldo, ws, device_status_ptr()};
     if (!p.status) return Q4_ERR_CUDA;
+    if (kernel_variant() != 1 && expert_layer_f4_stream_supported(p, flags & Q4_F4_BY16)) {
+        log_choice("q4_expert_layer_f4", "streaming kernels");
+        return launch_expert_layer_f4_stream(p, flags & Q4_F4_BY16, stream_of(stream));
+    }
     log_choice("q4_expert_layer_f4", "general kernels");
     return done(launch_expert_layer_f4_simt(p, flags & Q4_F4_BY16, stream_of(stream)));
 }

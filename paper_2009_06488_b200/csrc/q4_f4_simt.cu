@@ -142,11 +142,6 @@ cudaError_t launch_gemm_f4_simt(const f4::GemmParams& p, bool by16, cudaStream_t
     return cudaGetLastError();
 }
 
-int64_t expert_layer_f4_ws_bytes(int64_t pairs, int32_t D, int32_t H)
-{
-    return pairs * H * 4;
-}
-
 cudaError_t launch_expert_layer_f4_simt(const f4::LayerParams& p, bool by16, cudaStream_t st)
 {
     const int64_t pairs = (int64_t)p.tokens * p.topk;
