@@ -56,7 +56,9 @@ template <bool BY16> __device__ __forceinline__ float scale_value(uint32_t byte)
     return BY16 ? e4m3_value(byte & 0x7Fu) : pow2_value(byte);
 }
 
-// Whether the group that begins at column `at` exists, and the words' valid bytes of the word that begins there.
+__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+// The bytes that exist of a word of scales with `cols_left` columns from its first on.
 __device__ __forceinline__ uint32_t valid_bytes(int cols_left, int group)
 {
     const int n = (cols_left + group - 1) / group;

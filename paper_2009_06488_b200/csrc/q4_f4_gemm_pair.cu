@@ -396,7 +396,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 for (int q = 0; q < CW / 32; ++q) {
                     uint32_t r[32];
                     tc_ld32(ta + (uint32_t)(32 * q), r);
-                    tc_wait_ld();
+                    tc_wait_ld32(r);
                     if (q == CW / 32 - 1) release();
                     if (c0 + 32 * q >= g.N) continue;
                     reuse();
@@ -414,7 +414,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 for (int q = 0; q < CW / 32; ++q) {
                     uint32_t r[32];
                     tc_ld32(ta + (uint32_t)(32 * q), r);
-                    tc_wait_ld();
+                    tc_wait_ld32(r);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const float x = __uint_as_float(r[2 * j]) * f, y = __uint_as_float(r[2 * j + 1]) * f;

@@ -1,59 +1,63 @@
 // Expert layer for a few tokens on e2m1 weights with microscales: two kernels that stream the weights of the experts that
-// are hit, once, from HBM.
+// are hit, once, from HBM through the block-scaled tensor-core product.
 //
 //   kernel 1 (up)     h = silu(G_e x) * (U_e x)  (or silu(G_e x)) of every pair of a token and an expert, binary32
-//   kernel 2 (down)   y = W2_e h of every pair, binary32; the block that finishes a tile of columns last sums
+//   kernel 2 (down)   y = W2_e h of every pair, binary32; the block that finishes columns last sums, at its end,
 //                     Out[t] = sum_j w[t][j] y in the order of j
 //
-// Every block sorts the pairs by expert for itself (a few hundred numbers).  A unit is up to 8 * NT pairs of one expert, a
-// tile 64 rows of its weights (gated: 32 of G and the same 32 of U).  One persistent block per SM walks tiles, a
-// unit's one after the other, so that the unit's activations stay in shared memory:
+// The tensor core multiplies e2m1 by e2m1, and activations are not quantized: a group of them is written as a sum of PARTS
+// e2m1 vectors under one scale 2^a,
+//   x = 2^a (c0 + 2^-2 c1 + 2^-5 c2 + 2^-8 c3 + ... + 2^-17 c6) + rest,   max |x| / 2^a in [2, 4),
+// each the nearest to what the ones before leave (at most half a step: 1/2, then 1/4 of a range of +-2), so that the rest is
+// at most 2^-21 of the group's largest value.  Binary16 and bfloat16 values that are not far below their group's largest
+// are exact.  The parts are rows of the product's second operand and their results are added in binary32.  The scale is
+// that of the weights' kind: a power of two per 32, or per 16 one in e4m3 (17 powers, above 2^-17 of the row's
+// largest value) times a power of two for the row.
 //
-//   warps 8..11  producers   a stage (256 depth values) of the tile's rows by TMA (128-byte swizzle), its words of scales
-//                            by 4-byte asynchronous copies, tile after tile without a break
-//   warps 0..7   consumers   in turn a stage each: codes become binary16 numbers, warp-level matrix instructions (16 x 8 x 16)
-//                            with the weights' rows as their 16 and the pairs as their 8, binary32 sums in registers,
-//                            which are added over the warps, in order, at the tile's end
+// Every block sorts the pairs by expert for itself (a few hundred numbers).  A unit is up to NTOK pairs of one expert, a
+// tile 64 rows of its weights (gated: 32 of G and the same 32 of U) by PARTS * NTOK columns, the whole depth.  One
+// persistent block per SM walks tiles, a unit's one after the other:
 //
-// Activations are held in binary16, a row times a power of two that takes its largest value to 2^14 .. 2^15.  That is
-// exact for binary16 and bfloat16 values down to 2^-38 of a row's largest; h, computed in binary32, is rounded to
-// 11 bits by it (an eighth of a step of a bfloat16 output).
+//   warp 0        producer     stages of 256 depth values: two boxes of 32 rows by TMA (128-byte swizzle)
+//   warp 1        MMA issuer   a stage's scales to tensor memory, then four products (their upper 64 rows are not used)
+//   warps 2, 3    scales       a stage each in turn: the rows' words, three stages ahead, put in atoms
+//   warps 4, 5    epilogue     parts added, gate and product meet through shared memory
+//   warps 6, 7    (kernel 2)   a tile's counter, every other tile each
+//   warps 8..23   activations  the next unit's parts and scales, while this one's are multiplied
 //
-// The order of depth values inside a stage is free as long as both operands share it, and is chosen for the scales: BY16 a
-// lane holds 64 consecutive values of a row, whose four scales are one word, and a code times its scale is exact in
-// binary16; else the four lanes of a row share a group of 32, whose two products are scaled in binary32.
-// Bound: HBM, with instruction issue next (about 14 instructions for 128 bytes of codes by 16, 11 by 32).
+// Bound: HBM; ahead of it the start (sorting, the first unit's parts) of some 5 us.  What was tried: codes to binary16 in
+// registers and warp-level matrix instructions, the depth spread over a block's warps (16 tokens 86 us) or a strip of rows per
+// warp, brought by 16-byte copies (75) or TMA (77): eight instructions per 16 codes left HBM at a third of its rate.
 #include <cuda.h>
 
-#include "q4_f4.cuh"
-#include "q4_tc_ptx.cuh"
+#include "q4_f4_tc.cuh"
 
 namespace q4 {
-
-bool make_byte_map(CUtensorMap* tm, const uint8_t* base, int64_t ld, int rows, int kbytes, int box_rows);
-
 namespace f4 {
 
-constexpr int CONSUMERS = 8, PRODUCERS = 4;
-constexpr int LAYER_THREADS = (CONSUMERS + PRODUCERS) * 32;
+constexpr int PARTS = 7;
 constexpr int TROWS = 64, BOXROWS = 32;          // weights' rows of a tile and of a copy
-constexpr int SK = 256, SROWB = 128;             // depth values and bytes per row of a stage
 constexpr int MAX_PAIRS = 1024;                  // sorted by each block
+constexpr int ACT0 = 8, ACTS = 16;               // first of the activations' warps, their number
+constexpr int LAYER_THREADS = (ACT0 + ACTS) * 32;
+constexpr int MAX_STAGES = 12;
+constexpr int MAX_TILES = 4096;                  // of a block
 
-// Shared memory, in this order: stages, their scales, pairs' activations, partial sums, the sorted pairs, barriers.
-template <bool BY16, int NT> struct LayerCfg {
-    static constexpr int WORDS = BY16 ? 4 : 2;
-    static constexpr int STAGE = TROWS * SROWB;
-    static constexpr int SCALE = WORDS * TROWS * 4;
-    static constexpr int N = 8 * NT;                           // pairs of a unit
-    static constexpr int PITCH = TROWS + 4;
-    static constexpr int PART = CONSUMERS * N * PITCH * 4;
+// Shared memory, in this order: stages of codes, their atoms, units' parts, their atoms, lists and the rest.
+template <bool BY16, int NTOK> struct LayerCfg {
+    static constexpr int WORDS = kWords<BY16>;
+    static constexpr int N = 8 * NTOK;                         // columns of a tile (PARTS * NTOK, a multiple of 16)
+    static constexpr int STAGE = TROWS * ROWB, ATOMS = WORDS * ATOM;
+    static constexpr int BLOCK = N * ROWB + ATOMS;             // parts of 256 depth values, and their scales
     static constexpr int LISTS = MAX_PAIRS * 2 * 3 + (Q4_MAX_EXPERTS + 32) * 4 * 2;
-    static constexpr int TAIL = 2 * 16 * 8 + 64 + N * 8;       // barriers, words, pairs' scales
-    static __host__ __device__ constexpr int act_pitch(int nkb) { return nkb * SK * 2 + 64; }
-    static __host__ __device__ constexpr int bytes(int stages, int nkb)
+    static constexpr int REST = 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4 + (2 * MAX_STAGES + 12) * 8 + 8 + MAX_TILES / 8;
+    static constexpr int COL_SCALE = 2 * N;                    // tensor memory: two accumulators, two buffers of scales
+    static constexpr int COLS = 256;
+    static_assert(PARTS * NTOK <= N && COL_SCALE + 2 * 2 * WORDS * 4 <= COLS, "tensor memory");
+    // (a product reads 128 rows: past the last stage it reads what follows)
+    static __host__ __device__ constexpr int bytes(int stages, int bufs, int nkb)
     {
-        return stages * (STAGE + SCALE) + N * act_pitch(nkb) + PART + LISTS + TAIL + 1024;
+        return stages * (STAGE + ATOMS) + bufs * nkb * BLOCK + LISTS + REST + 1024;
     }
 };
 
@@ -61,48 +65,26 @@ struct LayerLaunch {
     LayerParams p;
     float* hidden;                   // [pairs][H]
     float* y;                        // [pairs][D]
-    int* done;                       // per tile of output columns
-    int stages;
+    int* done;                       // units that are finished per tile of output columns
+    int stages, bufs;
 };
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-                 "{%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-// the binary16 values of two e4m3 numbers
-__device__ __forceinline__ uint32_t scales2(uint32_t bytes)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)bytes));
-    return r;
-}
-__device__ __forceinline__ void copy_word(uint32_t dst, const uint32_t* src, bool in)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
 // Sorts the pairs by expert: order[] = pairs, expert by expert, in their own order; units of up to N pairs.  All threads.
-template <int N>
-__device__ __forceinline__ int sort_pairs(const LayerParams& p, uint16_t* order, uint16_t* rank, uint16_t* unit, int* first, int* units, int* total)
+template <int N, int THREADS>
+__device__ __forceinline__ int sort_pairs(const LayerParams& p, uint16_t* order, uint16_t* rank, uint16_t* unit, int* first, int* units)
 {
     const int n = p.tokens * p.topk, lane = threadIdx.x & 31, padded = (p.E + 31) & ~31;
-    for (int e = threadIdx.x; e < padded; e += LAYER_THREADS) first[e] = 0;
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const unsigned e = (unsigned)__ldg(p.ids + i);
+        unit[i] = (uint16_t)(e < (unsigned)p.E ? e : 0xFFFFu);              // (experts, until the units are known)
+    }
+    for (int e = threadIdx.x; e < padded; e += THREADS) first[e] = 0;
     __syncthreads();
     if (threadIdx.x < 32) {
         for (int i0 = 0; i0 < n; i0 += 32) {
-            const int i = i0 + lane, e = i < n ? __ldg(p.ids + i) : -1;
-            const bool in = (unsigned)e < (unsigned)p.E;
-            const unsigned same = __match_any_sync(0xFFFFFFFFu, in ? e : -1), before = same & ((1u << lane) - 1u);
+            const int i = i0 + lane, e = i < n ? unit[i] : 0xFFFF;
+            const bool in = e != 0xFFFF;
+            const unsigned same = __match_any_sync(0xFFFFFFFFu, e), before = same & ((1u << lane) - 1u);
             const int have = in ? first[e] : 0;
             __syncwarp();
             if (in) {
@@ -113,361 +95,533 @@ __device__ __forceinline__ int sort_pairs(const LayerParams& p, uint16_t* order,
         }
         int at = 0, un = 0;
         for (int e0 = 0; e0 < padded; e0 += 32) {
-            const int c = first[e0 + lane], u = (c + N - 1) / N;
-            int sc = c, su = u;
+            const int c = first[e0 + lane], both = c | ((c + N - 1) / N) << 16;      // at most 1024 of either
+            int sum = both;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int a = __shfl_up_sync(0xFFFFFFFFu, sc, o), b = __shfl_up_sync(0xFFFFFFFFu, su, o);
-                if (lane >= o) { sc += a; su += b; }
+                const int a = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= o) sum += a;
             }
-            first[e0 + lane] = at + sc - c;
-            units[e0 + lane] = un + su - u;
-            for (int k = 0; k < u; ++k) unit[un + su - u + k] = (uint16_t)(e0 + lane);
-            at += __shfl_sync(0xFFFFFFFFu, sc, 31);
-            un += __shfl_sync(0xFFFFFFFFu, su, 31);
+            first[e0 + lane] = at + (sum & 0xFFFF) - c;
+            units[e0 + lane] = un + (sum >> 16) - (both >> 16);
+            sum = __shfl_sync(0xFFFFFFFFu, sum, 31);
+            at += sum & 0xFFFF;
+            un += sum >> 16;
         }
         if (lane == 0) {
             first[padded] = at;
-            *total = un;
+            units[padded] = un;
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += LAYER_THREADS) {
-        const int e = __ldg(p.ids + i);
-        if ((unsigned)e < (unsigned)p.E) order[first[e] + rank[i]] = (uint16_t)i;
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const int e = unit[i];
+        if (e != 0xFFFF) order[first[e] + rank[i]] = (uint16_t)i;
     }
     __syncthreads();
-    return *total;
+    for (int e = threadIdx.x; e < p.E; e += THREADS)
+        for (int u = units[e]; u < units[e + 1]; ++u) unit[u] = (uint16_t)e;
+    __syncthreads();
+    return units[padded];
 }
 
-// A pair's activations (or hidden values) to shared memory as binary16 numbers times a power of two, in the stage's order;
-// by a warp.  Returns the power's inverse.
-template <bool BY16, typename T>
-__device__ __forceinline__ float put_activations(const T* row, int K, int nkb, uint32_t dst, int lane)
+
+// 8 consecutive values from k on, 0 where there are none.
+template <typename T> __device__ __forceinline__ f8::Eight<T> eight_at(const T* row, int k, int K)
 {
-    const bool vec = (uintptr_t)row % 16 == 0;
-    auto eight = [&](int k, float (&v)[8]) {
-        if (vec && k + 8 <= K) {
-            f8::Eight<T> e;
+    f8::Eight<T> e;
+    if ((uintptr_t)row % 16 == 0 && k + 8 <= K) {
 #pragma unroll
-            for (int q = 0; q < f8::Eight<T>::NW / 4; ++q) {
-                const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + k) + 16 * q);
-                e.w[4 * q] = u.x; e.w[4 * q + 1] = u.y; e.w[4 * q + 2] = u.z; e.w[4 * q + 3] = u.w;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = e.get(i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < K ? f8::to_f(row[k + i]) : 0.0f;
+        for (int q = 0; q < f8::Eight<T>::NW / 4; ++q) {
+            const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + k) + 16 * q);
+            e.w[4 * q] = u.x; e.w[4 * q + 1] = u.y; e.w[4 * q + 2] = u.z; e.w[4 * q + 3] = u.w;
         }
-    };
+    } else {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? f8::to_f(row[k + i]) : 0.0f;
+        f8::pack8(e, v);
+    }
+    return e;
+}
+template <typename T> __device__ __forceinline__ uint32_t largest(const f8::Eight<T>& e)
+{
     uint32_t a = 0;
-#pragma unroll 4
-    for (int k = lane * 8; k < K; k += 256) {
-        float v[8];
-        eight(k, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    }
-    a = __reduce_max_sync(0xFFFFFFFFu, a);
-    // a row that is not finite keeps its values
-    const uint32_t e = a == 0 || a >= 0x7F800000u ? 141u : max(a >> 23, 15u);
-    const float s = __uint_as_float((268u - e) << 23);
-#pragma unroll 4
-    for (int b = 0; b < nkb; ++b) {
-        float v[8];
-        eight(b * SK + lane * 8, v);
-        uint32_t h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = f8::pack2(v[2 * i] * s, v[2 * i + 1] * s, (const __half*)nullptr);
-        // BY16: value 64 t + 8 i + r of the stage lies at 16 bytes t of piece i
-        const int at = BY16 ? (lane & 7) * 64 + (lane >> 3) * 16 : lane * 16;
-        sts128(dst + (uint32_t)(b * SK * 2 + at), make_uint4(h[0], h[1], h[2], h[3]));
-    }
-    return __uint_as_float((e - 14u) << 23);
+    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(e.get(i)) & 0x7FFFFFFFu);
+    return a;
 }
 
-template <bool BY16, int NT, bool DOWN>
+// Parts and scales of 256 values of a pair (column n of the unit), eight per lane, by a warp.  rowe: the biased exponent of
+// the row's factor (BY16).  parts, atoms: the block's places.
+template <bool BY16, int NTOK, typename T>
+__device__ __forceinline__ void put_parts(const f8::Eight<T>& v, int n, uint32_t rowe, uint32_t parts, uint32_t atoms, int lane)
+{
+    uint32_t a = largest(v);
+    a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    if (!BY16) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+    const int e = (int)(a >> 23);
+    uint32_t byte;
+    int s;                                                     // biased exponent of the scale
+    if (BY16) {
+        const int se = clamp_to(e - 1 - (int)rowe, -9, 8);     // of its e4m3 part
+        byte = e == 255 ? 0x7Fu : se >= -6 ? (uint32_t)(se + 7) << 3 : 1u << (se + 9);
+        s = se + (int)rowe;
+    } else {
+        s = max(e, 2) - 1;
+        byte = e == 255 ? 255u : (uint32_t)s;
+    }
+    const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v.get(i) * inv;
+    // (not unrolled, like all that runs once: a block's first pass through its code waits for the instructions)
+    float mult = 4.0f;
+#pragma unroll 1
+    for (int row = n; row < PARTS * NTOK; row += NTOK) {
+        const uint32_t c = codes8(r);
+        sts32(parts + (uint32_t)(row * ROWB) + (uint32_t)((((lane >> 2) ^ row) & 7) << 4) + (uint32_t)(lane & 3) * 4u, (int)c);
+        // what the codes stand for, without decoding them: the nearest multiple of a half, from 2 on of one, ties to even
+        // (a sum with 1.5 * 2^22 or 2^23 rounds so)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float big = fabsf(r[i]) > 2.0f ? 12582912.0f : 6291456.0f;
+            r[i] = (r[i] - ((r[i] + big) - big)) * mult;
+        }
+        mult = 8.0f;
+    }
+    // the words: by 16 a word is 8 lanes' (a group two), else 16 lanes' (a group four)
+    constexpr int G = BY16 ? 2 : 4;
+    uint32_t w = byte << (8 * (lane / G & 3));
+    w |= __shfl_xor_sync(0xFFFFFFFFu, w, G);
+    w |= __shfl_xor_sync(0xFFFFFFFFu, w, 2 * G);
+    const int q = lane & (4 * G - 1), row = q * NTOK + n;      // lane q of a word writes it for part q
+    if (q < PARTS) sts32(atoms + (uint32_t)(lane / (4 * G) * ATOM + (row & 31) * 16 + (row >> 5) * 4), (int)w);
+}
+
+template <bool BY16, int NTOK, bool DOWN>
 __global__ void __launch_bounds__(LAYER_THREADS, 1)
 layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
 {
-    using C = LayerCfg<BY16, NT>;
+    using C = LayerCfg<BY16, NTOK>;
     const LayerParams& p = L.p;
     extern __shared__ uint8_t smem_raw[];
-    const int K = DOWN ? p.H : p.D, nkb = (K + SK - 1) / SK, pitch = C::act_pitch(nkb), STAGES = L.stages;
-    const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t scales_s = sbase + STAGES * C::STAGE, act_s = scales_s + STAGES * C::SCALE, part_s = act_s + C::N * pitch,
-                   lists_s = part_s + C::PART, tail_s = lists_s + C::LISTS;
+    const int K = DOWN ? p.H : p.D, nkb = (K + STAGE_K - 1) / STAGE_K, STAGES = L.stages;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u, act_s = sbase + STAGES * C::STAGE,
+                   atoms_s = act_s + L.bufs * nkb * C::N * ROWB, act_atoms = atoms_s + STAGES * C::ATOMS,
+                   lists_s = act_atoms + L.bufs * nkb * C::ATOMS;
     uint8_t* const lists = smem_raw + (lists_s - smem_u32(smem_raw));
-    int* const first = reinterpret_cast<int*>(lists);                       // [E, a multiple of 32, + 1]
+    int* const first = reinterpret_cast<int*>(lists);                       // pairs before each expert [E, a multiple of 32, + 1]
     int* const units = first + Q4_MAX_EXPERTS + 32;                         // units before each expert
     uint16_t* const order = reinterpret_cast<uint16_t*>(units + Q4_MAX_EXPERTS + 32);
     uint16_t* const rank = order + MAX_PAIRS;
     uint16_t* const unit = rank + MAX_PAIRS;                                // expert of each unit
-    int* const words = reinterpret_cast<int*>(smem_raw + (tail_s + 2 * 16 * 8 - smem_u32(smem_raw)));
-    float* const inverse = reinterpret_cast<float*>(words + 16);            // [N]
-    auto bar_full  = [&](int s) { return tail_s + 8u * (uint32_t)s; };
-    auto bar_empty = [&](int s) { return tail_s + 8u * (uint32_t)(16 + s); };
-    const uint32_t abort_flag = tail_s + 2 * 16 * 8;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float* const row_factor = reinterpret_cast<float*>(lists + C::LISTS);   // [unit & 3][8]
+    unsigned* const row_max = reinterpret_cast<unsigned*>(row_factor + 32); // [8]
+    float* const exchange = reinterpret_cast<float*>(row_max + 8);          // [NTOK][32]
+    const uint32_t bar0 = lists_s + C::LISTS + 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4;
+    auto bar_full   = [&](uint32_t s) { return bar0 + 8u * s; };
+    auto bar_empty  = [&](uint32_t s) { return bar0 + 8u * (MAX_STAGES + s); };
+    auto bar_tfull  = [&](uint32_t a) { return bar0 + 8u * (2 * MAX_STAGES + a); };
+    auto bar_tempty = [&](uint32_t a) { return bar0 + 8u * (2 * MAX_STAGES + 2 + a); };
+    auto bar_act    = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 4 + b); };     // a unit's parts are there
+    auto bar_used   = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 6 + b); };     // ... and have been multiplied
+    auto bar_done   = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 8 + b); };     // a tile's results are written (kernel 2)
+    auto bar_noted  = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 10 + b); };    // ... and counted
+    const uint32_t abort_flag = bar0 + 8u * (2 * MAX_STAGES + 12), tmem_slot = abort_flag + 4;
+    unsigned* const last_of = reinterpret_cast<unsigned*>(smem_raw + (abort_flag + 8 - smem_u32(smem_raw)));      // a bit per tile
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(bar_full(s), 1 + 32);        // the copies' announcement, and each producer lane's scales
+            mbar_init(bar_full(s), 2);       // the copies' announcement, the scales' warp
             mbar_init(bar_empty(s), 1);
         }
-        words[0] = 0;
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(bar_tfull(a), 1);
+            mbar_init(bar_tempty(a), 2);     // the epilogue's warps
+            mbar_init(bar_act(a), ACTS);
+            mbar_init(bar_used(a), 1);
+            mbar_init(bar_done(a), 2);
+            mbar_init(bar_noted(a), 1);
+        }
+        sts32(abort_flag, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
+    }
+    if (DOWN && warp == 2)
+        for (int i = lane; i < MAX_TILES / 32; i += 32) last_of[i] = 0;
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)C::COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // Kernel 2 starts when every block of kernel 1 has waited for what came before them: what it reads but for the
     // hidden values is there, and its bounded waits ahead of those last as long as kernel 1 at most.
     if (!DOWN) f8::wait_for_predecessor();
-    const int nunits = sort_pairs<C::N>(p, order, rank, unit, first, units, words + 1);
+    tc_fence_before();
+    const int nunits = sort_pairs<NTOK, LAYER_THREADS>(p, order, rank, unit, first, units);
+    tc_fence_after();
+    const uint32_t tmem_base = (uint32_t)lds32(tmem_slot);
+    const bool gated = !DOWN && p.gated;
     const int rows = DOWN ? p.D : p.H;                          // of the output
-    const int per_tile = !DOWN && p.gated ? TROWS / 2 : TROWS;
-    const int ntr = (rows + per_tile - 1) / per_tile, ntiles = nunits * ntr;
-    if (!DOWN)
-        for (int i = blockIdx.x * LAYER_THREADS + threadIdx.x; i < (p.D + TROWS - 1) / TROWS; i += gridDim.x * LAYER_THREADS) L.done[i] = 0;
+    const int per = gated ? BOXROWS : TROWS;                    // of them in a tile
+    const int each = (rows + per - 1) / per, ntiles = nunits * each;
+    const int expert_rows = DOWN ? p.D : gated ? 2 * p.H : p.H, half = gated ? p.H : BOXROWS;
     // a block's tiles lie together
     const int t0 = (int)((int64_t)ntiles * blockIdx.x / gridDim.x), t1 = (int)((int64_t)ntiles * (blockIdx.x + 1) / gridDim.x);
-    const int64_t wrows = (int64_t)p.E * (DOWN ? p.D : p.gated ? 2 * p.H : p.H);
+    if (!DOWN)
+        for (int i = blockIdx.x * LAYER_THREADS + threadIdx.x; i < (p.D + TROWS - 1) / TROWS; i += gridDim.x * LAYER_THREADS) L.done[i] = 0;
 
-    if (warp >= CONSUMERS) {
-        // ------------------------------------------------------------ producers
+    if (warp == 0) {
+        // ------------------------------------------------------------ producer
+        uint32_t st = 0, ph = 0;
+        for (int tile = t0; tile < t1 && !lds32(abort_flag); ++tile) {
+            const int u = tile / each, row = unit[u] * expert_rows + (tile - u * each) * per;
+            for (int b = 0; b < nkb; ++b) {
+                mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, p.status);
+                if (elect_one()) {
+                    const uint32_t dst = sbase + st * C::STAGE;
+                    mbar_expect_tx(bar_full(st), (uint32_t)C::STAGE);
+                    tma_load_2d(dst, &tmW, b * ROWB, row, bar_full(st));
+                    tma_load_2d(dst + BOXROWS * ROWB, &tmW, b * ROWB, row + half, bar_full(st));
+                }
+                __syncwarp();
+                if (++st == (uint32_t)STAGES) { st = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer
+        const uint64_t desc0 = make_kmajor_sw128_desc(sbase), act0 = make_kmajor_sw128_desc(act_s), scales0 = scales_desc(atoms_s),
+                       act_scales0 = scales_desc(act_atoms);
+        uint32_t st = 0, ph = 0, buf = 0, acc = 0, aph = 0, ab = 0, abph = 0;
+        int at_unit = t0 < t1 ? t0 / each : 0;
+        if (t0 < t1) mbar_wait_suspend(bar_act(0), 0, abort_flag, p.status);
+        for (int tile = t0; tile < t1 && !lds32(abort_flag); ++tile) {
+            const int u = tile / each;
+            if (u != at_unit) {
+                at_unit = u;
+                if (++ab == (uint32_t)L.bufs) { ab = 0; abph ^= 1u; }
+                mbar_wait_suspend(bar_act(ab), abph, abort_flag, p.status);
+            }
+            const bool last_of_unit = tile + 1 == t1 || (tile + 1) / each != u;
+            mbar_wait(bar_tempty(acc), aph ^ 1u, abort_flag, p.status);
+            for (int b = 0; b < nkb; ++b) {
+                mbar_wait(bar_full(st), ph, abort_flag, p.status);
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4));
+                    const uint64_t bdesc = act0 + (uint64_t)((ab * nkb + b) * (uint32_t)(C::N * ROWB >> 4));
+                    const uint64_t sa_desc = scales0 + (uint64_t)(st * (uint32_t)(C::ATOMS >> 4));
+                    const uint64_t sb_desc = act_scales0 + (uint64_t)((ab * nkb + b) * (uint32_t)(C::ATOMS >> 4));
+                    const uint32_t sa = tmem_base + C::COL_SCALE + buf * (8 * C::WORDS), sb = sa + 4 * C::WORDS;
+#pragma unroll
+                    for (int w = 0; w < C::WORDS; ++w) {
+                        tc_copy_scales<1>(sa + 4 * w, sa_desc + (uint64_t)(w * (ATOM >> 4)));
+                        tc_copy_scales<1>(sb + 4 * w, sb_desc + (uint64_t)(w * (ATOM >> 4)));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int w = BY16 ? k : k >> 1;
+                        tc_mma_f4<BY16, 1>(tmem_base + acc * C::N, adesc + 2 * k, bdesc + 2 * k, idesc<BY16>(128, C::N, BY16 ? 0 : 2 * (k & 1)),
+                                           sa + 4 * w, sb + 4 * w, b | k ? 1u : 0u);
+                    }
+                    tc_commit(bar_empty(st));
+                    if (b == nkb - 1) {
+                        tc_commit(bar_tfull(acc));
+                        if (last_of_unit) tc_commit(bar_used(ab));
+                    }
+                }
+                __syncwarp();
+                buf ^= 1u;
+                if (++st == (uint32_t)STAGES) { st = 0; ph ^= 1u; }
+            }
+            aph ^= acc;
+            acc ^= 1u;
+        }
+    } else if (warp < 4) {
+        // ------------------------------------------------------------ scales
+        // (the wait for the stage before told that stages up to STAGES + 2 back are consumed: a parity cannot be an older round's)
         const uint32_t* const S = DOWN ? p.S2 : p.S1;
         const int64_t lds = DOWN ? p.lds2 : p.lds1;
         const int nw = (int)words_of(K, BY16);
-        int it = 0;
-        for (int tile = t0; tile < t1; ++tile) {
-            const int u = tile / ntr, r0 = (tile - u * ntr) * per_tile;
-            const int64_t ra = (int64_t)unit[u] * (wrows / p.E) + r0, rb = ra + (!DOWN && p.gated ? p.H : BOXROWS);
-            for (int b = 0; b < nkb; ++b, ++it) {
-                if ((it & (PRODUCERS - 1)) != warp - CONSUMERS) continue;
-                const int st = it % STAGES;
-                mbar_wait_suspend(bar_empty(st), ((uint32_t)(it / STAGES) & 1u) ^ 1u, abort_flag, p.status);
-                const uint32_t dst = sbase + st * C::STAGE, sc = scales_s + st * C::SCALE + 4u * (uint32_t)lane;
-                if (elect_one()) {
-                    mbar_expect_tx(bar_full(st), (uint32_t)C::STAGE);
-                    tma_load_2d(dst, &tmW, b * SROWB, (int)ra, bar_full(st));
-                    tma_load_2d(dst + BOXROWS * SROWB, &tmW, b * SROWB, (int)rb, bar_full(st));
+        const uint32_t last_mask = valid_bytes(K - (nw - 1) * word_cols(BY16), group_of(BY16));
+        int tile = t0, b = warp - 2;                           // what is loaded next
+        const uint32_t *lo = nullptr, *hi = nullptr;
+        auto place = [&]() {
+            while (tile < t1 && b >= nkb) {
+                b -= nkb;
+                ++tile;
+            }
+            if (tile >= t1) return;
+            const int u = tile / each, r0 = (tile - u * each) * per;
+            const uint32_t* const at = S + unit[u] * expert_rows;
+            // (a row past the end is the last one again: its results are not written)
+            lo = at + min(r0 + lane, rows - 1);
+            hi = gated ? lo + half : at + min(r0 + BOXROWS + lane, rows - 1);
+        };
+        auto load = [&](uint2 (&v)[C::WORDS]) {
+            if (tile >= t1) return false;
+#pragma unroll
+            for (int w = 0; w < C::WORDS; ++w) {
+                const int word = b * C::WORDS + w;
+                v[w] = make_uint2(load_word(lo + word * lds, word < nw), load_word(hi + word * lds, word < nw));
+            }
+            if ((b += 2) >= nkb) place();
+            return true;
+        };
+        uint32_t it = (uint32_t)(warp - 2);
+        int kb = warp - 2;
+        auto put = [&](uint2 (&v)[C::WORDS]) {
+            while (kb >= nkb) kb -= nkb;
+            const uint32_t st = it % (uint32_t)STAGES, ph = it / (uint32_t)STAGES & 1u;
+            mbar_wait_suspend(bar_empty(st), ph ^ 1u, abort_flag, p.status);
+            const uint32_t dst = atoms_s + st * C::ATOMS + (uint32_t)lane * 16u;
+#pragma unroll
+            for (int w = 0; w < C::WORDS; ++w) {
+                const uint32_t mask = kb * C::WORDS + w == nw - 1 ? last_mask : 0xFFFFFFFFu;
+                sts32(dst + (uint32_t)(w * ATOM), (int)(v[w].x & mask));
+                sts32(dst + (uint32_t)(w * ATOM + 4), (int)(v[w].y & mask));
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_full(st));
+            it += 2;
+            kb += 2;
+        };
+        place();
+        uint2 v0[C::WORDS], v1[C::WORDS], v2[C::WORDS];
+        bool h0 = load(v0), h1 = load(v1), h2 = load(v2);
+        while (h0 && !lds32(abort_flag)) {
+            put(v0);
+            h0 = load(v0);
+            if (!h1) break;
+            put(v1);
+            h1 = load(v1);
+            if (!h2) break;
+            put(v2);
+            h2 = load(v2);
+        }
+    } else if (warp < 6) {
+        // ------------------------------------------------------------ epilogue
+        const int h = warp - 4;
+        uint32_t acc = 0, aph = 0;
+        for (int tile = t0; tile < t1; ++tile) {               // (no way out: the warps meet)
+            const int u = tile / each, r0 = (tile - u * each) * per, e = unit[u];
+            const int begin = first[e] + (u - units[e]) * NTOK, count = min(NTOK, first[e + 1] - begin);
+            const float* const F = DOWN ? p.F2 : p.F1;
+            const float f = F ? __ldg(F + e) : 1.0f;
+            mbar_wait_suspend(bar_tfull(acc), aph, abort_flag, p.status);
+            tc_fence_after();
+            const uint32_t ta = tmem_base + ((uint32_t)(h * 32) << 16) + acc * C::N;
+            float v[NTOK];
+#pragma unroll
+            for (int n = 0; n < NTOK; ++n) v[n] = 0.0f;
+            // smallest parts first
+#pragma unroll
+            for (int c = C::N / 32 - 1; c >= 0; --c) {
+                uint32_t r[32];
+                tc_ld32(ta + 32 * c, r);
+                tc_wait_ld32(r);
+#pragma unroll
+                for (int i = 31; i >= 0; --i) {
+                    const int q = (32 * c + i) / NTOK;
+                    if (q < PARTS) v[i % NTOK] = fmaf(__uint_as_float(r[i]), q ? 1.0f / (float)(1 << (3 * q - 1)) : 1.0f, v[i % NTOK]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_tempty(acc));
+            aph ^= acc;
+            acc ^= 1u;
+#pragma unroll
+            for (int n = 0; n < NTOK; ++n) v[n] *= (BY16 ? row_factor[(u & 3) * 8 + n] : 1.0f) * f;
+            if (gated) {
+                if (h == 1) {
+#pragma unroll
+                    for (int n = 0; n < NTOK; ++n) exchange[n * 32 + lane] = v[n];
+                }
+                asm volatile("bar.sync 2, 64;" ::: "memory");
+                if (h == 0 && r0 + lane < rows) {
+#pragma unroll
+                    for (int n = 0; n < NTOK; ++n)
+                        if (n < count) L.hidden[(int64_t)order[begin + n] * p.H + r0 + lane] = v[n] / (1.0f + expf(-v[n])) * exchange[n * 32 + lane];
+                }
+                asm volatile("bar.sync 2, 64;" ::: "memory");
+            } else {
+                const int r = r0 + 32 * h + lane;
+                // (kernel 2: the counter of the tile two before has been taken)
+                if (DOWN && tile - t0 >= 2) mbar_wait_suspend(bar_noted(tile - t0 & 1), (uint32_t)(tile - t0 - 2) >> 1 & 1u, abort_flag, p.status);
+                if (r < rows) {
+#pragma unroll
+                    for (int n = 0; n < NTOK; ++n)
+                        if (n < count) {
+                            const int pair = order[begin + n];
+                            if (DOWN) L.y[(int64_t)pair * p.D + r] = v[n];
+                            else L.hidden[(int64_t)pair * p.H + r] = v[n] / (1.0f + expf(-v[n]));
+                        }
+                }
+            }
+            if (DOWN) {
+                __syncwarp();                                  // my half of the tile is written
+                if (lane == 0) mbar_arrive(bar_done(tile - t0 & 1));
+            }
+        }
+    } else if (warp < 8) {
+        // ------------------------------------------------------------ counters
+        // each warp every other tile: which tiles are the last of their columns
+        if (DOWN) {
+            f8::wait_for_predecessor();                        // the counters' zeros
+            for (int i = warp - 6; i < t1 - t0 && !lds32(abort_flag); i += 2) {
+                mbar_wait_suspend(bar_done(i & 1), (uint32_t)i >> 1 & 1u, abort_flag, p.status);
+                if (lane == 0) {
+                    __threadfence();
+                    const bool last = atomicAdd(L.done + (t0 + i) % each * per / TROWS, 1) == nunits - 1;
+                    __threadfence();
+                    if (last) atomicOr(last_of + (i >> 5), 1u << (i & 31));
+                    mbar_arrive(bar_noted(i & 1));
                 }
                 __syncwarp();
-#pragma unroll
-                for (int w = 0; w < C::WORDS; ++w) {
-                    const bool in = b * C::WORDS + w < nw;
-                    const uint32_t* const src = S + (in ? (b * C::WORDS + w) * lds : 0);
-                    const bool ia = in && ra + lane < wrows, ib = in && rb + lane < wrows;
-                    copy_word(sc + (uint32_t)(w * TROWS * 4), ia ? src + ra + lane : S, ia);
-                    copy_word(sc + (uint32_t)((w * TROWS + BOXROWS) * 4), ib ? src + rb + lane : S, ib);
-                }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full(st)) : "memory");
             }
-            if (lds32(abort_flag)) break;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        return;
-    }
-    // ---------------------------------------------------------------- consumers
-    if (DOWN) f8::wait_for_predecessor();                      // the hidden values, and the counters' zeros
-    const int g = lane >> 2, t = lane & 3;
-    int at_unit = -1, begin = 0, count = 0, it0 = 0;
-    float f = 1.0f;
-    for (int tile = t0; tile < t1; ++tile, it0 += nkb) {
-        const int u = tile / ntr, r0 = (tile - u * ntr) * per_tile;
-        if (u != at_unit) {
-            at_unit = u;
-            const int e = unit[u];
-            begin = first[e] + (u - units[e]) * C::N;
-            count = min(C::N, first[e + 1] - begin);
-            const float* const F = DOWN ? p.F2 : p.F1;
-            f = F ? __ldg(F + e) : 1.0f;
-            // (the tile before ended with a barrier behind its last reading of activations)
-            for (int n = warp; n < count; n += CONSUMERS) {
-                const int pair = order[begin + n];
-                const uint32_t dst = act_s + (uint32_t)(n * pitch);
-                const int64_t x0 = (int64_t)(pair / p.topk) * p.ldx;
-                float inv;
-                if (DOWN) inv = put_activations<BY16>(L.hidden + (int64_t)pair * p.H, K, nkb, dst, lane);
-                else if (p.type == Q4_BF16) inv = put_activations<BY16>(static_cast<const __nv_bfloat16*>(p.X) + x0, K, nkb, dst, lane);
-                else inv = put_activations<BY16>(static_cast<const __half*>(p.X) + x0, K, nkb, dst, lane);
-                if (lane == 0) inverse[n] = inv;
-            }
-            sync_consumers();
-        }
-        float acc[4][NT][4] = {};
-        for (int b = (warp - it0) & (CONSUMERS - 1); b < nkb; b += CONSUMERS) {
-            const int it = it0 + b, st = it % STAGES;
-            mbar_wait_suspend(bar_full(st), (uint32_t)(it / STAGES) & 1u, abort_flag, p.status);
-            const uint32_t ws = sbase + st * C::STAGE, sc = scales_s + st * C::SCALE;
-            const uint32_t xs = act_s + (uint32_t)(g * pitch + b * SK * 2 + t * 16);
-            const int nw = (int)words_of(K, BY16) - b * C::WORDS;      // words that exist
-            auto masked = [&](int row, int w) {
-                const uint32_t v = (uint32_t)lds32(sc + 4u * (uint32_t)(w * TROWS + row));
-                return w < nw - 1 ? v : w == nw - 1 ? v & valid_bytes(K - b * SK - w * word_cols(BY16), group_of(BY16)) : 0u;
-            };
-            if constexpr (BY16) {
-                uint32_t sw[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) sw[r] = masked(8 * r + g, t) & 0x7F7F7F7Fu;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    // 32 codes of each of my rows: piece 2 t + h
-                    uint4 c[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) c[r] = lds128(ws + (uint32_t)((8 * r + g) * SROWB + (((2 * t + h) ^ g) << 4)));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint4 x[NT];
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) x[j] = lds128(xs + (uint32_t)(8 * j * pitch + (4 * h + i) * 64));
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            uint32_t a[4], d[4];
-                            const uint4 &ca = c[2 * r], &cd = c[2 * r + 1];
-                            values8(i == 0 ? ca.x : i == 1 ? ca.y : i == 2 ? ca.z : ca.w, a);
-                            values8(i == 0 ? cd.x : i == 1 ? cd.y : i == 2 ? cd.z : cd.w, d);
-                            const uint32_t pick = i < 2 ? 0x1010 : 0x3232;
-                            const uint32_t sa = __byte_perm(scales2(sw[2 * r] >> (16 * h)), 0, pick);
-                            const uint32_t sd = __byte_perm(scales2(sw[2 * r + 1] >> (16 * h)), 0, pick);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) { a[k] = mul2(a[k], sa); d[k] = mul2(d[k], sd); }
-#pragma unroll
-                            for (int j = 0; j < NT; ++j) {
-                                mma_f16(acc[r][j], a[0], d[0], a[1], d[1], x[j].x, x[j].y);
-                                mma_f16(acc[r][j], a[2], d[2], a[3], d[3], x[j].z, x[j].w);
-                            }
-                        }
+    } else if (warp >= ACT0) {
+        // ------------------------------------------------------------ activations
+        if (DOWN) f8::wait_for_predecessor();                  // the hidden values
+        const int me = warp - ACT0;
+        const int u0 = t0 < t1 ? t0 / each : 0, u1 = t0 < t1 ? (t1 - 1) / each : -1;
+        auto all = [&](auto zero, const void* src, int64_t ld, int div) {
+            using T = decltype(zero);
+            uint32_t ab = 0, abph = 0;
+            for (int u = u0; u <= u1; ++u) {                    // (no way out: the warps meet)
+                const int e = unit[u], begin = first[e] + (u - units[e]) * NTOK, count = min(NTOK, first[e + 1] - begin);
+                const int items = count * nkb;                 // 256 values of a pair each: pair i % count, block i / count
+                auto value = [&](int i) {
+                    const int n = i % count;
+                    return eight_at(static_cast<const T*>(src) + (int64_t)(order[begin + n] / div) * ld, i / count * STAGE_K + lane * 8, K);
+                };
+                if (BY16) {
+                    // the rows' largest values
+                    if (me == 0 && lane < 8) row_max[lane] = 0;
+                    asm volatile("bar.sync 3, 512;" ::: "memory");
+#pragma unroll 1
+                    for (int i = me; i < items; i += ACTS) {
+                        const uint32_t a = __reduce_max_sync(0xFFFFFFFFu, largest(value(i)));
+                        if (lane == 0) atomicMax(row_max + i % count, a);
                     }
+                    asm volatile("bar.sync 3, 512;" ::: "memory");
                 }
-            } else {
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    uint32_t sw[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) sw[r] = masked(8 * r + g, w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint4 x[NT];
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) x[j] = lds128(xs + (uint32_t)(8 * j * pitch + (4 * w + i) * 64));
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint32_t at = ws + (uint32_t)((16 * r + g) * SROWB + (((4 * w + i) ^ g) << 4) + 4 * t);
-                            uint32_t a[4], d[4];
-                            values8((uint32_t)lds32(at), a);
-                            values8((uint32_t)lds32(at + 8 * SROWB), d);
-                            // 2^(byte - 127): 0 is 2^-127, 255 becomes NaN
-                            auto scale = [&](uint32_t word) {
-                                const uint32_t top = i == 0 ? word << 24 : i == 1 ? (word << 16) & 0xFF000000u : i == 2 ? (word << 8) & 0xFF000000u : word & 0xFF000000u;
-                                const float s = __uint_as_float(max(top >> 1, 0x00400000u));
-                                return fmaf(s, 0.0f, s);
-                            };
-                            const float sa = scale(sw[2 * r]), sd = scale(sw[2 * r + 1]);
-#pragma unroll
-                            for (int j = 0; j < NT; ++j) {
-                                float m[4] = {};
-                                mma_f16(m, a[0], d[0], a[1], d[1], x[j].x, x[j].y);
-                                mma_f16(m, a[2], d[2], a[3], d[3], x[j].z, x[j].w);
-                                acc[r][j][0] = fmaf(m[0], sa, acc[r][j][0]);
-                                acc[r][j][1] = fmaf(m[1], sa, acc[r][j][1]);
-                                acc[r][j][2] = fmaf(m[2], sd, acc[r][j][2]);
-                                acc[r][j][3] = fmaf(m[3], sd, acc[r][j][3]);
-                            }
-                        }
-                    }
+                // biased exponent of a row's factor: its largest group's scale is e4m3's 2^8
+                auto row_exponent = [&](int n) {
+                    const uint32_t m = row_max[n];
+                    return (m >= 0x7F800000u ? 127u : max(m >> 23, 20u)) - 9u;
+                };
+                if (BY16 && me == 0 && lane < count) row_factor[(u & 3) * 8 + lane] = __uint_as_float(row_exponent(lane) << 23);
+                f8::Eight<T> v;
+                if (me < items) v = value(me);
+                mbar_wait_suspend(bar_used(ab), abph ^ 1u, abort_flag, p.status);
+#pragma unroll 1
+                for (int i = me; i < items; i += ACTS) {
+                    const int n = i % count, at = ab * nkb + i / count;
+                    const f8::Eight<T> now = v;
+                    if (i + ACTS < items) v = value(i + ACTS);
+                    put_parts<BY16, NTOK>(now, n, BY16 ? row_exponent(n) : 0u, act_s + (uint32_t)(at * C::N * ROWB),
+                                          act_atoms + (uint32_t)(at * C::ATOMS), lane);
                 }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_act(ab));
+                if (BY16) asm volatile("bar.sync 3, 512;" ::: "memory");       // row_max has been read
+                if (++ab == (uint32_t)L.bufs) { ab = 0; abph ^= 1u; }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_empty(st));
-        }
-        // partial sums [warp][pair][row]
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    sts32(part_s + 4u * (uint32_t)((warp * C::N + 8 * j + 2 * t + (i & 1)) * C::PITCH + 16 * r + 8 * (i >> 1) + g),
-                          __float_as_int(acc[r][j][i]));
-        sync_consumers();
-        auto sum = [&](int n, int row) {
-            float v = 0.0f;
-#pragma unroll
-            for (int k = 0; k < CONSUMERS; ++k) v += __int_as_float(lds32(part_s + 4u * (uint32_t)((k * C::N + n) * C::PITCH + row)));
-            return v * inverse[n] * f;
         };
-        for (int i = threadIdx.x; i < count * per_tile; i += CONSUMERS * 32) {
-            const int n = i / per_tile, row = i % per_tile, pair = order[begin + n];
-            if (r0 + row >= rows) continue;
-            const float v = sum(n, row);
-            if (DOWN) {
-                L.y[(int64_t)pair * p.D + r0 + row] = v;
-            } else {
-                const float s = v / (1.0f + expf(-v));
-                L.hidden[(int64_t)pair * p.H + r0 + row] = p.gated ? s * sum(n, BOXROWS + row) : s;
-            }
-        }
-        if (DOWN) {
-            __threadfence();
-            sync_consumers();                                  // all of the tile is written
-            if (threadIdx.x == 0) words[2] = atomicAdd(L.done + r0 / TROWS, 1) == nunits - 1;
-        }
-        sync_consumers();                                      // partial sums have been read
-        if (DOWN && words[2]) {
-            // these columns of every pair are there
-            __threadfence();
-            for (int i = threadIdx.x; i < p.tokens * TROWS; i += CONSUMERS * 32) {
-                const int tok = i / TROWS, d = r0 + i % TROWS;
-                if (d >= p.D) continue;
-                float out = 0.0f;
-#pragma unroll 4
-                for (int j = 0; j < p.topk; ++j) {
-                    const int64_t pair = (int64_t)tok * p.topk + j;
-                    if ((unsigned)__ldg(p.ids + pair) >= (unsigned)p.E) continue;
-                    out = fmaf(p.w ? __ldg(p.w + pair) : 1.0f, __ldcg(L.y + pair * p.D + d), out);
-                }
-                store_value(p.Out, tok * p.ldo + d, p.type, out);
-            }
-        }
+        if (DOWN) all(0.0f, L.hidden, p.H, 1);
+        else if (p.type == Q4_BF16) all(__nv_bfloat16(), p.X, p.ldx, p.topk);
+        else all(__half(), p.X, p.ldx, p.topk);
     }
-    if (DOWN && nunits == 0)                                   // no pair at all
-        for (int64_t i = (int64_t)blockIdx.x * CONSUMERS * 32 + threadIdx.x; i < (int64_t)p.tokens * p.D; i += (int64_t)gridDim.x * CONSUMERS * 32)
-            store_value(p.Out, i / p.D * p.ldo + i % p.D, p.type, 0.0f);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (DOWN) {
+        // Columns that this block was the last to finish: the sum over each token's pairs, in their order, by all threads; a
+        // thread's 8 values are under way together (every address exists; what does not count is left out).
+        const int words = (t1 - t0 + 31) / 32;
+        for (int k = 0; k < words; ++k)
+            for (uint32_t m = last_of[k]; m; m &= m - 1) {
+                const int r0 = (t0 + 32 * k + __ffs((int)m) - 1) % each * per;
+                for (int i = threadIdx.x; i < p.tokens * TROWS; i += LAYER_THREADS) {
+                    const int tok = i / TROWS, d = r0 + i % TROWS;
+                    const float* const y = L.y + (int64_t)tok * p.topk * p.D + min(d, p.D - 1);
+                    float out = 0.0f;
+#pragma unroll 1
+                    for (int j0 = 0; j0 < p.topk; j0 += 8) {
+                        float yv[8], wt[8];
+                        int id[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int at = min(j0 + j, p.topk - 1);
+                            id[j] = __ldg(p.ids + tok * p.topk + at);
+                            wt[j] = p.w ? __ldg(p.w + tok * p.topk + at) : 1.0f;
+                            yv[j] = __ldcg(y + (int64_t)at * p.D);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j0 + j < p.topk && (unsigned)id[j] < (unsigned)p.E) out = fmaf(wt[j], yv[j], out);
+                    }
+                    if (d < p.D) store_value(p.Out, (int64_t)tok * p.ldo + d, p.type, out);
+                }
+            }
+        if (nunits == 0)                                       // no pair at all
+            for (int64_t i = (int64_t)blockIdx.x * LAYER_THREADS + threadIdx.x; i < (int64_t)p.tokens * p.D; i += (int64_t)gridDim.x * LAYER_THREADS)
+                store_value(p.Out, i / p.D * p.ldo + i % p.D, p.type, 0.0f);
+    }
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::COLS) : "memory");
 }
 
 constexpr int SMEM_MOST = 232448;
 
-template <bool BY16, int NT> static int stages_for(int K)
+// Stages and units whose parts are held: two where six stages fit beside them, else one; {0, 0}: none.
+struct Room { int stages, bufs; };
+template <bool BY16, int NTOK> static Room room_for(int K)
 {
-    using C = LayerCfg<BY16, NT>;
-    const int nkb = (K + SK - 1) / SK;
-    return C::bytes(16, nkb) <= SMEM_MOST ? 16 : C::bytes(8, nkb) <= SMEM_MOST ? 8 : 0;
+    using C = LayerCfg<BY16, NTOK>;
+    const int nkb = (K + STAGE_K - 1) / STAGE_K;
+    for (int bufs = 2; bufs >= 1; --bufs) {
+        int stages = (SMEM_MOST - C::bytes(0, bufs, nkb)) / (C::STAGE + C::ATOMS);
+        if (stages > MAX_STAGES) stages = MAX_STAGES;
+        if (stages >= (bufs == 2 ? 6 : 4)) return {stages, bufs};
+    }
+    return {0, 0};
 }
 
-template <bool BY16, int NT, bool DOWN>
-static cudaError_t launch_layer(LayerLaunch L, const CUtensorMap& m, cudaStream_t st)
+template <bool BY16, int NTOK, bool DOWN>
+static q4_status launch_layer(LayerLaunch L, cudaStream_t st)
 {
-    using C = LayerCfg<BY16, NT>;
-    auto kernel = layer_kernel<BY16, NT, DOWN>;
+    using C = LayerCfg<BY16, NTOK>;
+    const LayerParams& p = L.p;
+    auto kernel = layer_kernel<BY16, NTOK, DOWN>;
     static bool ready[64] = {};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return Q4_ERR_CUDA;
     if (!ready[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
-        if (e != cudaSuccess) return e;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST) != cudaSuccess) return Q4_ERR_CUDA;
         ready[dev] = true;
     }
-    const int K = DOWN ? L.p.H : L.p.D;
-    L.stages = stages_for<BY16, NT>(K);
-    return f8::launch(kernel, (unsigned)(2 * f8_pairs_of_device()), LAYER_THREADS, C::bytes(L.stages, (K + SK - 1) / SK), st, m, L);
+    const int K = DOWN ? p.H : p.D;
+    const Room r = room_for<BY16, NTOK>(K);
+    L.stages = r.stages;
+    L.bufs = r.bufs;
+    CUtensorMap m;
+    if (!make_byte_map(&m, DOWN ? p.W2 : p.W1, DOWN ? p.ldw2 : p.ldw1, p.E * (DOWN ? p.D : p.gated ? 2 * p.H : p.H), (K + 1) / 2, BOXROWS))
+        return Q4_ERR_CUDA;
+    const int smem = C::bytes(r.stages, r.bufs, (K + STAGE_K - 1) / STAGE_K);
+    return f8::launch(kernel, (unsigned)(2 * f8_pairs_of_device()), LAYER_THREADS, smem, st, m, L) == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
-
-template <bool BY16, int NT>
-static cudaError_t launch_both(const LayerLaunch& L, const CUtensorMap& up, const CUtensorMap& down, cudaStream_t st)
+template <bool BY16, int NTOK>
+static q4_status launch_both(const LayerLaunch& L, cudaStream_t st)
 {
-    const cudaError_t e = launch_layer<BY16, NT, false>(L, up, st);
-    return e != cudaSuccess ? e : launch_layer<BY16, NT, true>(L, down, st);
+    const q4_status e = launch_layer<BY16, NTOK, false>(L, st);
+    return e != Q4_OK ? e : launch_layer<BY16, NTOK, true>(L, st);
 }
 
 }  // namespace f4
@@ -482,33 +636,33 @@ int64_t expert_layer_f4_ws_bytes(int64_t pairs, int32_t D, int32_t H)
     return counters_bytes(D) + 4 * pairs * ((int64_t)H + D);
 }
 
-// 16-bit activations whose rows fit shared memory eight at a time, weights that a tensor map can name, few pairs.
-bool expert_layer_f4_stream_supported(const f4::LayerParams& p, bool by16)
+template <int NTOK> static bool fits(const f4::LayerParams& p, bool by16)
 {
     const int K = p.D > p.H ? p.D : p.H;
+    return K <= 16384 && (by16 ? room_for<true, NTOK>(K) : room_for<false, NTOK>(K)).stages > 0;
+}
+
+// 16-bit activations whose parts fit shared memory four pairs at a time, weights that a tensor map can name, few pairs.
+bool expert_layer_f4_stream_supported(const f4::LayerParams& p, bool by16)
+{
     const int64_t rows1 = (int64_t)p.E * (p.gated ? 2 : 1) * p.H, rows2 = (int64_t)p.E * p.D;
-    return p.type != Q4_F32 && (int64_t)p.tokens * p.topk <= MAX_PAIRS && K <= 16384 &&
-           (by16 ? stages_for<true, 1>(K) : stages_for<false, 1>(K)) > 0 && rows1 < INT32_MAX - 512 && rows2 < INT32_MAX - 512 &&
+    return p.type != Q4_F32 && (int64_t)p.tokens * p.topk <= MAX_PAIRS && fits<4>(p, by16) &&
+           rows1 < INT32_MAX - 512 && rows2 < INT32_MAX - 512 &&
+           (int64_t)MAX_PAIRS * ((p.D + TROWS - 1) / TROWS) / (2 * f8_pairs_of_device()) < MAX_TILES &&
            (uintptr_t)p.W1 % 16 == 0 && (uintptr_t)p.W2 % 16 == 0 && p.ldw1 % 16 == 0 && p.ldw2 % 16 == 0;
 }
 
 q4_status launch_expert_layer_f4_stream(const f4::LayerParams& p, bool by16, cudaStream_t st)
 {
     const int64_t pairs = (int64_t)p.tokens * p.topk;
-    LayerLaunch L{p, nullptr, nullptr, nullptr, 0};
+    LayerLaunch L{p, nullptr, nullptr, nullptr, 0, 0};
     L.done = static_cast<int*>(p.ws);
     L.hidden = reinterpret_cast<float*>(static_cast<uint8_t*>(p.ws) + counters_bytes(p.D));
     L.y = L.hidden + pairs * p.H;
-    CUtensorMap up, down;
-    if (!make_byte_map(&up, p.W1, p.ldw1, p.E * (p.gated ? 2 : 1) * p.H, (p.D + 1) / 2, BOXROWS) ||
-        !make_byte_map(&down, p.W2, p.ldw2, p.E * p.D, (p.H + 1) / 2, BOXROWS)) return Q4_ERR_CUDA;
-    // sixteen pairs per unit where experts are hit by more than eight on average: the weights pass once for them
-    const int K = p.D > p.H ? p.D : p.H;                       // both kernels alike
-    const bool two = pairs > 8 * (int64_t)p.E && (by16 ? stages_for<true, 2>(K) : stages_for<false, 2>(K)) > 0;
-    cudaError_t e;
-    if (by16) e = two ? launch_both<true, 2>(L, up, down, st) : launch_both<true, 1>(L, up, down, st);
-    else e = two ? launch_both<false, 2>(L, up, down, st) : launch_both<false, 1>(L, up, down, st);
-    return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
+    // Eight pairs per unit where their parts fit, so that an expert's weights pass once for them; four where experts are hit by
+    // three at most on average: their parts leave room for more stages.
+    if (pairs > 3 * (int64_t)p.E && fits<8>(p, by16)) return by16 ? launch_both<true, 8>(L, st) : launch_both<false, 8>(L, st);
+    return by16 ? launch_both<true, 4>(L, st) : launch_both<false, 4>(L, st);
 }
 
 }  // namespace q4

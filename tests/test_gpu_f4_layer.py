@@ -223,3 +223,31 @@ def test_quantized_weights_serve_both_ways(q4):
         assert (np.abs(got - want) <= off + (np.abs(want) + off) * 2.0 ** -8).all()
         # an e2m1 rounding is off by a quarter of the value at most, a third of that typically: two layers of them
         assert np.linalg.norm(batch.double().cpu().numpy() - want) < 0.5 * np.linalg.norm(want)
+
+
+def test_scales_that_binary16_does_not_hold(q4):
+    """Powers of two far below and above: some groups, some rows, and 2^-127 itself."""
+    import torch
+    T, topk, E, D, H = 3, 1, 2, 320, 64
+    r = np.random.default_rng(5)
+    for gated in (False, True):
+        up = (2 if gated else 1) * H
+        mats, dev = [], []
+        for n, k, spread in ((E * up, D, 1), (E * D, H, 3)):
+            byte = r.integers(120, 128, (n, -(-k // 32))).astype(np.uint8)
+            byte[::3, 0] = 127 - 40 * spread
+            byte[1::5, -1] = 0
+            byte[2::7, 1] = 127 + 5 * spread
+            q, s = f4.pack(r.integers(0, 16, (n, k)).astype(np.uint8)), f4.to_words(byte)
+            mats.append(f4.values(q, s, k))
+            dev += [placed(q, up16(q.shape[1])), word_tensor(s)]
+        # the second matrix gets rows of tiny values only: nothing else of these rows is in the result
+        x = torch.from_numpy(r.standard_normal((T, D)).astype(np.float32) * 0.01).cuda().half()
+        ids = np.array([[0], [1], [0]], dtype=np.int32)
+        out = torch.empty_like(x)
+        ws = torch.empty(q4.q4_expert_layer_f4_workspace_bytes(T, topk, D, H), dtype=torch.uint8, device="cuda")
+        q4.q4_expert_layer_f4(x, torch.from_numpy(ids).cuda(), None, *dev, out, E, H, ws, gated=gated)
+        want, off = f4.layer(x.double().cpu().numpy(), ids, None, mats[0].reshape(E, up, D), mats[1].reshape(E, D, H), gated)
+        got = out.double().cpu().numpy()
+        fine = np.abs(want) < 60000
+        assert fine.any() and (np.abs(got - want) <= off + (np.abs(want) + off) * HALF_ULP["f16"] + HALF_SMALLEST["f16"])[fine].all()
