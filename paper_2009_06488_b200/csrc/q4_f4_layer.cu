@@ -15,15 +15,16 @@
 // largest value) times a power of two for the row.
 //
 // Every block sorts the pairs by expert for itself (a few hundred numbers).  A unit is up to NTOK pairs of one expert, a
-// tile 64 rows of its weights (gated: 32 of G and the same 32 of U) by PARTS * NTOK columns, the whole depth.  One
+// tile 128 rows of its weights (gated: 64 of G and the same 64 of U) by PARTS * NTOK columns, the whole depth.  (A product
+// of 128 rows takes about 118 clk however few its columns are: with tiles of 64 rows these were the bound.)  One
 // persistent block per SM walks tiles, a unit's one after the other:
 //
-//   warp 0        producer     stages of 256 depth values: two boxes of 32 rows by TMA (128-byte swizzle)
-//   warp 1        MMA issuer   a stage's scales to tensor memory, then four products (their upper 64 rows are not used)
-//   warps 2, 3    scales       a stage each in turn: the rows' words, three stages ahead, put in atoms
-//   warps 4, 5    epilogue     parts added, gate and product meet through shared memory
-//   warps 6, 7    (kernel 2)   a tile's counter, every other tile each
-//   warps 8..23   activations  the next unit's parts and scales, while this one's are multiplied
+//   warp 0        producer     stages of 256 depth values: two boxes of 64 rows by TMA (128-byte swizzle)
+//   warp 1        MMA issuer   a stage's scales to tensor memory, then four products
+//   warps 2, 3    scales       a stage each in turn: the rows' words, two turns ahead, put in atoms
+//   warps 4..7    epilogue     parts added, gate and product meet through shared memory
+//   warps 8, 9    (kernel 2)   a tile's counter, every other tile each
+//   warps 10..23  activations  the next unit's parts and scales, while this one's are multiplied
 //
 // Bound: HBM; ahead of it the start (sorting, the first unit's parts) of some 5 us.  What was tried: codes to binary16 in
 // registers and warp-level matrix instructions, the depth spread over a block's warps (16 tokens 86 us) or a strip of rows per
@@ -36,9 +37,10 @@ namespace q4 {
 namespace f4 {
 
 constexpr int PARTS = 7;
-constexpr int TROWS = 64, BOXROWS = 32;          // weights' rows of a tile and of a copy
+constexpr int TROWS = 128, BOXROWS = 64;          // weights' rows of a tile and of a copy
 constexpr int MAX_PAIRS = 1024;                  // sorted by each block
-constexpr int ACT0 = 8, ACTS = 16;               // first of the activations' warps, their number
+constexpr int ACT0 = 10, ACTS = 14;              // first of the activations' warps, their number
+static_assert(ACTS * 32 == 448, "the activations' warps meet");
 constexpr int LAYER_THREADS = (ACT0 + ACTS) * 32;
 constexpr int MAX_STAGES = 12;
 constexpr int MAX_TILES = 4096;                  // of a block
@@ -54,7 +56,6 @@ template <bool BY16, int NTOK> struct LayerCfg {
     static constexpr int COL_SCALE = 2 * N;                    // tensor memory: two accumulators, two buffers of scales
     static constexpr int COLS = 256;
     static_assert(PARTS * NTOK <= N && COL_SCALE + 2 * 2 * WORDS * 4 <= COLS, "tensor memory");
-    // (a product reads 128 rows: past the last stage it reads what follows)
     static __host__ __device__ constexpr int bytes(int stages, int bufs, int nkb)
     {
         return stages * (STAGE + ATOMS) + bufs * nkb * BLOCK + LISTS + REST + 1024;
@@ -219,7 +220,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
     uint16_t* const unit = rank + MAX_PAIRS;                                // expert of each unit
     float* const row_factor = reinterpret_cast<float*>(lists + C::LISTS);   // [unit & 3][8]
     unsigned* const row_max = reinterpret_cast<unsigned*>(row_factor + 32); // [8]
-    float* const exchange = reinterpret_cast<float*>(row_max + 8);          // [NTOK][32]
+    float* const exchange = reinterpret_cast<float*>(row_max + 8);          // [NTOK][BOXROWS]
     const uint32_t bar0 = lists_s + C::LISTS + 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4;
     auto bar_full   = [&](uint32_t s) { return bar0 + 8u * s; };
     auto bar_empty  = [&](uint32_t s) { return bar0 + 8u * (MAX_STAGES + s); };
@@ -239,10 +240,10 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(bar_tfull(a), 1);
-            mbar_init(bar_tempty(a), 2);     // the epilogue's warps
+            mbar_init(bar_tempty(a), 4);     // the epilogue's warps
             mbar_init(bar_act(a), ACTS);
             mbar_init(bar_used(a), 1);
-            mbar_init(bar_done(a), 2);
+            mbar_init(bar_done(a), 4);
             mbar_init(bar_noted(a), 1);
         }
         sts32(abort_flag, 0);
@@ -346,7 +347,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
         const int nw = (int)words_of(K, BY16);
         const uint32_t last_mask = valid_bytes(K - (nw - 1) * word_cols(BY16), group_of(BY16));
         int tile = t0, b = warp - 2;                           // what is loaded next
-        const uint32_t *lo = nullptr, *hi = nullptr;
+        const uint32_t* at[4] = {};
         auto place = [&]() {
             while (tile < t1 && b >= nkb) {
                 b -= nkb;
@@ -354,24 +355,27 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
             }
             if (tile >= t1) return;
             const int u = tile / each, r0 = (tile - u * each) * per;
-            const uint32_t* const at = S + unit[u] * expert_rows;
+            const uint32_t* const base = S + unit[u] * expert_rows;
             // (a row past the end is the last one again: its results are not written)
-            lo = at + min(r0 + lane, rows - 1);
-            hi = gated ? lo + half : at + min(r0 + BOXROWS + lane, rows - 1);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                at[c] = base + (gated ? min(r0 + 32 * (c & 1) + lane, rows - 1) + (c >> 1) * half : min(r0 + 32 * c + lane, rows - 1));
         };
-        auto load = [&](uint2 (&v)[C::WORDS]) {
+        auto load = [&](uint4 (&v)[C::WORDS]) {
             if (tile >= t1) return false;
 #pragma unroll
             for (int w = 0; w < C::WORDS; ++w) {
                 const int word = b * C::WORDS + w;
-                v[w] = make_uint2(load_word(lo + word * lds, word < nw), load_word(hi + word * lds, word < nw));
+                const int64_t off = word * lds;
+                v[w] = make_uint4(load_word(at[0] + off, word < nw), load_word(at[1] + off, word < nw), load_word(at[2] + off, word < nw),
+                                  load_word(at[3] + off, word < nw));
             }
             if ((b += 2) >= nkb) place();
             return true;
         };
         uint32_t it = (uint32_t)(warp - 2);
         int kb = warp - 2;
-        auto put = [&](uint2 (&v)[C::WORDS]) {
+        auto put = [&](uint4 (&v)[C::WORDS]) {
             while (kb >= nkb) kb -= nkb;
             const uint32_t st = it % (uint32_t)STAGES, ph = it / (uint32_t)STAGES & 1u;
             mbar_wait_suspend(bar_empty(st), ph ^ 1u, abort_flag, p.status);
@@ -379,8 +383,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
 #pragma unroll
             for (int w = 0; w < C::WORDS; ++w) {
                 const uint32_t mask = kb * C::WORDS + w == nw - 1 ? last_mask : 0xFFFFFFFFu;
-                sts32(dst + (uint32_t)(w * ATOM), (int)(v[w].x & mask));
-                sts32(dst + (uint32_t)(w * ATOM + 4), (int)(v[w].y & mask));
+                sts128(dst + (uint32_t)(w * ATOM), make_uint4(v[w].x & mask, v[w].y & mask, v[w].z & mask, v[w].w & mask));
             }
             fence_async_smem();
             __syncwarp();
@@ -389,19 +392,16 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
             kb += 2;
         };
         place();
-        uint2 v0[C::WORDS], v1[C::WORDS], v2[C::WORDS];
-        bool h0 = load(v0), h1 = load(v1), h2 = load(v2);
+        uint4 v0[C::WORDS], v1[C::WORDS];
+        bool h0 = load(v0), h1 = load(v1);
         while (h0 && !lds32(abort_flag)) {
             put(v0);
             h0 = load(v0);
             if (!h1) break;
             put(v1);
             h1 = load(v1);
-            if (!h2) break;
-            put(v2);
-            h2 = load(v2);
         }
-    } else if (warp < 6) {
+    } else if (warp < 8) {
         // ------------------------------------------------------------ epilogue
         const int h = warp - 4;
         uint32_t acc = 0, aph = 0;
@@ -436,17 +436,18 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
 #pragma unroll
             for (int n = 0; n < NTOK; ++n) v[n] *= (BY16 ? row_factor[(u & 3) * 8 + n] : 1.0f) * f;
             if (gated) {
-                if (h == 1) {
+                const int r = 32 * (h & 1) + lane;
+                if (h >= 2) {
 #pragma unroll
-                    for (int n = 0; n < NTOK; ++n) exchange[n * 32 + lane] = v[n];
+                    for (int n = 0; n < NTOK; ++n) exchange[n * BOXROWS + r] = v[n];
                 }
-                asm volatile("bar.sync 2, 64;" ::: "memory");
-                if (h == 0 && r0 + lane < rows) {
+                asm volatile("bar.sync 2, 128;" ::: "memory");
+                if (h < 2 && r0 + r < rows) {
 #pragma unroll
                     for (int n = 0; n < NTOK; ++n)
-                        if (n < count) L.hidden[(int64_t)order[begin + n] * p.H + r0 + lane] = v[n] / (1.0f + expf(-v[n])) * exchange[n * 32 + lane];
+                        if (n < count) L.hidden[(int64_t)order[begin + n] * p.H + r0 + r] = v[n] / (1.0f + expf(-v[n])) * exchange[n * BOXROWS + r];
                 }
-                asm volatile("bar.sync 2, 64;" ::: "memory");
+                asm volatile("bar.sync 2, 128;" ::: "memory");
             } else {
                 const int r = r0 + 32 * h + lane;
                 // (kernel 2: the counter of the tile two before has been taken)
@@ -466,12 +467,12 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 if (lane == 0) mbar_arrive(bar_done(tile - t0 & 1));
             }
         }
-    } else if (warp < 8) {
+    } else if (warp < ACT0) {
         // ------------------------------------------------------------ counters
         // each warp every other tile: which tiles are the last of their columns
         if (DOWN) {
             f8::wait_for_predecessor();                        // the counters' zeros
-            for (int i = warp - 6; i < t1 - t0 && !lds32(abort_flag); i += 2) {
+            for (int i = warp - 8; i < t1 - t0 && !lds32(abort_flag); i += 2) {
                 mbar_wait_suspend(bar_done(i & 1), (uint32_t)i >> 1 & 1u, abort_flag, p.status);
                 if (lane == 0) {
                     __threadfence();
@@ -483,7 +484,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 __syncwarp();
             }
         }
-    } else if (warp >= ACT0) {
+    } else {
         // ------------------------------------------------------------ activations
         if (DOWN) f8::wait_for_predecessor();                  // the hidden values
         const int me = warp - ACT0;
@@ -501,13 +502,13 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 if (BY16) {
                     // the rows' largest values
                     if (me == 0 && lane < 8) row_max[lane] = 0;
-                    asm volatile("bar.sync 3, 512;" ::: "memory");
+                    asm volatile("bar.sync 3, 448;" ::: "memory");
 #pragma unroll 1
                     for (int i = me; i < items; i += ACTS) {
                         const uint32_t a = __reduce_max_sync(0xFFFFFFFFu, largest(value(i)));
                         if (lane == 0) atomicMax(row_max + i % count, a);
                     }
-                    asm volatile("bar.sync 3, 512;" ::: "memory");
+                    asm volatile("bar.sync 3, 448;" ::: "memory");
                 }
                 // biased exponent of a row's factor: its largest group's scale is e4m3's 2^8
                 auto row_exponent = [&](int n) {
@@ -529,7 +530,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_act(ab));
-                if (BY16) asm volatile("bar.sync 3, 512;" ::: "memory");       // row_max has been read
+                if (BY16) asm volatile("bar.sync 3, 448;" ::: "memory");       // row_max has been read
                 if (++ab == (uint32_t)L.bufs) { ab = 0; abph ^= 1u; }
             }
         };
@@ -580,7 +581,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
 
 constexpr int SMEM_MOST = 232448;
 
-// Stages and units whose parts are held: two where six stages fit beside them, else one; {0, 0}: none.
+// Stages and units whose parts are held: two where four stages fit beside them, else one; {0, 0}: none.
 struct Room { int stages, bufs; };
 template <bool BY16, int NTOK> static Room room_for(int K)
 {
@@ -589,7 +590,7 @@ template <bool BY16, int NTOK> static Room room_for(int K)
     for (int bufs = 2; bufs >= 1; --bufs) {
         int stages = (SMEM_MOST - C::bytes(0, bufs, nkb)) / (C::STAGE + C::ATOMS);
         if (stages > MAX_STAGES) stages = MAX_STAGES;
-        if (stages >= (bufs == 2 ? 6 : 4)) return {stages, bufs};
+        if (stages >= (bufs == 2 ? 4 : 3)) return {stages, bufs};
     }
     return {0, 0};
 }
