@@ -51,7 +51,7 @@ template <bool BY16, int NTOK> struct LayerCfg {
     static constexpr int N = 8 * NTOK;                         // columns of a tile (PARTS * NTOK, a multiple of 16)
     static constexpr int STAGE = TROWS * ROWB, ATOMS = WORDS * ATOM;
     static constexpr int BLOCK = N * ROWB + ATOMS;             // parts of 256 depth values, and their scales
-    static constexpr int LISTS = MAX_PAIRS * 2 * 3 + (Q4_MAX_EXPERTS + 32) * 4 * 2;
+    static constexpr int LISTS = MAX_PAIRS * 2 * 4 + (Q4_MAX_EXPERTS + 32) * 4 * 2;
     static constexpr int REST = 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4 + (2 * MAX_STAGES + 12) * 8 + 8 + MAX_TILES / 8;
     static constexpr int COL_SCALE = 2 * N;                    // tensor memory: two accumulators, two buffers of scales
     static constexpr int COLS = 256;
@@ -75,15 +75,16 @@ template <int N, int THREADS>
 __device__ __forceinline__ int sort_pairs(const LayerParams& p, uint16_t* order, uint16_t* rank, uint16_t* unit, int* first, int* units)
 {
     const int n = p.tokens * p.topk, lane = threadIdx.x & 31, padded = (p.E + 31) & ~31;
+    uint16_t* const expert = unit + MAX_PAIRS;                 // of each pair
     for (int i = threadIdx.x; i < n; i += THREADS) {
         const unsigned e = (unsigned)__ldg(p.ids + i);
-        unit[i] = (uint16_t)(e < (unsigned)p.E ? e : 0xFFFFu);              // (experts, until the units are known)
+        expert[i] = (uint16_t)(e < (unsigned)p.E ? e : 0xFFFFu);
     }
     for (int e = threadIdx.x; e < padded; e += THREADS) first[e] = 0;
     __syncthreads();
     if (threadIdx.x < 32) {
         for (int i0 = 0; i0 < n; i0 += 32) {
-            const int i = i0 + lane, e = i < n ? unit[i] : 0xFFFF;
+            const int i = i0 + lane, e = i < n ? expert[i] : 0xFFFF;
             const bool in = e != 0xFFFF;
             const unsigned same = __match_any_sync(0xFFFFFFFFu, e), before = same & ((1u << lane) - 1u);
             const int have = in ? first[e] : 0;
@@ -116,10 +117,9 @@ __device__ __forceinline__ int sort_pairs(const LayerParams& p, uint16_t* order,
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += THREADS) {
-        const int e = unit[i];
+        const int e = expert[i];
         if (e != 0xFFFF) order[first[e] + rank[i]] = (uint16_t)i;
     }
-    __syncthreads();
     for (int e = threadIdx.x; e < p.E; e += THREADS)
         for (int u = units[e]; u < units[e + 1]; ++u) unit[u] = (uint16_t)e;
     __syncthreads();
@@ -494,19 +494,32 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
             uint32_t ab = 0, abph = 0;
             for (int u = u0; u <= u1; ++u) {                    // (no way out: the warps meet)
                 const int e = unit[u], begin = first[e] + (u - units[e]) * NTOK, count = min(NTOK, first[e + 1] - begin);
-                const int items = count * nkb;                 // 256 values of a pair each: pair i % count, block i / count
-                auto value = [&](int i) {
-                    const int n = i % count;
-                    return eight_at(static_cast<const T*>(src) + (int64_t)(order[begin + n] / div) * ld, i / count * STAGE_K + lane * 8, K);
+                // 256 values of a pair each: pair n, block b; every ACTS-th from mine on
+                const int dn = ACTS % count, db = ACTS / count, n0 = me % count, b0 = me / count;
+                auto value = [&](int n, int b) {
+                    return eight_at(static_cast<const T*>(src) + (int64_t)(order[begin + n] / div) * ld, b * STAGE_K + lane * 8, K);
                 };
+                auto step = [&](int& n, int& b) {
+                    n += dn;
+                    b += db;
+                    if (n >= count) {
+                        n -= count;
+                        ++b;
+                    }
+                };
+                f8::Eight<T> v;
+                if (b0 < nkb) v = value(n0, b0);
                 if (BY16) {
                     // the rows' largest values
                     if (me == 0 && lane < 8) row_max[lane] = 0;
                     asm volatile("bar.sync 3, 448;" ::: "memory");
+                    f8::Eight<T> w = v;
 #pragma unroll 1
-                    for (int i = me; i < items; i += ACTS) {
-                        const uint32_t a = __reduce_max_sync(0xFFFFFFFFu, largest(value(i)));
-                        if (lane == 0) atomicMax(row_max + i % count, a);
+                    for (int n = n0, b = b0; b < nkb;) {
+                        const uint32_t a = __reduce_max_sync(0xFFFFFFFFu, largest(w));
+                        if (lane == 0) atomicMax(row_max + n, a);
+                        step(n, b);
+                        if (b < nkb) w = value(n, b);
                     }
                     asm volatile("bar.sync 3, 448;" ::: "memory");
                 }
@@ -516,15 +529,14 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                     return (m >= 0x7F800000u ? 127u : max(m >> 23, 20u)) - 9u;
                 };
                 if (BY16 && me == 0 && lane < count) row_factor[(u & 3) * 8 + lane] = __uint_as_float(row_exponent(lane) << 23);
-                f8::Eight<T> v;
-                if (me < items) v = value(me);
                 mbar_wait_suspend(bar_used(ab), abph ^ 1u, abort_flag, p.status);
 #pragma unroll 1
-                for (int i = me; i < items; i += ACTS) {
-                    const int n = i % count, at = ab * nkb + i / count;
+                for (int n = n0, b = b0; b < nkb;) {
+                    const int row = n, at = ab * nkb + b;
                     const f8::Eight<T> now = v;
-                    if (i + ACTS < items) v = value(i + ACTS);
-                    put_parts<BY16, NTOK>(now, n, BY16 ? row_exponent(n) : 0u, act_s + (uint32_t)(at * C::N * ROWB),
+                    step(n, b);
+                    if (b < nkb) v = value(n, b);
+                    put_parts<BY16, NTOK>(now, row, BY16 ? row_exponent(row) : 0u, act_s + (uint32_t)(at * C::N * ROWB),
                                           act_atoms + (uint32_t)(at * C::ATOMS), lane);
                 }
                 fence_async_smem();
