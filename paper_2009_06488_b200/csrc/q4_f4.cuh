@@ -128,6 +128,8 @@ __device__ __forceinline__ float load_value(const void* base, int64_t at, int ty
 cudaError_t launch_f4_quantize(const f4::QuantizeParams& p, int x_type, bool by16, cudaStream_t st);
 cudaError_t launch_f4_dequantize(const f4::DequantizeParams& p, int y_type, bool by16, cudaStream_t st);
 cudaError_t launch_gemm_f4_simt(const f4::GemmParams& p, bool by16, cudaStream_t st);
+bool        gemm_f4_few_supported(const f4::GemmParams& p);
+q4_status   launch_gemm_f4_few(const f4::GemmParams& p, bool by16, cudaStream_t st);
 bool        gemm_f4_pair_supported(const f4::GemmParams& p);
 q4_status   launch_gemm_f4_pair(const f4::GemmParams& p, bool by16, cudaStream_t st);
 bool        expert_layer_f4_stream_supported(const f4::LayerParams& p, bool by16);

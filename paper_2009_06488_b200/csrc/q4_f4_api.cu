@@ -29,7 +29,12 @@ q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* 
         !aligned(p.C, f8::type_size(p.c_type))) return Q4_ERR_ALIGNMENT;
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
-    if (kernel_variant() != 1 && gemm_f4_pair_supported(p)) {
+    const int variant = kernel_variant();
+    if ((variant == 0 || variant == 3) && gemm_f4_few_supported(p)) {
+        log_choice(call, "few-rows kernel");
+        return launch_gemm_f4_few(p, by16, stream_of(stream));
+    }
+    if (variant != 1 && gemm_f4_pair_supported(p)) {
         log_choice(call, "CTA-pair tcgen05 kernel");
         return launch_gemm_f4_pair(p, by16, stream_of(stream));
     }

@@ -50,75 +50,6 @@ struct PairParams {
     int32_t c_vec;                   // rows of C begin on multiples of 16 bytes (and tmC is valid)
 };
 
-struct Tile {
-    int m0, m_end;                   // first row of the pair's tile and end of its segment
-    int n0;                          // first column
-    int64_t brow;                    // its row of Bt
-    int e;                           // expert
-};
-
-// The walk over the tiles.  Called by whole warps: an expert's segment is found 32 experts at a time.
-template <int BN>
-struct Walk {
-    const PairParams& p;
-    int lane;
-    int e0 = 0, cum = 0, lo = 0, hi = 0, incl = 0;
-    __device__ Walk(const PairParams& p_, int lane_) : p(p_), lane(lane_)
-    {
-        if (p.g.E) load();
-    }
-    __device__ void load()
-    {
-        const int e = e0 + lane;
-        lo = hi = 0;
-        if (e < p.g.E) {
-            lo = clamp_to(p.g.starts[e], 0, p.g.M);
-            hi = clamp_to(p.g.starts[e + 1], lo, p.g.M);
-        }
-        incl = (hi - lo + 255) / 256 * p.tiles_n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += u;
-        }
-    }
-    __device__ bool get(int t, Tile& o)
-    {
-        const GemmParams& g = p.g;
-        if (g.E) {
-            int total = __shfl_sync(0xFFFFFFFFu, incl, 31);
-            while (t >= cum + total) {
-                if (e0 + 32 >= g.E) return false;
-                cum += total;
-                e0 += 32;
-                load();
-                total = __shfl_sync(0xFFFFFFFFu, incl, 31);
-            }
-            const int i = __popc(__ballot_sync(0xFFFFFFFFu, t - cum >= incl));
-            const int before = i ? __shfl_sync(0xFFFFFFFFu, incl, i - 1) : 0;
-            const int s = __shfl_sync(0xFFFFFFFFu, lo, i), end = __shfl_sync(0xFFFFFFFFu, hi, i);
-            const int tm = (end - s + 255) / 256;
-            const int local = t - cum - before, n = local / tm;        // row tiles fastest: they share the weights
-            o.m0 = s + (local - n * tm) * 256;
-            o.m_end = end;
-            o.n0 = n * BN;
-            o.e = e0 + i;
-            o.brow = (int64_t)o.e * g.N + o.n0;
-            return true;
-        }
-        if (t >= p.tiles_m * p.tiles_n) return false;
-        // bands of eight row tiles: the tiles in flight at a time share rows of both operands
-        const int band = t / (8 * p.tiles_n), r = t - band * 8 * p.tiles_n;
-        const int h = min(8, p.tiles_m - band * 8), n = r / h;
-        o.m0 = (band * 8 + r - n * h) * 256;
-        o.m_end = g.M;
-        o.n0 = n * BN;
-        o.e = 0;
-        o.brow = o.n0;
-        return true;
-    }
-};
-
 // A slice (32 rows x 128 bytes, its 16-byte pieces swizzled by the row) to rows of C by pieces: `rows` of them, `cols`
 // columns (any number) from dst on, pitch in elements.
 template <typename U>
@@ -204,7 +135,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // every role waits for the kernel before ahead of its first access to global memory and of its first bounded wait
     f8::wait_for_predecessor();
 
-    Walk<BN> walk(p, lane);
+    Walk<256, BN> walk(p.g, p.tiles_m, p.tiles_n, lane);
     Tile t;
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
@@ -267,80 +198,37 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
     } else if (warp < 8) {
         // ------------------------------------------------------------ scales
-        // A team of warps takes a stage, teams in turn: one warp the words of A, one for each 128 rows of Bt.  The words of
-        // a team's next three stages are under way.  The wait for a team's stage before told that the stages up to
-        // STAGES + TEAMS back are consumed, so the parity waited for cannot be that of an older round.
+        // of a team's warps one brings the words of A, one each those of 128 rows of Bt
         const int part = (warp - 2) % C::PARTS, team = (warp - 2) / C::PARTS;
         const uint32_t full_leader = map_to_cta(bar_full(0), 0);
-        const int64_t ld = part ? g.ldsb : g.ldsa;
-        const int nw = (int)words_of(g.K, BY16);
-        const uint32_t last_mask = valid_bytes(g.K - (nw - 1) * word_cols(BY16), group_of(BY16));
-        int tile = cluster_id, b = team;                       // what is loaded next: block b of the tile
-        const uint32_t* src = nullptr;
-        bool in[4];
+        int tile = cluster_id, b = team;
         bool more = walk.get(tile, t);
-        auto place = [&]() {
-            const int row0 = t.m0 + (int)rank * TMC, rows = part ? g.N - t.n0 - 128 * (part - 1) : t.m_end - row0;
-            src = (part ? g.SB + t.brow + 128 * (part - 1) : g.SA + row0) + lane;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) in[c] = lane + 32 * c < rows;
-        };
-        auto settle = [&]() {                                  // b may lie past the tile's end
-            if (more && b >= nkb) {
-                do {
+        bring_scales<C::WORDS, BY16, C::STAGES, C::TEAMS>(team, g.K, abort_flag,
+            [&](const uint32_t*& src, int64_t& ld, int& rows, int& word0) {
+                while (more && b >= nkb) {
                     b -= nkb;
                     more = walk.get(tile += nclusters, t);
-                } while (more && b >= nkb);
-                if (more) place();
-            }
-        };
-        auto load = [&](uint4 (&v)[C::WORDS]) {                // the next stage's; false: there is none
-            if (!more) return false;
-#pragma unroll
-            for (int w = 0; w < C::WORDS; ++w) {
-                const int word = b * C::WORDS + w;
-                const uint32_t* at = src + word * ld;
-                v[w] = make_uint4(load_word(at, in[0] && word < nw), load_word(at + 32, in[1] && word < nw),
-                                  load_word(at + 64, in[2] && word < nw), load_word(at + 96, in[3] && word < nw));
-            }
-            b += C::TEAMS;
-            settle();
-            return true;
-        };
-        uint32_t it = (uint32_t)team, kb = (uint32_t)team;     // the stage that is written next, its block in its tile
-        auto put = [&](uint4 (&v)[C::WORDS]) {
-            while (kb >= (uint32_t)nkb) kb -= (uint32_t)nkb;
-            if ((int)(kb + 1) * C::WORDS >= nw) {
+                }
+                if (!more) return false;
+                const int row0 = t.m0 + (int)rank * TMC;
+                src = (part ? g.SB + t.brow + 128 * (part - 1) : g.SA + row0) + lane;
+                ld = part ? g.ldsb : g.ldsa;
+                rows = (part ? g.N - t.n0 - 128 * (part - 1) : t.m_end - row0) - lane;
+                word0 = b * C::WORDS;
+                b += C::TEAMS;
+                return true;
+            },
+            [&](uint32_t it, const uint4 (&v)[C::WORDS]) {
+                const uint32_t st = it % C::STAGES, ph = it / C::STAGES & 1u;
+                mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
+                const uint32_t dst = sbase + st * C::STAGE + (TMC + C::BSH) * ROWB + (uint32_t)lane * 16u;
 #pragma unroll
                 for (int w = 0; w < C::WORDS; ++w)
-                    if ((int)kb * C::WORDS + w == nw - 1) v[w] = make_uint4(v[w].x & last_mask, v[w].y & last_mask, v[w].z & last_mask, v[w].w & last_mask);
-            }
-            const uint32_t st = it % C::STAGES, ph = it / C::STAGES & 1u;
-            mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
-            const uint32_t dst = sbase + st * C::STAGE + (TMC + C::BSH) * ROWB + (uint32_t)lane * 16u;
-#pragma unroll
-            for (int w = 0; w < C::WORDS; ++w)
-                sts128(dst + (uint32_t)((part ? C::WORDS + w * C::BATOMS + part - 1 : w) * ATOM), v[w]);
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster_relaxed(full_leader + 8u * st);
-            it += C::TEAMS;
-            kb += C::TEAMS;
-        };
-        if (more) place();
-        settle();
-        uint4 v0[C::WORDS], v1[C::WORDS], v2[C::WORDS];
-        bool h0 = load(v0), h1 = load(v1), h2 = load(v2);
-        while (h0 && !lds32(abort_flag)) {
-            put(v0);
-            h0 = load(v0);
-            if (!h1) break;
-            put(v1);
-            h1 = load(v1);
-            if (!h2) break;
-            put(v2);
-            h2 = load(v2);
-        }
+                    sts128(dst + (uint32_t)((part ? C::WORDS + w * C::BATOMS + part - 1 : w) * ATOM), v[w]);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster_relaxed(full_leader + 8u * st);
+            });
     } else {
         // ------------------------------------------------------------ epilogue
         const int lg = warp & 3, set = warp >= 12 ? 1 : 0;

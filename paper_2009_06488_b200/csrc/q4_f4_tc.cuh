@@ -87,5 +87,125 @@ __device__ __forceinline__ void tc_wait_ld32(uint32_t (&r)[32])
                  :: "memory");
 }
 
+__device__ __forceinline__ void tc_wait_ld16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
+}
+
+struct Tile {
+    int m0, m_end;                   // first row and end of its segment
+    int n0;                          // first column
+    int64_t brow;                    // its row of Bt
+    int e;                           // expert
+};
+
+// The walk over tiles of TR rows x TN columns.  Called by whole warps: an expert's segment is found 32 experts at a time.
+template <int TR, int TN>
+struct Walk {
+    const GemmParams& g;
+    int tiles_m, tiles_n, lane;
+    int e0 = 0, cum = 0, lo = 0, hi = 0, incl = 0;
+    __device__ Walk(const GemmParams& g_, int tiles_m_, int tiles_n_, int lane_) : g(g_), tiles_m(tiles_m_), tiles_n(tiles_n_), lane(lane_)
+    {
+        if (g.E) load();
+    }
+    __device__ void load()
+    {
+        const int e = e0 + lane;
+        lo = hi = 0;
+        if (e < g.E) {
+            lo = clamp_to(g.starts[e], 0, g.M);
+            hi = clamp_to(g.starts[e + 1], lo, g.M);
+        }
+        incl = (hi - lo + TR - 1) / TR * tiles_n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += u;
+        }
+    }
+    __device__ bool get(int t, Tile& o)
+    {
+        if (g.E) {
+            int total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+            while (t >= cum + total) {
+                if (e0 + 32 >= g.E) return false;
+                cum += total;
+                e0 += 32;
+                load();
+                total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+            }
+            const int i = __popc(__ballot_sync(0xFFFFFFFFu, t - cum >= incl));
+            const int before = i ? __shfl_sync(0xFFFFFFFFu, incl, i - 1) : 0;
+            const int s = __shfl_sync(0xFFFFFFFFu, lo, i), end = __shfl_sync(0xFFFFFFFFu, hi, i);
+            const int tm = (end - s + TR - 1) / TR;
+            const int local = t - cum - before, n = local / tm;        // row tiles fastest: they share the weights
+            o.m0 = s + (local - n * tm) * TR;
+            o.m_end = end;
+            o.n0 = n * TN;
+            o.e = e0 + i;
+            o.brow = (int64_t)o.e * g.N + o.n0;
+            return true;
+        }
+        if (t >= tiles_m * tiles_n) return false;
+        // bands of eight row tiles: the tiles in flight at a time share rows of both operands
+        const int band = t / (8 * tiles_n), r = t - band * 8 * tiles_n;
+        const int h = min(8, tiles_m - band * 8), n = r / h;
+        o.m0 = (band * 8 + r - n * h) * TR;
+        o.m_end = g.M;
+        o.n0 = n * TN;
+        o.e = 0;
+        o.brow = o.n0;
+        return true;
+    }
+};
+
+// What brings words of scales to atoms: a team of PARTS warps takes a stage, TEAMS teams in turn, a team's next three stages
+// under way.  The wait for a team's stage before told that the stages up to STAGES + TEAMS back are consumed, so the
+// parity waited for cannot be that of an older round.  Place: moves to stage (the team's next) and says where this
+// warp's words are; false: there is none.
+template <int WORDS, bool BY16, int STAGES, int TEAMS, typename Place, typename Put>
+__device__ __forceinline__ void bring_scales(int team, int K, uint32_t abort_flag, Place&& place, Put&& put)
+{
+    const int nw = (int)words_of(K, BY16);
+    const uint32_t last_mask = valid_bytes(K - (nw - 1) * word_cols(BY16), group_of(BY16));
+    struct Stage { uint4 v[WORDS]; };
+    uint32_t it = (uint32_t)team;
+    auto load = [&](Stage& s) {
+        const uint32_t* src;
+        int64_t ld;
+        int rows, word0;                                       // rows: that exist from my lane's first on, 32 apart
+        if (!place(src, ld, rows, word0)) return false;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            const uint32_t* at = src + (word0 + w) * ld;
+            const bool in = word0 + w < nw;
+            const uint32_t mask = word0 + w == nw - 1 ? last_mask : 0xFFFFFFFFu;
+            s.v[w] = make_uint4(load_word(at, in && rows > 0), load_word(at + 32, in && rows > 32), load_word(at + 64, in && rows > 64),
+                                load_word(at + 96, in && rows > 96));
+            if (mask != 0xFFFFFFFFu) s.v[w] = make_uint4(s.v[w].x & mask, s.v[w].y & mask, s.v[w].z & mask, s.v[w].w & mask);
+        }
+        return true;
+    };
+    Stage a, b, c;
+    bool ha = load(a), hb = load(b), hc = load(c);
+    while (ha && !lds32(abort_flag)) {
+        put(it, a.v);
+        it += TEAMS;
+        ha = load(a);
+        if (!hb) break;
+        put(it, b.v);
+        it += TEAMS;
+        hb = load(b);
+        if (!hc) break;
+        put(it, c.v);
+        it += TEAMS;
+        hc = load(c);
+    }
+}
+
 }  // namespace f4
 }  // namespace q4

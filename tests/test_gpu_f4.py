@@ -233,6 +233,55 @@ def test_product(q4, by16, M, N, K):
 
 
 @pytest.mark.parametrize("by16", [False, True])
+@pytest.mark.parametrize("M,N,K", [(2304, 2310, 320), (2500, 2048, 1030), (130, 40, 4096), (300, 9500, 256)])
+def test_product_on_wide_tiles(q4, by16, M, N, K):
+    a, sa, va = operand(M + K, M, K, by16)
+    b, sb, vb = operand(N + K + 1, N, K, by16)
+    want, mag = f4.product(va, vb)
+    import torch
+    for t, pad in (("bf16", 2), ("f32", 0)):
+        buf = torch.full((M, N + pad), 9.0, dtype=types()[t], device="cuda")
+        q4.q4_gemm_f4(placed(a, up16(a.shape[1])), word_tensor(sa), placed(b, up16(b.shape[1])), word_tensor(sb, 1), buf[:, :N], M, N, K, by16=by16)
+        check(buf[:, :N], want, mag, K, t)
+        assert (buf[:, N:] == 9).all()
+
+
+@pytest.mark.parametrize("by16", [False, True])
+@pytest.mark.parametrize("M", [1, 5, 16, 17, 40, 64, 90, 128])
+@pytest.mark.parametrize("N,K", [(300, 2048), (64, 700), (1536, 1100), (20000, 512)])
+def test_few_rows(q4, by16, M, N, K):
+    """Depth in one, two and four parts; every width of the tile; columns that end inside one."""
+    import torch
+    a, sa, va = operand(M + K, M, K, by16)
+    b, sb, vb = operand(N + K + 1, N, K, by16)
+    want, mag = f4.product(va, vb)
+    for t, pad in (("bf16", 3), ("f32", 0)):
+        buf = torch.full((M + 1, N + pad), 9.0, dtype=types()[t], device="cuda")
+        q4.q4_gemm_f4(placed(a, up16(a.shape[1])), word_tensor(sa, 2), placed(b, up16(b.shape[1])), word_tensor(sb), buf[:M, :N], M, N, K, by16=by16)
+        check(buf[:M, :N], want, mag, K, t, extra=4)
+        assert (buf[M:] == 9).all() and (buf[:, N:] == 9).all()
+
+
+@pytest.mark.parametrize("variant", [1, 2])
+def test_every_kernel_gives_the_same_product(q4, variant):
+    """The general kernel and the CTA-pair kernel on rows that the few-rows kernel takes."""
+    import torch
+    for by16 in (False, True):
+        a, sa, va = operand(3, 20, 600, by16)
+        b, sb, vb = operand(4, 3 * 200, 600, by16)
+        starts = np.array([0, 7, 7, 20], dtype=np.int32)
+        want, mag = f4.experts(va, vb, starts, 200)
+        try:
+            q4.q4_set_variant(variant)
+            C = torch.zeros(20, 200, device="cuda")
+            q4.q4_gemm_f4_experts(placed(a, 304), word_tensor(sa), placed(b, 304), word_tensor(sb), torch.from_numpy(starts).cuda(), C, 20, 200,
+                                  600, by16=by16)
+            check(C, want, mag, 600, "f32")
+        finally:
+            q4.q4_set_variant(0)
+
+
+@pytest.mark.parametrize("by16", [False, True])
 @pytest.mark.parametrize("counts,N,K", [([0, 5, 0, 1, 40, 0], 130, 300), ([128, 0, 129, 300], 256, 512), ([2] * 16, 200, 1024),
                                         ([0, 0, 0], 64, 64), ([700], 96, 192), ([1, 0, 0, 0, 0, 0, 0, 0, 1], 640, 257)])
 def test_product_by_experts(q4, by16, counts, N, K):
