@@ -21,6 +21,7 @@ namespace f4 {
 
 constexpr int FEW_THREADS = 12 * 32;
 constexpr int WR = 128;                  // rows of Bt of a tile
+constexpr int MAX_SPLITS = 8;            // parts of the depth
 
 template <int NB, bool BY16> struct FewCfg {
     static constexpr int WORDS = kWords<BY16>;
@@ -30,22 +31,22 @@ template <int NB, bool BY16> struct FewCfg {
     static constexpr int TEAMS = 3;
     static constexpr int COLS = NB <= 64 ? 256 : 512;
     static constexpr int COL_SCALE = 2 * NB;                   // tensor memory: two accumulators, two buffers of scales
-    static constexpr int OFF_PART = STAGES * STAGE;            // SPLIT: partial tile [NB][WR]
-    static constexpr int OFF_BAR = OFF_PART + (NB <= 64 ? NB : 0) * WR * 4;
+    static constexpr int OFF_BAR = STAGES * STAGE;
     static constexpr int OFF_MISC = OFF_BAR + (2 * STAGES + 4) * 8;
     static constexpr int SMEM = OFF_MISC + 16 + 1024;
-    static_assert(STAGE % 1024 == 0 && STAGES >= TEAMS && SMEM <= 232448 && COL_SCALE + 2 * 8 * WORDS <= COLS, "shared or tensor memory");
+    static_assert(NB * WR * 4 <= OFF_BAR && STAGE % 1024 == 0 && STAGES >= TEAMS && SMEM <= 232448 && COL_SCALE + 2 * 8 * WORDS <= COLS, "shared or tensor memory");
 };
 
 struct FewParams {
     GemmParams g;
     int32_t tiles_m, tiles_n, splits;
+    int32_t c_vec;                   // four values of C at a time are aligned
 };
 
-__device__ __forceinline__ float lds_cluster(uint32_t a)
+__device__ __forceinline__ float4 lds128_cluster(uint32_t a)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
     return v;
 }
 
@@ -187,9 +188,10 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 tc_wait_ld16(r);
                 const int64_t at = (int64_t)(t.m0 + j0) * g.ldc + n;
                 if (SPLIT) {
+                    // partial tile [NB][WR] over the stages, which nothing reads or fills any more: this part's blocks are all multiplied
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        sts32(sbase + C::OFF_PART + 4u * (uint32_t)((j0 + j) * WR + 32 * h + lane), nkb ? (int)r[j] : 0);
+                        sts32(sbase + 4u * (uint32_t)((j0 + j) * WR + 32 * h + lane), nkb ? (int)r[j] : 0);
                 } else if (n < g.N) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
@@ -214,12 +216,38 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         // one tile per cluster: each CTA adds its share of the rows of all partial tiles, in order
         if (walk.get(first, t)) {
             const float f = (g.FA ? __ldg(g.FA) : 1.0f) * (g.FB ? __ldg(g.FB + t.e) : 1.0f);
-            const int rows = min(NB, t.m_end - t.m0), n = (int)threadIdx.x & 127;
-            for (int m = split + splits * ((int)threadIdx.x >> 7); m < rows; m += 3 * splits) {
-                float v = 0.0f;
-                for (int s = 0; s < splits; ++s)
-                    v += lds_cluster(map_to_cta(sbase + C::OFF_PART + 4u * (uint32_t)(m * WR + n), (uint32_t)s));
-                if (t.n0 + n < g.N) store_value(g.C, (int64_t)(t.m0 + m) * g.ldc + t.n0 + n, g.c_type, v * f);
+            const int rows = min(NB, t.m_end - t.m0), lo = rows * split / splits, hi = rows * (split + 1) / splits;
+            const int n = t.n0 + 4 * lane, have = min(4, g.N - n);
+            for (int m = lo + warp; m < hi; m += FEW_THREADS / 32) {
+                float4 q[MAX_SPLITS];
+#pragma unroll
+                for (int s = 0; s < MAX_SPLITS; ++s) {
+                    q[s] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (s < splits) q[s] = lds128_cluster(map_to_cta(sbase + (uint32_t)((m * WR + 4 * lane) * 4), (uint32_t)s));
+                }
+                float v[4] = {};
+#pragma unroll
+                for (int s = 0; s < MAX_SPLITS; ++s) {
+                    v[0] += q[s].x;
+                    v[1] += q[s].y;
+                    v[2] += q[s].z;
+                    v[3] += q[s].w;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] *= f;
+                const int64_t at = (int64_t)(t.m0 + m) * g.ldc + n;
+                if (p.c_vec && have == 4) {
+                    if (g.c_type == Q4_F32)
+                        *reinterpret_cast<float4*>(static_cast<float*>(g.C) + at) = make_float4(v[0], v[1], v[2], v[3]);
+                    else
+                        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.C) + at) =
+                            g.c_type == Q4_BF16 ? make_uint2(f8::pack2(v[0], v[1], (const __nv_bfloat16*)nullptr), f8::pack2(v[2], v[3], (const __nv_bfloat16*)nullptr))
+                                                : make_uint2(f8::pack2(v[0], v[1], (const __half*)nullptr), f8::pack2(v[2], v[3], (const __half*)nullptr));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < have) store_value(g.C, at + j, g.c_type, v[j]);
+                }
             }
         }
         cluster_sync_all();                  // the partial tiles have been read
@@ -266,39 +294,50 @@ static q4_status launch_few(FewParams& p, int64_t tiles, cudaStream_t st)
 template <int NB, bool BY16>
 static q4_status launch_nb(FewParams& p, int64_t tiles, cudaStream_t st)
 {
-    if constexpr (NB <= 64) {
-        if (p.splits > 1) return launch_few<NB, BY16, true>(p, tiles, st);
-    }
-    p.splits = 1;
-    return launch_few<NB, BY16, false>(p, tiles, st);
+    return p.splits > 1 ? launch_few<NB, BY16, true>(p, tiles, st) : launch_few<NB, BY16, false>(p, tiles, st);
 }
 
 }  // namespace f4
 
 using namespace f4;
 
+// Parts of the depth of a dense product of `tiles` tiles: twice as many while the clusters fit the device at once (a cluster
+// lies within a GPC, so 33 of four CTAs and 15 of eight fit where 148 SMs do) and a part keeps two stages.
+static int few_splits(int64_t tiles, int blocks)
+{
+    int splits = 1;
+    while (splits < MAX_SPLITS && 2 * splits * tiles <= 2 * f8_pairs_of_device() * 8 / 10 + (splits == 1 ? 8 : splits == 2 ? 14 : 2) && blocks >= 4 * splits)
+        splits *= 2;
+    return splits;
+}
+
+// Where it pays: by experts up to 64 rows per expert on average; one product up to 128 rows, and more while its tiles are so
+// few that the depth in parts saves more (500 clk per stage that another part takes) than the exchange costs (300 x 300 x
+// 2000 6.5 us against 7.6 on pairs, 500 x 500 x 2048 6.5 against 7.2, 200 x 250 x 1024 6.5 against 6.0).
 bool gemm_f4_few_supported(const f4::GemmParams& g)
 {
     if ((uintptr_t)g.A % 16 || (uintptr_t)g.Bt % 16 || g.lda % 16 || g.ldb % 16) return false;
     if (g.M >= INT32_MAX - 512 || (int64_t)g.N * (g.E ? g.E : 1) >= INT32_MAX - 512) return false;
-    return g.E ? g.M <= 64 * (int64_t)g.E : g.M <= 128;
+    if (g.E) return g.M <= 64 * (int64_t)g.E;
+    if (g.M <= 128) return true;
+    const int64_t tiles = ((int64_t)g.M + 127) / 128 * (((int64_t)g.N + WR - 1) / WR);
+    const int blocks = (g.K + STAGE_K - 1) / STAGE_K, splits = few_splits(tiles, blocks);
+    return tiles <= 16 && (blocks - (blocks + splits - 1) / splits) * 500 > 2500;
 }
 
 q4_status launch_gemm_f4_few(const f4::GemmParams& g, bool by16, cudaStream_t st)
 {
     FewParams p{};
     p.g = g;
+    const size_t es = f8::type_size(g.c_type);
+    p.c_vec = (uintptr_t)g.C % (4 * es) == 0 && g.ldc % 4 == 0;
     // columns: what holds the rows, or twice an expert's average
     const int64_t want = g.E ? 2 * ((int64_t)g.M / g.E) : g.M;
     const int nb = want <= 16 ? 16 : want <= 32 ? 32 : want <= 64 ? 64 : 128;
     p.tiles_m = (int)(((int64_t)g.M + nb - 1) / nb);
     p.tiles_n = (int)(((int64_t)g.N + WR - 1) / WR);
     const int64_t tiles = (p.tiles_m + (g.E ? (g.E < g.M ? g.E : g.M) : 0)) * (int64_t)p.tiles_n;
-    // the depth in two or four parts while the clusters fit the device and a part has two stages
-    const int blocks = (g.K + STAGE_K - 1) / STAGE_K;
-    p.splits = 1;
-    if (!g.E)
-        while (p.splits < 4 && 2 * p.splits * tiles <= 2 * f8_pairs_of_device() - 16 && blocks >= 4 * p.splits) p.splits *= 2;
+    p.splits = g.E ? 1 : few_splits(tiles, (g.K + STAGE_K - 1) / STAGE_K);
     switch (nb) {
     case 16: return by16 ? launch_nb<16, true>(p, tiles, st) : launch_nb<16, false>(p, tiles, st);
     case 32: return by16 ? launch_nb<32, true>(p, tiles, st) : launch_nb<32, false>(p, tiles, st);

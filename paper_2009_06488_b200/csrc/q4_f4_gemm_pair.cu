@@ -76,13 +76,23 @@ __device__ __forceinline__ void put_slice(uint32_t slice, U* dst, int64_t pitch,
         }
         return;
     }
-    for (int r = 0; r < rows; ++r)
-        for (int c = lane; c < cols; c += 32) {
-            const int b = c * (int)sizeof(U);
-            const uint32_t at = slice + (uint32_t)(r * 128) + (uint32_t)((((b >> 4) ^ r) & 7) << 4) + (uint32_t)(b & 12);
-            const uint32_t w = (uint32_t)lds32(at);
-            dst[r * pitch + c] = sizeof(U) == 4 ? (U)w : (U)(w >> (8 * (b & 2)));
+    // rows that begin anywhere: by values, a warp's 32 of a row together; those of eight rows are read ahead of their stores
+    for (int c = lane; c < PER; c += 32) {
+        const int b = c * (int)sizeof(U);
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            U v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = r0 + k;
+                const uint32_t w = (uint32_t)lds32(slice + (uint32_t)(r * 128) + (uint32_t)((((b >> 4) ^ r) & 7) << 4) + (uint32_t)(b & 12));
+                v[k] = sizeof(U) == 4 ? (U)w : (U)(w >> (8 * (b & 2)));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c < cols && r0 + k < rows) dst[(r0 + k) * pitch + c] = v[k];
         }
+    }
 }
 
 template <int BN, bool BY16>
@@ -387,7 +397,12 @@ q4_status launch_gemm_f4_pair(const f4::GemmParams& g, bool by16, cudaStream_t s
     const int pairs = f8_pairs_of_device();
     const int64_t n256 = ((int64_t)g.N + 255) / 256, n128 = ((int64_t)g.N + 127) / 128;
     const int64_t tm = p.tiles_m + (g.E ? (g.E < g.M ? g.E : g.M) : 0);          // an expert's last row tile is its own
-    const bool wide = g.N > 128 && tm * n256 >= pairs;
+    // Tile width: clocks of the busiest pair, from measured ones per stage (720 wide, 490 narrow) and tile.  1024 x 4096 x 4096
+    // (64 wide tiles, one round; 128 narrow, two) 11.6 against 12.4 us, 512 x 4096 x 4096 10.6 against 8.7.
+    const int64_t stages = ((int64_t)g.K + STAGE_K - 1) / STAGE_K;
+    const int64_t t_wide = (tm * n256 + pairs - 1) / pairs * (stages * 720 + 3000);
+    const int64_t t_narrow = (tm * n128 + pairs - 1) / pairs * (stages * 490 + 2500);
+    const bool wide = g.N > 128 && t_wide <= t_narrow;
     p.tiles_n = (int)(wide ? n256 : n128);
     const size_t es = f8::type_size(g.c_type);
     p.c_vec = (uintptr_t)g.C % 16 == 0 && g.ldc * es % 16 == 0;
