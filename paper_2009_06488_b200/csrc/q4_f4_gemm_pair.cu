@@ -50,6 +50,13 @@ struct PairParams {
     int32_t c_vec;                   // rows of C begin on multiples of 16 bytes (and tmC is valid)
 };
 
+// A store whose lines leave L2 ahead of the operands', which other tiles read again.
+__device__ __forceinline__ void tma_store_2d_first(const CUtensorMap* tm, uint32_t src, int x, int y, uint64_t policy)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%2, %3}], [%1], %4;"
+                 ::"l"(tm), "r"(src), "r"(x), "r"(y), "l"(policy) : "memory");
+}
+
 // A slice (32 rows x 128 bytes, its 16-byte pieces swizzled by the row) to rows of C by pieces: `rows` of them, `cols`
 // columns (any number) from dst on, pitch in elements.
 template <typename U>
@@ -246,6 +253,8 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         const uint32_t slice = sbase + C::OFF_SLICE + (uint32_t)((warp - 8) * SLICE);
         const uint32_t mine = slice + (uint32_t)(lane * 128), sw = (uint32_t)(lane & 7);
         const float fa = g.FA ? __ldg(g.FA) : 1.0f;
+        uint64_t evict_first;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(evict_first));
         uint32_t acc = 0, aph = 0;
         for (int tile = cluster_id; walk.get(tile, t) && !lds32(abort_flag); tile += nclusters) {
             const int row0 = t.m0 + (int)rank * TMC + lg * 32, c0 = t.n0 + set * CW;
@@ -272,7 +281,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmC, slice, nc, row0);
+                        tma_store_2d_first(&tmC, slice, nc, row0, evict_first);
                         bulk_commit();
                     }
                 } else {
