@@ -172,36 +172,43 @@ __device__ __forceinline__ void bring_scales(int team, int K, uint32_t abort_fla
 {
     const int nw = (int)words_of(K, BY16);
     const uint32_t last_mask = valid_bytes(K - (nw - 1) * word_cols(BY16), group_of(BY16));
-    struct Stage { uint4 v[WORDS]; };
+    struct Stage { uint4 v[WORDS]; int word0; };
+    // (the mask of a matrix's last word is applied when a stage is put: any use of a word at its load would wait for it)
+    auto masked = [&](Stage& s) -> const uint4 (&)[WORDS] {
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            const uint32_t mask = s.word0 + w == nw - 1 ? last_mask : 0xFFFFFFFFu;
+            s.v[w] = make_uint4(s.v[w].x & mask, s.v[w].y & mask, s.v[w].z & mask, s.v[w].w & mask);
+        }
+        return s.v;
+    };
     uint32_t it = (uint32_t)team;
     auto load = [&](Stage& s) {
         const uint32_t* src;
         int64_t ld;
-        int rows, word0;                                       // rows: that exist from my lane's first on, 32 apart
-        if (!place(src, ld, rows, word0)) return false;
+        int rows;                                              // that exist from my lane's first on, 32 apart
+        if (!place(src, ld, rows, s.word0)) return false;
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
-            const uint32_t* at = src + (word0 + w) * ld;
-            const bool in = word0 + w < nw;
-            const uint32_t mask = word0 + w == nw - 1 ? last_mask : 0xFFFFFFFFu;
+            const uint32_t* at = src + (s.word0 + w) * ld;
+            const bool in = s.word0 + w < nw;
             s.v[w] = make_uint4(load_word(at, in && rows > 0), load_word(at + 32, in && rows > 32), load_word(at + 64, in && rows > 64),
                                 load_word(at + 96, in && rows > 96));
-            if (mask != 0xFFFFFFFFu) s.v[w] = make_uint4(s.v[w].x & mask, s.v[w].y & mask, s.v[w].z & mask, s.v[w].w & mask);
         }
         return true;
     };
     Stage a, b, c;
     bool ha = load(a), hb = load(b), hc = load(c);
     while (ha && !lds32(abort_flag)) {
-        put(it, a.v);
+        put(it, masked(a));
         it += TEAMS;
         ha = load(a);
         if (!hb) break;
-        put(it, b.v);
+        put(it, masked(b));
         it += TEAMS;
         hb = load(b);
         if (!hc) break;
-        put(it, c.v);
+        put(it, masked(c));
         it += TEAMS;
         hc = load(c);
     }
