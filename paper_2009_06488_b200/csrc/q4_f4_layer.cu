@@ -1,9 +1,9 @@
 // Expert layer for a few tokens on e2m1 weights with microscales: two kernels that stream the weights of the experts that
-// are hit, once, from HBM through the block-scaled tensor-core product.
+// are hit, once, from HBM through the block-scaled tensor-core product, and a sum.
 //
 //   kernel 1 (up)     h = silu(G_e x) * (U_e x)  (or silu(G_e x)) of every pair of a token and an expert, binary32
-//   kernel 2 (down)   y = W2_e h of every pair, binary32; the block that finishes columns last sums, at its end,
-//                     Out[t] = sum_j w[t][j] y in the order of j
+//   kernel 2 (down)   y = W2_e h of every pair, binary32
+//   kernel 3 (sum)    Out[t] = sum_j w[t][j] y in the order of j
 //
 // The tensor core multiplies e2m1 by e2m1, and activations are not quantized: a group of them is written as a sum of PARTS
 // e2m1 vectors under one scale 2^a,
@@ -23,8 +23,7 @@
 //   warp 1        MMA issuer   a stage's scales to tensor memory, then four products
 //   warps 2, 3    scales       a stage each in turn: the rows' words, two turns ahead, put in atoms
 //   warps 4..7    epilogue     parts added, gate and product meet through shared memory
-//   warps 8, 9    (kernel 2)   a tile's counter, every other tile each
-//   warps 10..23  activations  the next unit's parts and scales, while this one's are multiplied
+//   warps 8..23   activations   the next unit's parts and scales, while this one's are multiplied
 //
 // Bound: HBM; ahead of it the start (sorting, the first unit's parts) of some 5 us.  What was tried: codes to binary16 in
 // registers and warp-level matrix instructions, the depth spread over a block's warps (16 tokens 86 us) or a strip of rows per
@@ -39,11 +38,10 @@ namespace f4 {
 constexpr int PARTS = 7;
 constexpr int TROWS = 128, BOXROWS = 64;          // weights' rows of a tile and of a copy
 constexpr int MAX_PAIRS = 1024;                  // sorted by each block
-constexpr int ACT0 = 10, ACTS = 14;              // first of the activations' warps, their number
-static_assert(ACTS * 32 == 448, "the activations' warps meet");
+constexpr int ACT0 = 8, ACTS = 16;              // first of the activations' warps, their number
+static_assert(ACTS * 32 == 512, "the activations' warps meet");
 constexpr int LAYER_THREADS = (ACT0 + ACTS) * 32;
 constexpr int MAX_STAGES = 12;
-constexpr int MAX_TILES = 4096;                  // of a block
 
 // Shared memory, in this order: stages of codes, their atoms, units' parts, their atoms, lists and the rest.
 template <bool BY16, int NTOK> struct LayerCfg {
@@ -52,7 +50,7 @@ template <bool BY16, int NTOK> struct LayerCfg {
     static constexpr int STAGE = TROWS * ROWB, ATOMS = WORDS * ATOM;
     static constexpr int BLOCK = N * ROWB + ATOMS;             // parts of 256 depth values, and their scales
     static constexpr int LISTS = MAX_PAIRS * 2 * 4 + (Q4_MAX_EXPERTS + 32) * 4 * 2;
-    static constexpr int REST = 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4 + (2 * MAX_STAGES + 12) * 8 + 8 + MAX_TILES / 8;
+    static constexpr int REST = 4 * 8 * 4 + 8 * 4 + BOXROWS * NTOK * 4 + (2 * MAX_STAGES + 8) * 8 + 8;
     static constexpr int COL_SCALE = 2 * N;                    // tensor memory: two accumulators, two buffers of scales
     static constexpr int COLS = 256;
     static_assert(PARTS * NTOK <= N && COL_SCALE + 2 * 2 * WORDS * 4 <= COLS, "tensor memory");
@@ -66,7 +64,6 @@ struct LayerLaunch {
     LayerParams p;
     float* hidden;                   // [pairs][H]
     float* y;                        // [pairs][D]
-    int* done;                       // units that are finished per tile of output columns
     int stages, bufs;
 };
 
@@ -140,7 +137,9 @@ template <typename T> __device__ __forceinline__ f8::Eight<T> eight_at(const T* 
     } else {
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? f8::to_f(row[k + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = f8::to_f(row[min(k + i, K - 1)]);      // (without conditions: all under way together)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? v[i] : 0.0f;
         f8::pack8(e, v);
     }
     return e;
@@ -151,6 +150,21 @@ template <typename T> __device__ __forceinline__ uint32_t largest(const f8::Eigh
 #pragma unroll
     for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(e.get(i)) & 0x7FFFFFFFu);
     return a;
+}
+
+// The field at bit `at` of eight values' halves of words, value n to nibble n.
+__device__ __forceinline__ uint32_t nibbles(const uint32_t (&w)[4], int at, uint32_t field)
+{
+    uint32_t r = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r |= (4 * j >= at ? w[j] << (4 * j - at) : w[j] >> (at - 4 * j)) & (field | field << 16) << (4 * j);
+    return r;
+}
+// Nibbles 0..7 that stand for digits -4..3 to the codes of half of these (the code of d / 2 is |d| and the sign).
+__device__ __forceinline__ uint32_t digit_codes(uint32_t w)
+{
+    const uint32_t neg = (~w & 0x44444444u) >> 2;
+    return ((w ^ neg * 3u) & 0x33333333u) + neg * 9u;          // negative: 8 + (~d & 3) + 1
 }
 
 // Parts and scales of 256 values of a pair (column n of the unit), eight per lane, by a warp.  rowe: the biased exponent of
@@ -173,24 +187,30 @@ __device__ __forceinline__ void put_parts(const f8::Eight<T>& v, int n, uint32_t
         byte = e == 255 ? 255u : (uint32_t)s;
     }
     const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
-    float r[8];
+    // x / 2^a in steps of 2^-18, plus 4 in each digit to base 8 (as digits of -4..3 are asked for) and in what is above them
+    uint32_t y[8], lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = v.get(i) * inv;
-    // (not unrolled, like all that runs once: a block's first pass through its code waits for the instructions)
-    float mult = 4.0f;
-#pragma unroll 1
-    for (int row = n; row < PARTS * NTOK; row += NTOK) {
-        const uint32_t c = codes8(r);
-        sts32(parts + (uint32_t)(row * ROWB) + (uint32_t)((((lane >> 2) ^ row) & 7) << 4) + (uint32_t)(lane & 3) * 4u, (int)c);
-        // what the codes stand for, without decoding them: the nearest multiple of a half, from 2 on of one, ties to even
-        // (a sum with 1.5 * 2^22 or 2^23 rounds so)
+    for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(fmaf(v.get(i) * inv, 262144.0f, 12582912.0f)) + (0x124924u - 0x4B400000u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float big = fabsf(r[i]) > 2.0f ? 12582912.0f : 6291456.0f;
-            r[i] = (r[i] - ((r[i] + big) - big)) * mult;
-        }
-        mult = 8.0f;
+    for (int j = 0; j < 4; ++j) {
+        lo[j] = __byte_perm(y[j], y[j + 4], 0x5410);           // bits 0..15 of both
+        hi[j] = __byte_perm(y[j], y[j + 4], 0x6521);           // bits 8..23
     }
+    auto put = [&](int q, uint32_t codes) {
+        const int row = q * NTOK + n;
+        sts32(parts + (uint32_t)(row * ROWB) + (uint32_t)((((lane >> 2) ^ row) & 7) << 4) + (uint32_t)(lane & 3) * 4u, (int)codes);
+    };
+    {
+        // 0..8 for -4..4, whose codes are 0, 2, 4, 5, 6 and the sign: bit by bit, eight values at a time
+        constexpr uint32_t ONES = 0x11111111u;
+        const uint32_t w = nibbles(hi, 10, 0xFu), b0 = w, b1 = w >> 1, b2 = w >> 2, b3 = w >> 3, neg = ~(b2 | b3);
+        const uint32_t c2 = (neg & ~(b1 & b0)) | (~neg & (b3 | b1)), c1 = (neg & ~(b1 ^ b0)) | (~neg & (b3 | (~b1 & b0))),
+                       c0 = b0 & (b1 ^ neg);
+        put(0, (c0 & ONES) | (c1 & ONES) << 1 | (c2 & ONES) << 2 | (neg & ONES) << 3);
+    }
+    put(1, digit_codes(nibbles(hi, 7, 7u)));
+#pragma unroll
+    for (int q = 2; q < PARTS; ++q) put(q, digit_codes(nibbles(lo, 3 * (PARTS - 1 - q), 7u)));
     // the words: by 16 a word is 8 lanes' (a group two), else 16 lanes' (a group four)
     constexpr int G = BY16 ? 2 : 4;
     uint32_t w = byte << (8 * (lane / G & 3));
@@ -228,10 +248,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
     auto bar_tempty = [&](uint32_t a) { return bar0 + 8u * (2 * MAX_STAGES + 2 + a); };
     auto bar_act    = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 4 + b); };     // a unit's parts are there
     auto bar_used   = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 6 + b); };     // ... and have been multiplied
-    auto bar_done   = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 8 + b); };     // a tile's results are written (kernel 2)
-    auto bar_noted  = [&](uint32_t b) { return bar0 + 8u * (2 * MAX_STAGES + 10 + b); };    // ... and counted
-    const uint32_t abort_flag = bar0 + 8u * (2 * MAX_STAGES + 12), tmem_slot = abort_flag + 4;
-    unsigned* const last_of = reinterpret_cast<unsigned*>(smem_raw + (abort_flag + 8 - smem_u32(smem_raw)));      // a bit per tile
+    const uint32_t abort_flag = bar0 + 8u * (2 * MAX_STAGES + 8), tmem_slot = abort_flag + 4;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -243,15 +260,11 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
             mbar_init(bar_tempty(a), 4);     // the epilogue's warps
             mbar_init(bar_act(a), ACTS);
             mbar_init(bar_used(a), 1);
-            mbar_init(bar_done(a), 4);
-            mbar_init(bar_noted(a), 1);
         }
         sts32(abort_flag, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (DOWN && warp == 2)
-        for (int i = lane; i < MAX_TILES / 32; i += 32) last_of[i] = 0;
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"((uint32_t)C::COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -270,8 +283,6 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
     const int expert_rows = DOWN ? p.D : gated ? 2 * p.H : p.H, half = gated ? p.H : BOXROWS;
     // a block's tiles lie together
     const int t0 = (int)((int64_t)ntiles * blockIdx.x / gridDim.x), t1 = (int)((int64_t)ntiles * (blockIdx.x + 1) / gridDim.x);
-    if (!DOWN)
-        for (int i = blockIdx.x * LAYER_THREADS + threadIdx.x; i < (p.D + TROWS - 1) / TROWS; i += gridDim.x * LAYER_THREADS) L.done[i] = 0;
 
     if (warp == 0) {
         // ------------------------------------------------------------ producer
@@ -450,8 +461,6 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 asm volatile("bar.sync 2, 128;" ::: "memory");
             } else {
                 const int r = r0 + 32 * h + lane;
-                // (kernel 2: the counter of the tile two before has been taken)
-                if (DOWN && tile - t0 >= 2) mbar_wait_suspend(bar_noted(tile - t0 & 1), (uint32_t)(tile - t0 - 2) >> 1 & 1u, abort_flag, p.status);
                 if (r < rows) {
 #pragma unroll
                     for (int n = 0; n < NTOK; ++n)
@@ -461,27 +470,6 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                             else L.hidden[(int64_t)pair * p.H + r] = v[n] / (1.0f + expf(-v[n]));
                         }
                 }
-            }
-            if (DOWN) {
-                __syncwarp();                                  // my half of the tile is written
-                if (lane == 0) mbar_arrive(bar_done(tile - t0 & 1));
-            }
-        }
-    } else if (warp < ACT0) {
-        // ------------------------------------------------------------ counters
-        // each warp every other tile: which tiles are the last of their columns
-        if (DOWN) {
-            f8::wait_for_predecessor();                        // the counters' zeros
-            for (int i = warp - 8; i < t1 - t0 && !lds32(abort_flag); i += 2) {
-                mbar_wait_suspend(bar_done(i & 1), (uint32_t)i >> 1 & 1u, abort_flag, p.status);
-                if (lane == 0) {
-                    __threadfence();
-                    const bool last = atomicAdd(L.done + (t0 + i) % each * per / TROWS, 1) == nunits - 1;
-                    __threadfence();
-                    if (last) atomicOr(last_of + (i >> 5), 1u << (i & 31));
-                    mbar_arrive(bar_noted(i & 1));
-                }
-                __syncwarp();
             }
         }
     } else {
@@ -512,7 +500,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 if (BY16) {
                     // the rows' largest values
                     if (me == 0 && lane < 8) row_max[lane] = 0;
-                    asm volatile("bar.sync 3, 448;" ::: "memory");
+                    asm volatile("bar.sync 3, 512;" ::: "memory");
                     f8::Eight<T> w = v;
 #pragma unroll 1
                     for (int n = n0, b = b0; b < nkb;) {
@@ -521,7 +509,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                         step(n, b);
                         if (b < nkb) w = value(n, b);
                     }
-                    asm volatile("bar.sync 3, 448;" ::: "memory");
+                    asm volatile("bar.sync 3, 512;" ::: "memory");
                 }
                 // biased exponent of a row's factor: its largest group's scale is e4m3's 2^8
                 auto row_exponent = [&](int n) {
@@ -542,7 +530,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_act(ab));
-                if (BY16) asm volatile("bar.sync 3, 448;" ::: "memory");       // row_max has been read
+                if (BY16) asm volatile("bar.sync 3, 512;" ::: "memory");       // row_max has been read
                 if (++ab == (uint32_t)L.bufs) { ab = 0; abph ^= 1u; }
             }
         };
@@ -554,41 +542,37 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (DOWN) {
-        // Columns that this block was the last to finish: the sum over each token's pairs, in their order, by all threads; a
-        // thread's 8 values are under way together (every address exists; what does not count is left out).
-        const int words = (t1 - t0 + 31) / 32;
-        for (int k = 0; k < words; ++k)
-            for (uint32_t m = last_of[k]; m; m &= m - 1) {
-                const int r0 = (t0 + 32 * k + __ffs((int)m) - 1) % each * per;
-                for (int i = threadIdx.x; i < p.tokens * TROWS; i += LAYER_THREADS) {
-                    const int tok = i / TROWS, d = r0 + i % TROWS;
-                    const float* const y = L.y + (int64_t)tok * p.topk * p.D + min(d, p.D - 1);
-                    float out = 0.0f;
-#pragma unroll 1
-                    for (int j0 = 0; j0 < p.topk; j0 += 8) {
-                        float yv[8], wt[8];
-                        int id[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int at = min(j0 + j, p.topk - 1);
-                            id[j] = __ldg(p.ids + tok * p.topk + at);
-                            wt[j] = p.w ? __ldg(p.w + tok * p.topk + at) : 1.0f;
-                            yv[j] = __ldcg(y + (int64_t)at * p.D);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j0 + j < p.topk && (unsigned)id[j] < (unsigned)p.E) out = fmaf(wt[j], yv[j], out);
-                    }
-                    if (d < p.D) store_value(p.Out, (int64_t)tok * p.ldo + d, p.type, out);
-                }
-            }
-        if (nunits == 0)                                       // no pair at all
-            for (int64_t i = (int64_t)blockIdx.x * LAYER_THREADS + threadIdx.x; i < (int64_t)p.tokens * p.D; i += (int64_t)gridDim.x * LAYER_THREADS)
-                store_value(p.Out, i / p.D * p.ldo + i % p.D, p.type, 0.0f);
-    }
     if (warp == 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::COLS) : "memory");
+}
+
+// Out[t][d] = sum_j w[t][j] y of pair (t, j) in the order of j: a thread per value, its eight next terms under way together
+// (every address exists; what does not count is left out).
+constexpr int SUM_THREADS = 128;
+__global__ void __launch_bounds__(SUM_THREADS)
+layer_sum_kernel(const LayerLaunch L)
+{
+    const LayerParams& p = L.p;
+    f8::wait_for_predecessor();
+    const int per = (p.D + SUM_THREADS - 1) / SUM_THREADS, tok = (int)blockIdx.x / per, d = ((int)blockIdx.x - tok * per) * SUM_THREADS + (int)threadIdx.x;
+    if (d >= p.D) return;
+    const float* const y = L.y + (int64_t)tok * p.topk * p.D + d;
+    float out = 0.0f;
+    for (int j0 = 0; j0 < p.topk; j0 += 8) {
+        float yv[8], wt[8];
+        int id[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = min(j0 + j, p.topk - 1);
+            id[j] = __ldg(p.ids + tok * p.topk + at);
+            wt[j] = p.w ? __ldg(p.w + tok * p.topk + at) : 1.0f;
+            yv[j] = __ldcg(y + (int64_t)at * p.D);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j0 + j < p.topk && (unsigned)id[j] < (unsigned)p.E) out = fmaf(wt[j], yv[j], out);
+    }
+    store_value(p.Out, (int64_t)tok * p.ldo + d, p.type, out);
 }
 
 constexpr int SMEM_MOST = 232448;
@@ -633,20 +617,21 @@ static q4_status launch_layer(LayerLaunch L, cudaStream_t st)
 template <bool BY16, int NTOK>
 static q4_status launch_both(const LayerLaunch& L, cudaStream_t st)
 {
-    const q4_status e = launch_layer<BY16, NTOK, false>(L, st);
-    return e != Q4_OK ? e : launch_layer<BY16, NTOK, true>(L, st);
+    q4_status e = launch_layer<BY16, NTOK, false>(L, st);
+    if (e == Q4_OK) e = launch_layer<BY16, NTOK, true>(L, st);
+    if (e != Q4_OK) return e;
+    const unsigned blocks = (unsigned)(L.p.tokens * ((L.p.D + SUM_THREADS - 1) / SUM_THREADS));
+    return f8::launch(layer_sum_kernel, blocks, SUM_THREADS, 0, st, L) == cudaSuccess ? Q4_OK : Q4_ERR_CUDA;
 }
 
 }  // namespace f4
 
 using namespace f4;
 
-// The workspace: a counter per tile of output columns, hidden values, what each pair adds to its token.
-static int64_t counters_bytes(int32_t D) { return (((int64_t)D + TROWS - 1) / TROWS * 4 + 255) / 256 * 256; }
-
+// The workspace: hidden values, each pair's results.
 int64_t expert_layer_f4_ws_bytes(int64_t pairs, int32_t D, int32_t H)
 {
-    return counters_bytes(D) + 4 * pairs * ((int64_t)H + D);
+    return 4 * pairs * ((int64_t)H + D);
 }
 
 template <int NTOK> static bool fits(const f4::LayerParams& p, bool by16)
@@ -661,16 +646,13 @@ bool expert_layer_f4_stream_supported(const f4::LayerParams& p, bool by16)
     const int64_t rows1 = (int64_t)p.E * (p.gated ? 2 : 1) * p.H, rows2 = (int64_t)p.E * p.D;
     return p.type != Q4_F32 && (int64_t)p.tokens * p.topk <= MAX_PAIRS && fits<4>(p, by16) &&
            rows1 < INT32_MAX - 512 && rows2 < INT32_MAX - 512 &&
-           (int64_t)MAX_PAIRS * ((p.D + TROWS - 1) / TROWS) / (2 * f8_pairs_of_device()) < MAX_TILES &&
            (uintptr_t)p.W1 % 16 == 0 && (uintptr_t)p.W2 % 16 == 0 && p.ldw1 % 16 == 0 && p.ldw2 % 16 == 0;
 }
 
 q4_status launch_expert_layer_f4_stream(const f4::LayerParams& p, bool by16, cudaStream_t st)
 {
     const int64_t pairs = (int64_t)p.tokens * p.topk;
-    LayerLaunch L{p, nullptr, nullptr, nullptr, 0, 0};
-    L.done = static_cast<int*>(p.ws);
-    L.hidden = reinterpret_cast<float*>(static_cast<uint8_t*>(p.ws) + counters_bytes(p.D));
+    LayerLaunch L{p, static_cast<float*>(p.ws), nullptr, 0, 0};
     L.y = L.hidden + pairs * p.H;
     // Eight pairs per unit where their parts fit, so that an expert's weights pass once for them; four where experts are hit by
     // three at most on average: their parts leave room for more stages.
