@@ -11,8 +11,8 @@
 // The transposed output (codes of X^T, groups along the rows of a column) comes from the same read.
 //
 // Layout: a thread holds 8 consecutive columns of RT rows as they lie in memory; 16 threads span 128 columns and 16
-// such rows of threads a tile of 16 * RT rows.  RT = 8 is the unit of the transposed output; straight codes alone take
-// RT = 2 below 128 such tiles, where more and smaller thread blocks start sooner.  A group is 4 (2) threads of a
+// such rows of threads a tile of 16 * RT rows.  RT = 8 is the unit of the transposed output; straight codes alone mostly
+// take RT = 2, where more and smaller thread blocks start sooner.  A group is 4 (2) threads of a
 // row: its maximum goes round them by shuffles that halve the rows as they double the threads, so that each of a
 // thread's rows has its scale computed once.  Along columns a group is 4 (2) rows of threads.
 // Bound: HBM, with instruction issue close behind.
@@ -308,7 +308,9 @@ static cudaError_t launch_quantize(const QuantizeParams& p, cudaStream_t st)
 {
     // column tiles vary fastest: neighbouring tiles read neighbouring pieces of the same rows
     const int64_t nc = ((int64_t)p.cols + TC - 1) / TC, t128 = nc * (((int64_t)p.rows + 127) / 128);
-    if (p.Qt || t128 >= 128) return f8::launch(quantize_kernel<TYPE, 8, BY16, VEC>, (unsigned)t128, 256, 0, st, p);
+    // Straight codes alone: the small tiles, with more threads per SM, win for binary32 (2048 x 2048 and read back 9.4 -> 8.0 us,
+    // 4096 x 4096 23.0 -> 21.6) and below two tiles per SM for 16 bits (2048 x 1024 5.8 -> 5.4; 2048 x 4096 9.8 against 10.3).
+    if (p.Qt || (TYPE != Q4_F32 && t128 >= 4 * f8_pairs_of_device())) return f8::launch(quantize_kernel<TYPE, 8, BY16, VEC>, (unsigned)t128, 256, 0, st, p);
     return f8::launch(quantize_kernel<TYPE, 2, BY16, VEC>, (unsigned)(nc * (((int64_t)p.rows + 31) / 32)), 256, 0, st, p);
 }
 template <int TYPE>
