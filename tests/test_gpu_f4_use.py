@@ -6,6 +6,7 @@ import pytest
 from oracle import f4
 from test_gpu_f4 import check, operand, placed, up16, word_tensor
 from test_gpu_f4_layer import Case
+from test_gpu_f8_behind_a_long_kernel import CLOCKS, long_kernel      # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -210,3 +211,30 @@ def test_layers_in_turn_share_a_workspace(q4):
             h = out
         return h
     assert torch.equal(layers(False), layers(True))
+
+
+def test_behind_a_kernel_that_outlasts_the_waits(q4, long_kernel):      # noqa: F811
+    """The bounded waits inside the kernels begin when their inputs are there, not when an early start lets them in."""
+    import torch
+
+    def behind(call, out):
+        call()
+        out.fill_(7)
+        torch.cuda.synchronize()
+        assert q4.q4_last_device_status() == q4.Q4_OK
+        assert long_kernel(CLOCKS, torch.cuda.current_stream().cuda_stream) == 0
+        call()
+        torch.cuda.synchronize()
+        assert q4.q4_last_device_status() == q4.Q4_OK
+    for M, N, K in ((5, 300, 400), (5, 300, 4096), (300, 520, 700), (2500, 2048, 300)):      # few rows, depth in parts, pairs: narrow and wide
+        a, sa, va = operand(M, M, K, False)
+        b, sb, vb = operand(N, N, K, False)
+        A, SA, B, SB = placed(a, up16(a.shape[1])), word_tensor(sa), placed(b, up16(b.shape[1])), word_tensor(sb)
+        C = torch.empty(M, N, device="cuda")
+        behind(lambda: q4.q4_gemm_f4(A, SA, B, SB, C, M, N, K), C)
+        want, mag = f4.product(va, vb)
+        check(C, want, mag, K, "f32", extra=4)
+    c = Case(71, 16, 4, 8, 512, 256, True, True, "bf16")
+    ids, w, ws = torch.from_numpy(c.ids).cuda(), torch.from_numpy(c.w).cuda(), c.ws(q4)
+    behind(lambda: q4.q4_expert_layer_f4(c.X, ids, w, c.W1, c.S1, c.W2, c.S2, c.Out, c.E, c.H, ws, gated=True, by16=True, F1=c.F1, F2=c.F2), c.Out)
+    c.check()
