@@ -539,7 +539,7 @@ q4_status q4_gemm_f4_experts(const uint8_t* A, int64_t lda, const uint32_t* SA, 
                              void* C, int32_t c_type, int64_t ldc, int32_t M, int32_t N, int32_t K, void* stream);
 
 /*
- * The whole expert layer for a few tokens, in two kernels and without quantizing the activations:
+ * The whole expert layer for a few tokens, without quantizing the activations:
  *   Out[t] = sum_j w[t][j] * W2_e h,   h = silu(G_e X[t])              or, with Q4_F4_GATED,
  *                                      h = silu(G_e X[t]) * (U_e X[t]),   e = ids[t][j]
  * X, Out [tokens x D] of type (a q4_type); ids [tokens][topk]: a number outside 0 .. E - 1 leaves the pair out; w
@@ -549,6 +549,9 @@ q4_status q4_gemm_f4_experts(const uint8_t* A, int64_t lda, const uint32_t* SA, 
  * ws: q4_expert_layer_f4_workspace_bytes(tokens, topk, D, H) bytes, 256-byte aligned, not shared by calls that may run
  * at the same time (captured graphs among them).  The same inputs give the same bits.  Meant for up to a few dozen
  * tokens: many are served by q4_expert_sort and the products by experts.
+ * Fast path (three kernels): 16-bit X, at most 1024 pairs, D and H up to 8704 (by 16: 7168; what shared memory holds of
+ * four tokens), W1, W2 16-byte aligned and ldw1, ldw2 multiples of 16; anything else runs slower general kernels.  On the
+ * fast path an activation (a value of X or h) enters the products within 2^-20 of the largest of its group of 32 (by 16: 16).
  */
 q4_status q4_expert_layer_f4(const void* X, int64_t ldx, int32_t type, int32_t tokens, int32_t D, int32_t H,
                              const int32_t* ids, const float* w, int32_t topk, int32_t E, int32_t flags,

@@ -576,7 +576,7 @@ def q4_expert_layer_f4_workspace_bytes(tokens: int, topk: int, D: int, H: int) -
 def q4_expert_layer_f4(X, ids, w, W1, S1, W2, S2, Out, E: int, H: int, ws, gated: bool = True, by16: bool = False,
                        F1=None, F2=None):
     """Out[t] = sum_j w[t, j] * W2_e h, h = silu(G_e X[t]) * (U_e X[t]) (not gated: silu(G_e X[t])), e = ids[t, j]: the
-    expert layer for a few tokens on 4-bit weights, in two kernels.  W1 [E * 2 H (not gated: E * H), D], W2 [E * D, H]
+    expert layer for a few tokens on 4-bit weights.  W1 [E * 2 H (not gated: E * H), D], W2 [E * D, H]
     as codes, their scales at the same rows; F1, F2 float32 [E] or None; ws uint8.  See include/q4.h."""
     _check(_t.expert_layer_f4(X, ids, w, W1, S1, W2, S2, Out, E, H, ws,
                               (Q4_F4_GATED if gated else 0) | (Q4_F4_BY16 if by16 else 0), F1, F2), "q4_expert_layer_f4")

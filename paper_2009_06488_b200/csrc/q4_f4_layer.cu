@@ -8,9 +8,11 @@
 // The tensor core multiplies e2m1 by e2m1, and activations are not quantized: a group of them is written as a sum of PARTS
 // e2m1 vectors under one scale 2^a,
 //   x = 2^a (c0 + 2^-2 c1 + 2^-5 c2 + 2^-8 c3 + ... + 2^-17 c6) + rest,   max |x| / 2^a in [2, 4),
-// each the nearest to what the ones before leave (at most half a step: 1/2, then 1/4 of a range of +-2), so that the rest is
-// at most 2^-21 of the group's largest value.  Binary16 and bfloat16 values that are not far below their group's largest
-// are exact.  The parts are rows of the product's second operand and their results are added in binary32.  The scale is
+// the rest at most half a step of the last, 2^-20 of the group's largest value: binary16 and bfloat16 values that are not far
+// below it are exact.  x / 2^a is rounded once to an integer of steps 2^-18; c0 is an integer of -4..4 and the others are half
+// of its digits to base 8, -4..3: codes 0 to 4 of e2m1 are 0, 1/2, 1, 3/2, 2.  (Parts made one after the other in floating
+// point, each the nearest to what is left, took three times the instructions.)
+// The parts are rows of the product's second operand and their results are added in binary32.  The scale is
 // that of the weights' kind: a power of two per 32, or per 16 one in e4m3 (17 powers, above 2^-17 of the row's
 // largest value) times a power of two for the row.
 //
@@ -23,9 +25,12 @@
 //   warp 1        MMA issuer   a stage's scales to tensor memory, then four products
 //   warps 2, 3    scales       a stage each in turn: the rows' words, two turns ahead, put in atoms
 //   warps 4..7    epilogue     parts added, gate and product meet through shared memory
-//   warps 8..23   activations   the next unit's parts and scales, while this one's are multiplied
+//   warps 8..23   activations  the next unit's parts and scales, while this one's are multiplied
 //
-// Bound: HBM; ahead of it the start (sorting, the first unit's parts) of some 5 us.  What was tried: codes to binary16 in
+// Bound: HBM, behind each kernel's start (sorting, the first unit's parts: 7 us of the first) and beside
+// blocks with a tile more than others (7 against 6.2 on average).  64 experts of 2048 -> 1024 (gated) -> 2048: sixteen tokens
+// 44 us = 4.2 TB/s of weights, one token (8 experts) 19 us.  What was tried: the sum by the block that finishes columns
+// last (its tail 6 to 14 us); all in one cooperative kernel (63); later stages to L2 ahead of their copies (54); codes to binary16 in
 // registers and warp-level matrix instructions, the depth spread over a block's warps (16 tokens 86 us) or a strip of rows per
 // warp, brought by 16-byte copies (75) or TMA (77): eight instructions per 16 codes left HBM at a third of its rate.
 #include <cuda.h>
@@ -38,7 +43,7 @@ namespace f4 {
 constexpr int PARTS = 7;
 constexpr int TROWS = 128, BOXROWS = 64;          // weights' rows of a tile and of a copy
 constexpr int MAX_PAIRS = 1024;                  // sorted by each block
-constexpr int ACT0 = 8, ACTS = 16;              // first of the activations' warps, their number
+constexpr int ACT0 = 8, ACTS = 16;               // first of the activations' warps, their number
 static_assert(ACTS * 32 == 512, "the activations' warps meet");
 constexpr int LAYER_THREADS = (ACT0 + ACTS) * 32;
 constexpr int MAX_STAGES = 12;
@@ -577,7 +582,8 @@ layer_sum_kernel(const LayerLaunch L)
 
 constexpr int SMEM_MOST = 232448;
 
-// Stages and units whose parts are held: two where four stages fit beside them, else one; {0, 0}: none.
+// Stages and units whose parts are held: two where four stages fit beside them, else one; {0, 0}: none.  Two stages are enough
+// to be worth it: eight tokens, 32 experts of 7168 -> 2048 -> 7168 by 16, 169 us = 3.5 TB/s.
 struct Room { int stages, bufs; };
 template <bool BY16, int NTOK> static Room room_for(int K)
 {
@@ -586,7 +592,7 @@ template <bool BY16, int NTOK> static Room room_for(int K)
     for (int bufs = 2; bufs >= 1; --bufs) {
         int stages = (SMEM_MOST - C::bytes(0, bufs, nkb)) / (C::STAGE + C::ATOMS);
         if (stages > MAX_STAGES) stages = MAX_STAGES;
-        if (stages >= (bufs == 2 ? 4 : 3)) return {stages, bufs};
+        if (stages >= (bufs == 2 ? 4 : NTOK == 8 ? 3 : 2)) return {stages, bufs};
     }
     return {0, 0};
 }

@@ -183,6 +183,12 @@ def test_layer_at_its_largest_lists(q4, T, topk):
     Case(T + topk, T, topk, 5, 64, 48, True, topk > 1, "bf16").run(q4).check()
 
 
+@pytest.mark.parametrize("D,H,by16", [(8704, 200, False), (7168, 256, True), (300, 8704, False), (4608, 130, False), (7169, 130, True), (5000, 6401, True)])
+def test_layer_of_the_widest_tokens(q4, D, H, by16):
+    """Depths at which one unit's activations fill shared memory, and the first that do not fit."""
+    Case(D, 5, 2, 3, D, H, True, by16, "bf16").run(q4).check()
+
+
 def test_layer_of_as_many_experts_as_there_may_be(q4):
     Case(51, 7, 4, 1024, 64, 32, True, True, "f16").run(q4).check()
 
