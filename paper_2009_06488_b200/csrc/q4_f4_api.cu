@@ -16,6 +16,8 @@ bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 q4_status done(cudaError_t e) { return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA; }
 int64_t bytes_of(int64_t cols) { return (cols + 1) / 2; }
+// (the kernels' indexes pass a size by less than a tile)
+constexpr int32_t MOST = INT32_MAX - 512;
 
 q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* stream)
 {
@@ -27,6 +29,7 @@ q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* 
     if (!p.A || !p.Bt || !p.SA || !p.SB || !p.C) return Q4_ERR_INVALID_ARG;
     if (!aligned(p.SA, 4) || !aligned(p.SB, 4) || !aligned(p.FA, 4) || !aligned(p.FB, 4) || !aligned(p.starts, 4) ||
         !aligned(p.C, f8::type_size(p.c_type))) return Q4_ERR_ALIGNMENT;
+    if (p.N > MOST || p.K > MOST) return Q4_ERR_RANGE;
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
     const int variant = kernel_variant();
@@ -61,7 +64,7 @@ q4_status q4_f4_quantize(const void* X, int32_t x_type, int64_t ldx, int32_t row
     if (!X && !(source && x_rows == 0)) return Q4_ERR_INVALID_ARG;         // an empty matrix to pick from: every row is absent
     if (!aligned(X, f8::type_size(x_type)) || !aligned(S, 4) || !aligned(St, 4) || !aligned(source, 4) || !aligned(factor, 4))
         return Q4_ERR_ALIGNMENT;
-    if (((int64_t)cols + 127) / 128 * (((int64_t)rows + 31) / 32) > INT32_MAX) return Q4_ERR_RANGE;
+    if (rows > MOST || cols > MOST || ((int64_t)cols + 127) / 128 * (((int64_t)rows + 31) / 32) > INT32_MAX) return Q4_ERR_RANGE;
     f4::QuantizeParams p{};
     p.X = X; p.ldx = ldx; p.rows = rows; p.cols = cols;
     p.source = source; p.topk = source ? topk : 1; p.x_rows = source ? x_rows : rows;
@@ -82,7 +85,7 @@ q4_status q4_f4_dequantize(const uint8_t* Q, int64_t ldq, const uint32_t* S, int
     if (rows == 0 || cols == 0) return Q4_OK;
     if (!Q || !S || !Y) return Q4_ERR_INVALID_ARG;
     if (!aligned(S, 4) || !aligned(factor, 4) || !aligned(Y, f8::type_size(y_type))) return Q4_ERR_ALIGNMENT;
-    if (((int64_t)cols + 127) / 128 * (((int64_t)rows + 63) / 64) > INT32_MAX) return Q4_ERR_RANGE;
+    if (rows > MOST || cols > MOST || ((int64_t)cols + 127) / 128 * (((int64_t)rows + 63) / 64) > INT32_MAX) return Q4_ERR_RANGE;
     f4::DequantizeParams p{Q, ldq, S, lds, rows, cols, factor, Y, ldy, 0, 0};
     p.q_vec = aligned(Q, 4) && ldq % 4 == 0;
     p.y_vec = cols % 8 == 0 && aligned(Y, 16) && ldy * (int64_t)f8::type_size(y_type) % 16 == 0;
@@ -127,7 +130,7 @@ q4_status q4_expert_layer_f4(const void* X, int64_t ldx, int32_t type, int32_t t
     const int32_t up = flags & Q4_F4_GATED ? 2 : 1;
     if (!type_ok(type) || tokens < 0 || D < 1 || H < 1 || topk < 1 || E < 1 || (flags & ~(Q4_F4_BY16 | Q4_F4_GATED)))
         return Q4_ERR_INVALID_ARG;
-    if (E > Q4_MAX_EXPERTS || (int64_t)E * D > INT32_MAX || (int64_t)E * up * H > INT32_MAX || (int64_t)tokens * topk > INT32_MAX)
+    if (E > Q4_MAX_EXPERTS || (int64_t)E * D > INT32_MAX || (int64_t)E * up * H > INT32_MAX || D > MOST || H > MOST || (int64_t)tokens * topk > INT32_MAX)
         return Q4_ERR_RANGE;
     if (ldx < D || ldo < D || ldw1 < bytes_of(D) || ldw2 < bytes_of(H) || lds1 < (int64_t)E * up * H || lds2 < (int64_t)E * D)
         return Q4_ERR_INVALID_ARG;

@@ -81,6 +81,18 @@ def test_layer(lib):
     assert f(T=0, ws=None) == 0
 
 
+def test_sizes_at_the_end_of_32_bits(lib):
+    """Indexes that run past a size by a part of a tile would leave 32 bits."""
+    big, half = 2 ** 31 - 100, 2 ** 30
+    assert lib.q4_f4_quantize(fake, 1, big, 1, big, None, 1, 1, 0, None, fake, half, fake, 1, None, 0, None, 0, None) == RANGE
+    assert lib.q4_f4_quantize(fake, 1, 1, big, 1, None, 1, big, 0, None, fake, 1, fake, big, None, 0, None, 0, None) == RANGE
+    assert lib.q4_f4_dequantize(fake, half, fake, 1, 1, big, 0, None, fake, 1, big, None) == RANGE
+    assert lib.q4_gemm_f4(fake, half, fake, 1, fake, half, fake, 1, 0, None, None, fake, 0, 1, 1, 1, big, None) == RANGE
+    assert lib.q4_gemm_f4(fake, 1, fake, 1, fake, 1, fake, big, 0, None, None, fake, 0, big, 1, big, 1, None) == RANGE
+    assert lib.q4_expert_layer_f4(fake, big, 1, 1, big, 1, fake, None, 1, 1, 0, fake, half, fake, 1, None, fake, 1, fake, big, None, fake, big,
+                                  256, 2 ** 60, None) == RANGE
+
+
 def test_the_binding_refuses_what_does_not_fit():
     import torch
     from paper_2009_06488_b200 import binding as q4
