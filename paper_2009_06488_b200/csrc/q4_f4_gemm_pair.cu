@@ -13,9 +13,9 @@
 //   warps 8..15  epilogue       each thread one row and BN / 2 columns: times f, rounded, out through swizzled staging slices
 //                               and TMA stores (whole 32-row groups of aligned rows) or by pieces
 //
-// Bound: what L2 brings to an SM, 38 KB per stage (by 16) in about 720 clk, where four products of a wide tile take 512; without
-// the scales' 6 KB 8192^3 takes 169 us.  Then a tile's end, some 3000 clk in which a wide tile's accumulator (the only one that
-// fits beside the scales) is drained.  8192^3 to bf16: by 16 200 us = 5.5 PFLOP/s, by 32 184 us = 6.0 (four times the bf16
+// Bound: the ring of stages and a tile's end.  A stage of a wide tile lasts about 720 clk where its four products take 512 (without
+// the scales' loads 8192^3 takes 169 us; with four stages instead of five 210; L2 runs at a quarter of its rate), and the only
+// wide accumulator that fits beside the scales is drained for some 3000 clk per tile.  8192^3 to bf16: by 16 200 us = 5.5 PFLOP/s, by 32 184 us = 6.0 (four times the bf16
 // product's measured rate is 6.6); under the power cap 239.  Scales by TMA boxes: 290 us; two accumulators of 192 columns:
 // as long as one of 256.
 #include <cuda.h>
