@@ -445,13 +445,14 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                     if (q < PARTS) v[i % NTOK] = fmaf(__uint_as_float(r[i]), q ? 1.0f / (float)(1 << (3 * q - 1)) : 1.0f, v[i % NTOK]);
                 }
             }
+            // (the rows' factors are read ahead of the arrival: it is what lets their slot be written again)
+#pragma unroll
+            for (int n = 0; n < NTOK; ++n) v[n] *= (BY16 ? row_factor[(u & 3) * 8 + n] : 1.0f) * f;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_tempty(acc));
             aph ^= acc;
             acc ^= 1u;
-#pragma unroll
-            for (int n = 0; n < NTOK; ++n) v[n] *= (BY16 ? row_factor[(u & 3) * 8 + n] : 1.0f) * f;
             if (gated) {
                 const int r = 32 * (h & 1) + lane;
                 if (h >= 2) {
@@ -522,8 +523,10 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                     const uint32_t m = row_max[n];
                     return (m >= 0x7F800000u ? 127u : max(m >> 23, 20u)) - 9u;
                 };
-                if (BY16 && me == 0 && lane < count) row_factor[(u & 3) * 8 + lane] = __uint_as_float(row_exponent(lane) << 23);
                 mbar_wait_suspend(bar_used(ab), abph ^ 1u, abort_flag, p.status);
+                // The slot's last reader is unit u - 4.  This wait tells that unit u - 2 is multiplied (one buffer: u - 1), and its
+                // first product waited until the tile two before it, u - 4's or a later one, was read.
+                if (BY16 && me == 0 && lane < count) row_factor[(u & 3) * 8 + lane] = __uint_as_float(row_exponent(lane) << 23);
 #pragma unroll 1
                 for (int n = n0, b = b0; b < nkb;) {
                     const int row = n, at = ab * nkb + b;
