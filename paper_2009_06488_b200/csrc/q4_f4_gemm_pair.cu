@@ -248,8 +248,12 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 #pragma unroll
                 for (int w = 0; w < C::WORDS; ++w)
                     sts128(dst + (uint32_t)((part ? C::WORDS + w * C::BATOMS + part - 1 : w) * ATOM), v[w]);
+                // The leader's products read this CTA's atoms: the proxy fence and, behind the meeting, a release of shared
+                // memory to the cluster.  (A releasing arrival waits for the loads under way as well, 320 us for 8192^3; through
+                // a warp of its own that has none, 410.  The fence costs nothing that can be measured.)
                 fence_async_smem();
                 __syncwarp();
+                fence_release_smem_cluster();
                 if (lane == 0) mbar_arrive_cluster_relaxed(full_leader + 8u * st);
             });
     } else {

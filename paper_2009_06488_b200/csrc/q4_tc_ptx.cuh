@@ -246,14 +246,21 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar)
                  : "memory");
 }
-// Arrive without release semantics: only for a thread whose prior writes have already
-// been completed by explicit fences (tcgen05.wait::st, fence.proxy.async).  The
-// releasing form drains the thread's outstanding memory traffic and costs about a
-// thousand clocks when issued to another CTA once per pipeline stage.
+// Arrive without release semantics: for tensor-memory accesses that have been waited for and
+// fenced (tcgen05.wait::ld / ::st, tcgen05.fence::before_thread_sync), and behind
+// fence_release_smem_cluster() for writes to shared memory.  The releasing form drains the
+// thread's outstanding memory traffic and costs about a thousand clocks when issued to
+// another CTA once per pipeline stage.
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar)
                  : "memory");
+}
+// Releases what this thread has written to its CTA's shared memory, or has seen written there, to the cluster: with a
+// relaxed arrival behind it a releasing one that leaves the thread's traffic to global memory alone.
+__device__ __forceinline__ void fence_release_smem_cluster()
+{
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
 }
 __device__ __forceinline__ void sts32_cluster(uint32_t cluster_saddr, int v)
 {
