@@ -622,6 +622,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             fence_async_smem();           // my shared-memory stores are visible to the MMA
             tc_fence_before();
             __syncwarp();
+            fence_release_smem_cluster(); // the leader's MMA reads the warp's rows of Bt in this CTA
             if (lane == 0) {
                 mbar_arrive_cluster_relaxed(full_u_leader + 8u * (uint32_t)ust);
                 mbar_arrive_relaxed(bar_empty_p(pst));
