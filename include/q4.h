@@ -498,8 +498,9 @@ q4_status q4_expert_combine_grad(const void* dOut, int64_t ldd, const void* Y, i
  * Codes and scales of a matrix X [rows x cols] (x_type a q4_type, pitch ldx elements), a = max |x| over a group:
  *   by default    s = the smallest power of two that is not below max(a, 2^-60) / 6,  code = e2m1(x / s);
  *   Q4_F4_BY16    r = 1 / factor, s = max(e4m3(a * (r / 6)), 2^-9),  code = e2m1(x * (r / s)).
- * All steps are float32; e2m1() and e4m3() round to nearest even and saturate.  factor (Q4_F4_BY16 only, else NULL) is
- * positive; max |X| / 2688 puts the largest scale at e4m3's largest value.
+ * All steps are float32; e2m1() and e4m3() round to nearest even and saturate, and a quotient by the factor or by s that passes
+ * float32's largest value is that value.  factor (Q4_F4_BY16 only, else NULL) is finite and positive, or 0 where X holds
+ * zeros only: max |X| / 2688, which puts the largest scale at e4m3's largest value, is one.
  * Q [rows][ldq bytes], S: the codes and their scales.  Qt [cols][ldqt bytes], St: the same of X transposed (its groups
  * run along the rows of X), taken from the same read.  Either pair may be NULL, not both.
  * source, topk, x_rows: as in q4_f8_quantize.  A group that holds a NaN or an infinity gets the scale NaN and

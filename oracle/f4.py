@@ -11,6 +11,7 @@ import numpy as np
 from . import f8
 
 FLOOR = np.float32(2.0 ** -60)
+LARGEST = np.finfo(np.float32).max
 MAGNITUDES = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
 _VALUES = np.concatenate([MAGNITUDES, -MAGNITUDES])
 
@@ -73,10 +74,10 @@ def quantize(x: np.ndarray, by16: bool = False, factor=None):
     with np.errstate(all="ignore"):
         a = np.abs(v).max(axis=2)
         if by16:
-            r = np.float32(1) / np.float32(1 if factor is None else factor)
+            r = np.minimum(np.float32(1) / np.float32(1 if factor is None else factor), LARGEST)      # (NaN stays)
             byte = np.maximum(f8.encode(a * (r / np.float32(6))), 1)
             byte = np.where(np.isfinite(a), byte, 0x7F).astype(np.uint8)
-            inv = r / f8.decode(byte).astype(np.float32)
+            inv = np.minimum(r / f8.decode(byte).astype(np.float32), LARGEST)
         else:
             m, e = np.frexp(np.maximum(a, FLOOR).astype(np.float64) / 6)
             e = np.where(m == 0.5, e - 1, e)                   # 2^e is the next power of two

@@ -4,7 +4,8 @@
 //   by 32: s = the smallest power of two >= max(a, 2^-60) / 6,         code = e2m1(x / s)
 //   by 16: r = 1 / factor, s = max(e4m3(a * (r / 6)), 2^-9),           code = e2m1(x * (r / s))
 // All steps are binary32 with round to nearest even, so a code -- decided by floating-point arithmetic -- is
-// reproducible.  s never is below a group's need by more than its own rounding: codes saturate at 6 only there.  Maxima
+// reproducible.  Quotients past binary32's largest number are that number: a matrix of zeros has the factor 0 by
+// max |X| / 2688, and a zero times an infinite r would be NaN.  s never is below a group's need by more than its own rounding: codes saturate at 6 only there.  Maxima
 // are taken on the bit patterns of |x|, which order NaN above infinity above every number: a group that holds either
 // gets the scale NaN.
 //
@@ -43,6 +44,8 @@ template <typename T> __device__ __forceinline__ uint32_t max_of(const Eight<T>&
     return sizeof(T) == 4 ? m.w[0] : max(pattern(m, 0), pattern(m, 1));
 }
 
+__device__ __forceinline__ float at_most_largest(float v) { return v > 3.402823466e38f ? 3.402823466e38f : v; }      // (NaN stays)
+
 // Scale byte of a group whose largest |x| has the bit pattern `a`, and what its values are multiplied with.
 // r = 1 / factor, r6 = r / 6.
 template <bool BY16> __device__ __forceinline__ uint32_t scale_of(uint32_t a, float r, float r6, float& inv)
@@ -50,7 +53,7 @@ template <bool BY16> __device__ __forceinline__ uint32_t scale_of(uint32_t a, fl
     if (BY16) {
         uint32_t byte = __nv_cvt_float_to_fp8(__uint_as_float(a) * r6, __NV_SATFINITE, __NV_E4M3);
         byte = a > 0x7F7FFFFFu ? 0x7Fu : max(byte, 1u);
-        inv = __fdiv_rn(r, e4m3_value(byte));
+        inv = at_most_largest(__fdiv_rn(r, e4m3_value(byte)));
         return byte;
     }
     // a / 6 = (m / 1.5) 2^(e - 2): the next power of two is 2^(e - 2) where the mantissa is at most 1.5
@@ -84,7 +87,7 @@ quantize_kernel(const QuantizeParams p)
     const int nc = min(8, max(0, p.cols - c0));
     float r = 1.0f, r6 = 1.0f;
     if (BY16) {
-        if (p.factor) r = __fdiv_rn(1.0f, __ldg(p.factor));
+        if (p.factor) r = at_most_largest(__fdiv_rn(1.0f, __ldg(p.factor)));
         r6 = __fdiv_rn(r, 6.0f);
     }
 

@@ -52,3 +52,20 @@ def test_the_layer_by_hand():
     h0, h1, h2 = silu(1.0) * 6, silu(2.0) * 4, silu(1.0) * 2
     want = np.array([[0.5 * h0 - 0.25 * h1, h0 + 0.125 * h1], [-2 * h2, h2]])
     assert np.allclose(f4.layer(x, ids, w, w1, w2, True)[0], want, rtol=1e-14)
+
+
+def test_a_factor_of_zero_stands_for_a_matrix_of_zeros():
+    """1 / factor and its quotient by the scale end at binary32's largest value: zeros times it are zeros."""
+    x = np.zeros((2, 40), dtype=np.float32)
+    x[1] = -0.0
+    for factor in (np.float32(0), np.float32(1e-45), np.float32(1)):
+        q, s = f4.quantize(x, by16=True, factor=factor)
+        assert f4.from_words(s, 2).tolist() == [[1, 1, 1, 0]] * 2
+        assert f4.unpack(q, 40).tolist() == [[0] * 40, [8] * 40]
+        assert (f4.values(q, s, 40, True, factor) == 0).all()
+    x[0, :3] = [2.0 ** -140, -2.0 ** -149, 0]                 # a factor that is 0 in binary32: nothing but saturated quotients
+    q, s = f4.quantize(x, by16=True, factor=np.float32(0))
+    assert f4.from_words(s, 2)[0].tolist() == [1, 1, 1, 0] and f4.unpack(q, 3)[0].tolist() == [0, 8, 0]
+    x[0, 0] = 1
+    q, s = f4.quantize(x, by16=True, factor=np.float32(0))
+    assert f4.from_words(s, 2)[0].tolist() == [0x7E, 1, 1, 0] and f4.unpack(q, 3)[0].tolist() == [7, 8, 0]
