@@ -111,12 +111,23 @@ def experts(a, b, starts, n: int):
     return c, mag
 
 
-def layer(x, ids, w, w1, w2, gated: bool):
+def entered(v, by16=None):
+    """How far from itself a value of a row of activations may enter the layer's products: 2^-20 of the largest of its group
+    or, by 16, 2^-37 of the row's largest where that is more; 2^-144 where these are less.  None: the more of both kinds."""
+    if by16 is None:
+        return np.maximum(entered(v, False), entered(v, True))
+    group = group_of(by16)
+    m = np.zeros(-(-v.size // group) * group)
+    m[:v.size] = np.abs(v)
+    largest = np.repeat(m.reshape(-1, group).max(axis=1), group)[:v.size]
+    return np.maximum(largest * 2.0 ** -20, m.max() * 2.0 ** -37 if by16 else 0) + 2.0 ** -144
+
+
+def layer(x, ids, w, w1, w2, gated: bool, by16=None):
     """(Out, how far a binary32 evaluation may be off, before the last rounding).  w1 [E, up * H, D], w2 [E, D, H] values.
 
     Counted: one last place (2^-23 of the magnitudes: an addition may cut) per term of a sum; silu's slope is at most
-    1.1 and its own evaluation 8 last places; hidden values may be held in 11 bits under a power of two that is common
-    to a row (half a step: 2^-11 of the value, or 2^-25 of the row's largest where they are small).
+    1.1 and its own evaluation 8 last places; what values of x and hidden values may be off when they enter a product (`entered`).
     """
     E, D, H = w2.shape
     out, off = np.zeros(x.shape), np.zeros(x.shape)
@@ -128,13 +139,14 @@ def layer(x, ids, w, w1, w2, gated: bool):
                 continue
             p = 1.0 if w is None else float(w[t, j])
             up, mag = w1[e] @ x[t], np.abs(w1[e]) @ np.abs(x[t])
-            err = (D + 4) * last * mag
+            err = (D + 4) * last * mag + np.abs(w1[e]) @ entered(x[t], by16)
             g, ge = up[:H], err[:H]
             with np.errstate(over="ignore"):
                 s = g / (1 + np.exp(-g))
             u, ue = (up[H:], err[H:]) if gated else (np.ones(H), np.zeros(H))
             h = s * u
-            he = 1.1 * ge * (np.abs(u) + ue) + np.abs(s) * ue + np.abs(h) * (8 * last + 2.0 ** -11) + np.abs(h).max() * 2.0 ** -25
+            he = 1.1 * ge * (np.abs(u) + ue) + np.abs(s) * ue + np.abs(h) * 8 * last
+            he += entered(np.abs(h) + he, by16)
             out[t] += p * (w2[e] @ h)
             off[t] += abs(p) * (np.abs(w2[e]) @ (he + (H + ids.shape[1] + 4) * last * np.abs(h)))
     return out, off
