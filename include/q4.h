@@ -552,7 +552,8 @@ q4_status q4_gemm_f4_experts(const uint8_t* A, int64_t lda, const uint32_t* SA, 
  * tokens: many are served by q4_expert_sort and the products by experts.
  * Fast path (three kernels): 16-bit X, at most 1024 pairs, D and H up to 8704 (by 16: 7168; what shared memory holds of
  * four tokens), W1, W2 16-byte aligned and ldw1, ldw2 multiples of 16; anything else runs slower general kernels.  On the
- * fast path an activation (a value of X or h) enters the products within 2^-20 of the largest of its group of 32 (by 16: 16).
+ * fast path an activation (a value of X or h) enters the products within 2^-20 of the largest of its group of 32 values; by 16
+ * within that of its group of 16 or 2^-37 of the largest of its row (a token's X, a pair's h), whichever is more; or 2^-144.
  */
 q4_status q4_expert_layer_f4(const void* X, int64_t ldx, int32_t type, int32_t tokens, int32_t D, int32_t H,
                              const int32_t* ids, const float* w, int32_t topk, int32_t E, int32_t flags,

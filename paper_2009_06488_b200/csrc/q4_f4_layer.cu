@@ -13,8 +13,9 @@
 // of its digits to base 8, -4..3: codes 0 to 4 of e2m1 are 0, 1/2, 1, 3/2, 2.  (Parts made one after the other in floating
 // point, each the nearest to what is left, took three times the instructions.)
 // The parts are rows of the product's second operand and their results are added in binary32.  The scale is
-// that of the weights' kind: a power of two per 32, or per 16 one in e4m3 (17 powers, above 2^-17 of the row's
-// largest value) times a power of two for the row.
+// that of the weights' kind: a power of two per 32, or per 16 one in e4m3 times a power of two for the row.  e4m3 holds 18
+// powers of two, so that a group more than 2^17 below the row's largest value has the steps of one that is not: its rest is 2^-37
+// of the row's largest.  (20 bits are enough for what the layer writes, 11 at most; binary32 activations run the general kernels.)
 //
 // Every block sorts the pairs by expert for itself (a few hundred numbers).  A unit is up to NTOK pairs of one expert, a
 // tile 128 rows of its weights (gated: 64 of G and the same 64 of U) by PARTS * NTOK columns, the whole depth.  (A product

@@ -75,6 +75,23 @@ class Digits:
         return (np.abs(got - want) > off + (np.abs(want) + off) * 2.0 ** -11 + 2.0 ** -25).sum()
 
 
+def far_below(by16):
+    """(x, w1, w2): tokens whose first group holds 1 and meets weights that are 0, and whose second one holds values 2^-d."""
+    g = f4.group_of(by16)
+    r = np.random.default_rng(23)
+    x = np.zeros((40, 2 * g))
+    x[:, 0] = 1
+    x[:, g:] = r.uniform(1, 2, (40, g)) * 2.0 ** -np.arange(1.0, 41)[:, None]
+    x = (x * 2.0 ** 60).astype(np.float32).view(np.uint32) & 0xFFFF0000                       # to bfloat16, towards 0
+    x = x.view(np.float32).astype(np.float64) * 2.0 ** -60
+    c = np.zeros((g, 2 * g), dtype=np.uint8)
+    c[np.arange(g), g + np.arange(g)] = r.integers(1, 8, g)
+    one = np.full((g, 2), 0x38 if by16 else 127, dtype=np.uint8)
+    q1, s1 = f4.pack(c), f4.to_words(one)
+    q2, s2 = f4.pack(np.concatenate([2 * np.eye(g), 2 * np.eye(g)]).astype(np.uint8)), f4.to_words(np.full((2 * g, 1), one[0, 0], dtype=np.uint8))
+    return x, q1, s1, q2, s2
+
+
 @pytest.mark.parametrize("by16", [False, True])
 def test_seven_parts_keep_the_bound(by16):
     r = np.random.default_rng(5)
@@ -92,3 +109,11 @@ def test_the_cases_see_every_part(where, by16):
     assert c.outside(rounded()) == 0
     for parts in range(1, 7):
         assert c.outside(rounded(**{"parts_" + where: parts})) > 10
+
+
+def test_by_16_a_small_group_has_the_rows_steps():
+    """2^-20 of a group's largest is not kept where it is 2^-17 of the row's largest: 2^-37 of that is."""
+    x, q1, s1, q2, s2 = far_below(True)
+    off = np.abs(as_parts(x, True) - x)[:, 16:]
+    assert (off[30:] > x[30:, 16:].max(axis=1, keepdims=True) * 2.0 ** -20).any()
+    assert all((np.abs(as_parts(r[None], True)[0] - r) <= f4.entered(r, True)).all() for r in x)
