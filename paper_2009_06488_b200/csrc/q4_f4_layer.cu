@@ -322,7 +322,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 if (++ab == (uint32_t)L.bufs) { ab = 0; abph ^= 1u; }
                 mbar_wait_suspend(bar_act(ab), abph, abort_flag, p.status);
             }
-            const bool last_of_unit = tile + 1 == t1 || (tile + 1) / each != u;
+            const bool unit_follows = tile + 1 < t1 && (tile + 1) / each != u;
             mbar_wait(bar_tempty(acc), aph ^ 1u, abort_flag, p.status);
             for (int b = 0; b < nkb; ++b) {
                 mbar_wait(bar_full(st), ph, abort_flag, p.status);
@@ -346,8 +346,8 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                     }
                     tc_commit(bar_empty(st));
                     if (b == nkb - 1) {
-                        tc_commit(bar_tfull(acc));
-                        if (last_of_unit) tc_commit(bar_used(ab));
+                        if (unit_follows) tc_commit(bar_used(ab));
+                        tc_commit(bar_tfull(acc));         // the block's last arrival: it is waited for
                     }
                 }
                 __syncwarp();
