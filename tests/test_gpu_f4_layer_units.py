@@ -42,3 +42,27 @@ def test_five_units_and_more_of_one_tile_each(q4, gated, H):
     c.ids = np.random.default_rng(83).permutation(1024).reshape(128, 8).astype(np.int32)
     assert most_units(c.ids, 1024, 4, H * (2 if gated else 1)) >= 6 and most_units(c.ids, 1024, 4, 64) >= 6
     c.run(q4).check()
+
+
+# ------------------------------------------------------------------------------- buffers from unit to unit
+# T, topk, E, D, H, gated, by16, pairs per unit, units of a block in the first and the second kernel at least
+CHAINS = [(128, 8, 256, 64, 160, True, False, 8, 3, 2), (128, 8, 1024, 64, 100, True, False, 4, 6, 6), (128, 8, 1024, 300, 200, False, True, 4, 6, 6),
+          (50, 6, 300, 2880, 16, True, True, 4, 2, 2),         # four pairs' parts of the first kernel fill one buffer
+          (50, 6, 300, 24, 2880, False, True, 4, 2, 2),        # ... of the second
+          (128, 8, 100, 2048, 64, True, False, 8, 2, 2),       # eight pairs' of the first
+          (128, 8, 100, 100, 2048, False, False, 8, 2, 2)]
+
+
+@pytest.mark.parametrize("T,topk,E,D,H,gated,by16,per,up,down", CHAINS)
+def test_parts_of_one_unit_after_another(q4, T, topk, E, D, H, gated, by16, per, up, down):
+    """A unit's parts are written where an earlier unit's were read, with two buffers and with one."""
+    c = scaled(Case(T + E + D, T, topk, E, D, H, gated, by16, "bf16"), E)
+    assert (T * topk > 3 * E) == (per == 8)
+    if T * topk <= E:                            # every expert once
+        c.ids = np.random.default_rng(D).permutation(E)[:T * topk].reshape(T, topk).astype(np.int32)
+    assert most_units(c.ids, E, per, H * (2 if gated else 1)) >= up and most_units(c.ids, E, per, D) >= down
+    c.run(q4).check()
+    first = c.Out.clone()
+    c.Out.fill_(9)
+    c.run(q4)
+    assert (c.Out == first).all()
