@@ -101,8 +101,8 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         uint32_t st = 0, ph = 0;
         for (int tile = first; walk.get(tile, t) && !lds32(abort_flag); tile += step)
             for (int b = 0; b < nkb; ++b) {
-                mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
-                if (elect_one()) {
+                const bool ok = mbar_wait_or_leave(bar_empty(st), ph ^ 1u, abort_flag, g.status);
+                if (elect_one() && ok) {
                     const uint32_t dst = sbase + st * C::STAGE;
                     mbar_expect_tx(bar_full(st), (uint32_t)((WR + NB) * ROWB));
                     tma_load_2d(dst, &tmB, (k_lo + b) * ROWB, (int)t.brow, bar_full(st));
@@ -111,6 +111,7 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 __syncwarp();
                 if (++st == C::STAGES) { st = 0; ph ^= 1u; }
             }
+        settle(abort_flag);
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer
         const uint64_t desc0 = make_kmajor_sw128_desc(sbase), scales0 = scales_desc(sbase + (WR + NB) * ROWB);
@@ -118,7 +119,7 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         for (int tile = first; walk.get(tile, t) && !lds32(abort_flag); tile += step) {
             mbar_wait(bar_tempty(acc), aph ^ 1u, abort_flag, g.status);
             for (int b = 0; b < nkb; ++b) {
-                mbar_wait(bar_full(st), ph, abort_flag, g.status);
+                mbar_wait_or_leave(bar_full(st), ph, abort_flag, g.status);
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4)), bdesc = adesc + (WR * ROWB >> 4);
@@ -142,6 +143,7 @@ gemm_f4_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             aph ^= acc;
             acc ^= 1u;
         }
+        settle(abort_flag);
     } else if (warp < 8) {
         // ------------------------------------------------------------ scales
         const int part = warp & 1, team = (warp - 2) >> 1;     // 0: Bt's rows, 1: A's

@@ -170,8 +170,8 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             const int few = (rows + FEW - 1) / FEW;
             const uint32_t bytes = (uint32_t)((rows > TMC - FEW ? TMC : few * FEW) + C::BSH) * ROWB;
             for (int b = 0; b < nkb; ++b) {
-                mbar_wait(bar_empty(st), ph ^ 1u, abort_flag, g.status);
-                if (elect_one()) {
+                const bool ok = mbar_wait_or_leave(bar_empty(st), ph ^ 1u, abort_flag, g.status);
+                if (elect_one() && ok) {
                     const uint32_t full = full_leader + 8u * st;
                     mbar_expect_tx_cluster(full, bytes);
                     const uint32_t dst = sbase + st * C::STAGE;
@@ -185,6 +185,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 if (++st == C::STAGES) { st = 0; ph ^= 1u; }
             }
         }
+        settle(abort_flag);
     } else if (warp == 1) {
         // ------------------------------------------------------------ pair MMA issuer (leader)
         if (rank == 0) {
@@ -194,7 +195,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 mbar_wait(bar_tempty(acc), aph ^ 1u, abort_flag, g.status);
                 tc_fence_after();
                 for (int b = 0; b < nkb; ++b) {
-                    mbar_wait_cl(bar_full(st), ph, abort_flag, g.status);
+                    mbar_wait_or_leave<true>(bar_full(st), ph, abort_flag, g.status);
                     tc_fence_after();
                     if (elect_one()) {
                         const uint64_t adesc = desc0 + (uint64_t)(st * (uint32_t)(C::STAGE >> 4)), bdesc = adesc + (TMC * ROWB >> 4);
@@ -218,6 +219,7 @@ gemm_f4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 }
                 if (++acc == C::ACCS) { acc = 0; aph ^= 1u; }
             }
+            settle(abort_flag);
         }
     } else if (warp < 8) {
         // ------------------------------------------------------------ scales

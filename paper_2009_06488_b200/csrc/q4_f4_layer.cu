@@ -308,6 +308,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
                 if (++st == (uint32_t)STAGES) { st = 0; ph ^= 1u; }
             }
         }
+        settle(abort_flag);
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer
         const uint64_t desc0 = make_kmajor_sw128_desc(sbase), act0 = make_kmajor_sw128_desc(act_s), scales0 = scales_desc(atoms_s),
@@ -357,6 +358,7 @@ layer_kernel(const __grid_constant__ CUtensorMap tmW, const LayerLaunch L)
             aph ^= acc;
             acc ^= 1u;
         }
+        settle(abort_flag);
     } else if (warp < 4) {
         // ------------------------------------------------------------ scales
         // (the wait for the stage before told that stages up to STAGES + 2 back are consumed: a parity cannot be an older round's)

@@ -118,6 +118,13 @@ __device__ __forceinline__ bool mbar_wait_suspend(uint32_t bar, uint32_t parity,
     }
     return true;
 }
+// At the end of a role that issues copies or products, behind a wait that has run out: about 1 ms for those under way to end,
+// ahead of the meeting behind which the block's tensor memory is freed and its shared memory goes.
+__device__ __forceinline__ void settle(uint32_t abort_flag)
+{
+    if (!lds32(abort_flag)) return;
+    for (const long long t0 = clock64(); clock64() - t0 < kWaitShort;) {}
+}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y,
                                             uint32_t bar)
 {
@@ -291,6 +298,16 @@ __device__ __forceinline__ bool mbar_wait_cl(uint32_t bar, uint32_t parity, uint
         }
     }
     return true;
+}
+// A bounded wait that fails at once where one has run out in the block before, so that a depth of millions of stages is left
+// soon.  Copies are not issued behind a failed one; products are (in the block's own memory, of no meaning: a branch around
+// them costs the few-rows kernel 1 to 2 %).  CLUSTER: the arrivals may come from the peer CTA.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool mbar_wait_or_leave(uint32_t bar, uint32_t parity, uint32_t abort_flag, unsigned* status)
+{
+    if (CLUSTER ? mbar_try_cl(bar, parity) : mbar_try(bar, parity)) return true;
+    if (lds32(abort_flag)) return false;
+    return CLUSTER ? mbar_wait_cl(bar, parity, abort_flag, status) : mbar_wait(bar, parity, abort_flag, status);
 }
 __device__ __forceinline__ void cluster_sync_all()
 {
