@@ -532,7 +532,7 @@ q4_status q4_gemm_f4(const uint8_t* A, int64_t lda, const uint32_t* SA, int64_t 
  * The product by experts: rows starts[e] .. starts[e + 1] of A and C (starts: device, E + 1 non-decreasing values of
  * 0 .. M) are multiplied with expert e's weights, rows e * N .. of Bt [E * N][ldb], whose words of scales are at the same
  * rows of SB, its factor FB[e].  Rows of C outside every segment are left untouched; experts without rows cost nothing.
- * E <= Q4_MAX_EXPERTS.
+ * E <= Q4_MAX_EXPERTS, K <= 2^30.
  */
 q4_status q4_gemm_f4_experts(const uint8_t* A, int64_t lda, const uint32_t* SA, int64_t ldsa,
                              const uint8_t* Bt, int64_t ldb, const uint32_t* SB, int64_t ldsb, int32_t flags,

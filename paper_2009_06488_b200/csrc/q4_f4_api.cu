@@ -18,6 +18,9 @@ q4_status done(cudaError_t e) { return e == cudaSuccess ? Q4_OK : Q4_ERR_CUDA; }
 int64_t bytes_of(int64_t cols) { return (cols + 1) / 2; }
 // (the kernels' indexes pass a size by less than a tile)
 constexpr int32_t MOST = INT32_MAX - 512;
+// A tile's depth by experts is one block's, and its end is waited for for 4e9 clk at most: 2^22 stages of 500 to 720 clk.  (A dense
+// product that deep has few rows, whose depth goes to eight blocks.)
+constexpr int32_t DEEPEST_BY_EXPERTS = 1 << 30;
 
 q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* stream)
 {
@@ -29,7 +32,7 @@ q4_status run_product(f4::GemmParams& p, int32_t flags, const char* call, void* 
     if (!p.A || !p.Bt || !p.SA || !p.SB || !p.C) return Q4_ERR_INVALID_ARG;
     if (!aligned(p.SA, 4) || !aligned(p.SB, 4) || !aligned(p.FA, 4) || !aligned(p.FB, 4) || !aligned(p.starts, 4) ||
         !aligned(p.C, f8::type_size(p.c_type))) return Q4_ERR_ALIGNMENT;
-    if (p.N > MOST || p.K > MOST) return Q4_ERR_RANGE;
+    if (p.N > MOST || p.K > MOST || (p.E && p.K > DEEPEST_BY_EXPERTS)) return Q4_ERR_RANGE;
     p.status = device_status_ptr();
     if (!p.status) return Q4_ERR_CUDA;
     const int variant = kernel_variant();
