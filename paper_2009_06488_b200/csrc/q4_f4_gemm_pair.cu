@@ -401,8 +401,6 @@ static q4_status launch_pair(const PairParams& p, const CUtensorMap& a, const CU
 
 using namespace f4;
 
-namespace f8 { bool make_out_map(CUtensorMap* tm, void* base, int type, int64_t ldc, int64_t rows, int cols); }
-
 bool gemm_f4_pair_supported(const f4::GemmParams& g)
 {
     // A's rows of a tile may pass M by up to a tile; the maps count rows in 32 bits

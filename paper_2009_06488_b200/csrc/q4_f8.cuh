@@ -2,6 +2,7 @@
 // expert-layer kernels: element types, eight-at-a-time loads and stores, launch parameters.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -271,6 +272,9 @@ struct GemmF8Params {
     const int32_t* starts;         // E + 1 row (kExpertRows) or depth (kExpertDepth) positions
     unsigned* status;
 };
+
+// Tensor map of C [rows x cols] (a q4_type) for stores of 32 rows x 128 bytes out of a 128-byte-swizzled staging slice.
+bool make_out_map(CUtensorMap* tm, void* base, int type, int64_t ldc, int64_t rows, int cols);
 
 }  // namespace f8
 

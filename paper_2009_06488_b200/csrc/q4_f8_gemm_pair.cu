@@ -739,7 +739,6 @@ gemm_f8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
 }
 
-// C [rows x cols], box = 128 bytes x 32 rows, read from a 128-byte-swizzled staging slice.
 bool make_out_map(CUtensorMap* tm, void* base, int type, int64_t ldc, int64_t rows, int cols)
 {
     using Fn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
