@@ -10,9 +10,9 @@
 //
 // One persistent CTA per SM walks the tiles; with SPLIT a cluster of CTAs shares one tile's depth and adds its partial
 // tiles through distributed shared memory, in order (a product of few tiles).
-// Bound: HBM.  A product of 128 rows takes about 118 clk for 64 depth values up to NB = 64 and 128 at 128, 39 bytes of weights
-// per clk and SM, where HBM brings 23.  64 experts of 2048 x 2048, sixteen tokens of eight: 20 us = 6.3 TB/s; one token through
-// 4096 x 4096, by 16: 5.6 us.
+// Bound: HBM, behind the grid's start and ends.  A product of 128 rows takes about 118 clk for 64 depth values up to NB = 64 and 128
+// at 128, 39 bytes of weights per clk and SM, where HBM brings 23.  Sixteen tokens of eight, 64 experts by 16 whose weights change
+// from call to call: 2048 x 2048 23.3 us = 5.2 TB/s, 2048 x 1024 14.4 us = 4.2; one token through 4096 x 4096, by 16: 5.6 us.
 #include <cuda.h>
 
 #include "q4_f4_tc.cuh"

@@ -15,9 +15,9 @@
 //
 // Bound: the ring of stages and a tile's end.  A stage of a wide tile lasts about 720 clk where its four products take 512 (without
 // the scales' loads 8192^3 takes 169 us; with four stages instead of five 210; L2 runs at a quarter of its rate), and the only
-// wide accumulator that fits beside the scales is drained for some 3000 clk per tile.  8192^3 to bf16: by 16 200 us = 5.5 PFLOP/s, by 32 184 us = 6.0 (four times the bf16
-// product's measured rate is 6.6); under the power cap 239.  Scales by TMA boxes: 290 us; two accumulators of 192 columns:
-// as long as one of 256.
+// wide accumulator that fits beside the scales is drained for some 3000 clk per tile.  8192^3 to bf16: by 16 195 to 206 us = 5.3 to 5.6
+// PFLOP/s, by 32 183 to 186 us = 5.9 to 6.0 (four times the bf16 product's measured rate is 6.6); under the power
+// cap 222 to 245.  Scales by TMA boxes: 290 us; two accumulators of 192 columns: as long as one of 256.
 #include <cuda.h>
 
 #include "q4_f4_tc.cuh"

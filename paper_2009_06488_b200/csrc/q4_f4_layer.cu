@@ -29,8 +29,8 @@
 //   warps 8..23   activations  the next unit's parts and scales, while this one's are multiplied
 //
 // Bound: HBM, behind each kernel's start (sorting, the first unit's parts: 7 us of the first) and beside blocks with a tile
-// more than others (7 against 6.2 on average).  64 experts of 2048 -> 1024 (gated) -> 2048: sixteen tokens 44 us = 4.2 TB/s of
-// weights, one token (8 experts) 19 us.  What was tried: the sum in kernel 2 by the block that finishes columns last (its tail
+// more than others (7 against 6.2 on average).  64 experts of 2048 -> 1024 (gated) -> 2048: sixteen tokens 46 us = 3.6 TB/s of
+// weights (50 experts are hit), one token (8 experts) 19 us.  What was tried: the sum in kernel 2 by the block that finishes columns last (its tail
 // 6 to 14 us), or by warps of their own that count each token's pairs (16 tokens 47.5 against 46.6 us, one 20.1 against 19.1,
 // 32 by 16 68 against 62); all in one cooperative kernel (63); later stages to L2 ahead of their copies (54); codes to
 // binary16 in registers and warp-level matrix instructions, the depth spread over a block's warps (86) or a strip of rows per
